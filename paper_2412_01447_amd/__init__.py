@@ -27,12 +27,18 @@ __all__ = [
     "pld_verify_sample_finish", "PLD_MAX_SAMPLE_ROWS", "pld_select_prefix", "pld_draft_prefix",
     "pld_commit", "pld_accept_commit",
     "PLD_MAX_MATCH",
+    "pld_model_version", "pld_cache_write", "pld_cache_attn", "pld_cache_attn_workspace_bytes",
+    "pld_cache_attn_rows", "pld_token_logprobs", "pld_token_logprobs_workspace_bytes", "PLD_E4M3",
+    "PLD_ROPE_HALVES", "PLD_ROPE_NEIGHBOURS", "PLD_MAX_TOP",
 ]
 
 PLD_OK, PLD_ERR_INVALID, PLD_ERR_ALIGN, PLD_ERR_WORKSPACE, PLD_ERR_LAUNCH, PLD_ERR_SCRATCH = range(6)
 NOALLOC_MAX_KEYS = 65536        # pld_verify_greedy_noalloc: B*(K+1) limit
 PLD_F32, PLD_BF16 = 0, 1
+PLD_E4M3 = 2                    # a quantised cache's elements (include/pld_model.h)
 PLD_AGG_SUM, PLD_AGG_MAX = 0, 1
+PLD_ROPE_HALVES, PLD_ROPE_NEIGHBOURS = 0, 1
+PLD_MAX_TOP = 64                # alternatives per row of pld_token_logprobs
 PLD_MAX_NGRAM, PLD_MAX_HIDDEN, PLD_MAX_BATCH, PLD_MAX_DRAFT_SPLIT = 8, 16384, 4096, 1024
 PLD_MAX_SAMPLE_ROWS = 16384
 PLD_MAX_MATCH = 1024
@@ -45,6 +51,17 @@ _lib = None
 
 _vp, _i64, _int, _sz, _f32 = (ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t,
                               ctypes.c_float)
+
+
+class _Cache(ctypes.Structure):
+    """struct pld_cache of include/pld_model.h."""
+    _fields_ = [("k", _vp), ("v", _vp), ("dtype", _int), ("k_scale", _vp), ("v_scale", _vp),
+                ("scale_page_stride", _i64), ("page_stride", _i64), ("slot_stride", _i64),
+                ("head_stride", _i64), ("table", _vp), ("table_stride", _i64), ("num_pages", _int),
+                ("page_size", _int), ("max_pages", _int), ("heads", _int), ("head_dim", _int)]
+
+
+_cachep = ctypes.POINTER(_Cache)
 
 _SIGNATURES = {
     "pld_version": ([], _int),
@@ -94,6 +111,18 @@ _SIGNATURES = {
     "pld_draft_attn": ([_vp, _i64, _vp, _int, _int, _int, _vp, _i64, _i64, _i64, _int, _int, _f32,
                         _int, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _int, _vp, _sz, _vp],
                        _int),
+    "pld_model_version": ([], _int),
+    "pld_cache_write": ([_cachep, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _f32,
+                         _vp, _i64, _int, _int, _int, _vp, _vp, _int, _int, _int, _vp, _i64, _i64,
+                         _vp], _int),
+    "pld_cache_attn_workspace_bytes": ([_int, _int, _int, _int, _int], _sz),
+    "pld_cache_attn": ([_cachep, _vp, _i64, _i64, _vp, _vp, _int, _int, _int, _f32, _f32, _int, _vp,
+                        _i64, _i64, _vp, _vp, _sz, _vp], _int),
+    "pld_cache_attn_rows": ([_cachep, _vp, _i64, _i64, _vp, _vp, _vp, _int, _vp, _int, _int, _int,
+                             _f32, _f32, _int, _vp, _i64, _i64, _i64, _vp], _int),
+    "pld_token_logprobs_workspace_bytes": ([_int, _int, _int, _int, _int], _sz),
+    "pld_token_logprobs": ([_vp, _int, _i64, _i64, _int, _int, _vp, _vp, _int, ctypes.c_double, _vp,
+                            _vp, _int, _vp, _vp, _vp, _sz, _vp], _int),
 }
 
 
@@ -173,6 +202,7 @@ class Prepared:
         self.name = name
         # converted once, to the declared types; a function object of its own, without
         # argument types, passes them on as they are
+        # (a struct is passed by a pointer, which keeps it)
         self.args = tuple(a if a is None else t(a) for a, t in zip(args, _SIGNATURES[name][0]))
         self.fn = _load()[name]
 
@@ -548,3 +578,217 @@ def pld_verify_accept(draft, draft_len, accept_len, out_tokens, out_count, works
     return _run("pld_verify_accept", (_ptr(draft), _ptr(draft_len), B, K, _ptr(accept_len),
           _ptr(out_tokens), _ptr(out_count), _ptr(workspace), _nbytes(workspace),
           _stream(stream),), prepare)
+
+
+# ------------------------------------------------- the verification pass's model side
+def _on_one_device(stream, **tensors):
+    """The calls of include/pld_model.h take many tensors at once: all of them on one
+    device, which is the current one (the kernels run there)."""
+    torch = _torch or _th()
+    dev = None
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise TypeError(f"{name}: expected a device tensor, got one on {t.device}")
+        if dev is None:
+            dev = t.get_device()
+        elif t.get_device() != dev:
+            raise TypeError(f"{name} is on cuda:{t.get_device()}, the other tensors on cuda:{dev}")
+    if dev != torch.cuda.current_device():
+        raise TypeError(f"the tensors are on cuda:{dev}, the current device is "
+                        f"cuda:{torch.cuda.current_device()}")
+    sd = getattr(stream, "device_index", dev)
+    if sd != dev:
+        raise TypeError(f"the stream is on cuda:{sd}, the tensors on cuda:{dev}")
+
+
+def _ints(t, name, *shape):
+    """A contiguous int32 tensor of `shape` (None: absent)."""
+    torch = _torch or _th()
+    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != shape
+                          or not t.is_contiguous()):
+        raise TypeError(f"{name} must be a contiguous int32 tensor of shape {shape}")
+
+
+def _floats(t, name, *shape):
+    torch = _torch or _th()
+    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != shape
+                          or not t.is_contiguous()):
+        raise TypeError(f"{name} must be a contiguous float32 tensor of shape {shape}")
+
+
+def _rows_of(t, name, B, n, heads, D):
+    """Strides (sequence, row) of a bf16 [B][n][heads][D] tensor whose heads follow each other."""
+    torch = _torch or _th()
+    if t.dtype != torch.bfloat16 or tuple(t.shape) != (B, n, heads, D):
+        raise TypeError(f"{name}: expected bfloat16 {(B, n, heads, D)}, got {t.dtype} "
+                        f"{tuple(t.shape)}")
+    st = t.stride()
+    if st[3] != 1 or (heads > 1 and st[2] != D):
+        raise TypeError(f"{name}: a row's heads must follow each other")
+    return st
+
+
+def _cache_of(k_cache, v_cache, table, k_scale, v_scale, B):
+    """struct pld_cache of [page][slot][head][D] tensors (any strides but the last)."""
+    torch = _torch or _th()
+    if k_cache.dim() != 4 or k_cache.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+        raise TypeError("k_cache must be a bfloat16 or float8_e4m3fn [pages][slots][heads][D] tensor")
+    P, page, heads, D = k_cache.shape
+    ks = k_cache.stride()
+    if ks[3] != 1:
+        raise TypeError("k_cache: the last dimension must be contiguous")
+    if v_cache is not None and (v_cache.dtype != k_cache.dtype or v_cache.shape != k_cache.shape
+                                or v_cache.stride() != ks):
+        raise TypeError("v_cache must have k_cache's type, shape and strides")
+    _need(table, torch.int32, "table", 2)
+    if table.shape[0] != B:
+        raise TypeError(f"table must be [B = {B}][pages], got {tuple(table.shape)}")
+    q8 = k_cache.dtype == torch.float8_e4m3fn
+    sp = 0
+    for t, name, used in ((k_scale, "k_scale", True), (v_scale, "v_scale", v_cache is not None)):
+        if not q8:
+            if t is not None:
+                raise TypeError(f"{name}: a bfloat16 cache has no scales")
+        elif used or t is not None:
+            if t is None or t.dtype != torch.float32 or tuple(t.shape) != (P, heads, page):
+                raise TypeError(f"{name} must be a float32 [pages][heads][slots] tensor")
+            if t.stride(2) != 1 or (heads > 1 and t.stride(1) != page):
+                raise TypeError(f"{name}: a page's scales must follow each other")
+            if sp and t.stride(0) != sp:
+                raise TypeError("k_scale and v_scale must have the same strides")
+            sp = t.stride(0)
+    return _Cache(_ptr(k_cache), _ptr(v_cache), PLD_E4M3 if q8 else PLD_BF16, _ptr(k_scale),
+                  _ptr(v_scale), sp, ks[0], ks[1], ks[2], _ptr(table), table.stride(0), P, page,
+                  table.shape[1], heads, D)
+
+
+def pld_model_version():
+    return _load().pld_model_version()
+
+
+def pld_cache_attn_workspace_bytes(B, n, Hq, heads, head_dim):
+    return int(_load().pld_cache_attn_workspace_bytes(B, n, Hq, heads, head_dim))
+
+
+def pld_token_logprobs_workspace_bytes(B, n, V, dtype, top):
+    return int(_load().pld_token_logprobs_workspace_bytes(B, n, V, dtype, top))
+
+
+def pld_cache_write(q, k, v, k_cache, v_cache, table, lens, q_out, draft_len=None, k_scale=None,
+                    v_scale=None, q_norm=None, k_norm=None, eps=1e-6, rope=None,
+                    rope_pairs=PLD_ROPE_HALVES, stream=None, prepare=False):
+    """q bf16 [B][n][Hq][D], k and v [B][n][heads][D] of the rows at positions lens[b]-1+i,
+    i <= draft_len[b]: heads normed (q_norm, k_norm bf16 [D]) and turned by rope (fp32
+    [positions][rot_dim], cosines then sines), keys and values stored in the pages
+    table[b][position / slots] of k_cache / v_cache [pages][slots][heads][D] (bfloat16, or
+    float8_e4m3fn with scales fp32 [pages][heads][slots]), queries written to q_out."""
+    torch = _torch or _th()
+    _on_one_device(stream, q=q, k=k, v=v, k_cache=k_cache, v_cache=v_cache, table=table, lens=lens,
+                   q_out=q_out, draft_len=draft_len, k_scale=k_scale, v_scale=v_scale,
+                   q_norm=q_norm, k_norm=k_norm, rope=rope)
+    if q.dim() != 4:
+        raise TypeError("q must be [B][n][Hq][D]")
+    B, n, Hq, D = q.shape
+    cache = _cache_of(k_cache, v_cache, table, k_scale, v_scale, B)
+    if cache.head_dim != D:
+        raise TypeError(f"q has heads of {D} elements, the cache of {cache.head_dim}")
+    qs, ks = _rows_of(q, "q", B, n, Hq, D), _rows_of(k, "k", B, n, cache.heads, D)
+    vs, os_ = _rows_of(v, "v", B, n, cache.heads, D), _rows_of(q_out, "q_out", B, n, Hq, D)
+    _ints(lens, "lens", B)
+    _ints(draft_len, "draft_len", B)
+    for t, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+        if t is not None and (t.dtype != torch.bfloat16 or tuple(t.shape) != (D,)
+                              or not t.is_contiguous()):
+            raise TypeError(f"{name} must be a contiguous bfloat16 tensor of {D} elements")
+    rs = (0, 0) if rope is None else _need(rope, torch.float32, "rope", 2)
+    n_pos, rot = (0, 0) if rope is None else rope.shape
+    if rope is not None and n_pos == 1:
+        rs = (rot, 1)
+    return _run("pld_cache_write", (
+        cache, _ptr(q), qs[0], qs[1], _ptr(k), ks[0], ks[1], _ptr(v), vs[0], vs[1], _ptr(q_norm),
+        _ptr(k_norm), float(eps), _ptr(rope), rs[0], n_pos, rot, int(rope_pairs), _ptr(lens),
+        _ptr(draft_len), B, n, Hq, _ptr(q_out), os_[0], os_[1], _stream(stream)), prepare)
+
+
+def pld_cache_attn(q, k_cache, v_cache, table, lens, out, workspace, draft_len=None, k_scale=None,
+                   v_scale=None, lse=None, scale=None, softcap=0.0, window=0, stream=None,
+                   prepare=False):
+    """Attention of the rows q bf16 [B][n][Hq][D] (positions lens[b]-1+i, i <= draft_len[b])
+    over the cache: out like q, lse fp32 [B][n][Hq]; scale defaults to 1 / sqrt(D), softcap
+    and window are off at 0."""
+    _on_one_device(stream, q=q, k_cache=k_cache, v_cache=v_cache, table=table, lens=lens, out=out,
+                   workspace=workspace, draft_len=draft_len, k_scale=k_scale, v_scale=v_scale,
+                   lse=lse)
+    if q.dim() != 4:
+        raise TypeError("q must be [B][n][Hq][D]")
+    B, n, Hq, D = q.shape
+    cache = _cache_of(k_cache, v_cache, table, k_scale, v_scale, B)
+    if cache.head_dim != D:
+        raise TypeError(f"q has heads of {D} elements, the cache of {cache.head_dim}")
+    qs, os_ = _rows_of(q, "q", B, n, Hq, D), _rows_of(out, "out", B, n, Hq, D)
+    _ints(lens, "lens", B)
+    _ints(draft_len, "draft_len", B)
+    _floats(lse, "lse", B, n, Hq)
+    return _run("pld_cache_attn", (
+        cache, _ptr(q), qs[0], qs[1], _ptr(lens), _ptr(draft_len), B, n, Hq,
+        D ** -0.5 if scale is None else float(scale), float(softcap), int(window), _ptr(out),
+        os_[0], os_[1], _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream)), prepare)
+
+
+def pld_cache_attn_rows(q, k_cache, table, lens, row, heads, lse, attn, k_scale=None, scale=None,
+                        softcap=0.0, window=0, stream=None, prepare=False):
+    """The attention weights of query heads `heads` (int32 [R]) at row row[b] of each sequence,
+    from the q and lse of pld_cache_attn: attn fp32 [B][R][n_keys], as pld_rank_attn takes it."""
+    torch = _torch or _th()
+    _on_one_device(stream, q=q, k_cache=k_cache, table=table, lens=lens, row=row, heads=heads,
+                   lse=lse, attn=attn, k_scale=k_scale)
+    if q.dim() != 4:
+        raise TypeError("q must be [B][n][Hq][D]")
+    B, n, Hq, D = q.shape
+    cache = _cache_of(k_cache, None, table, k_scale, None, B)
+    if cache.head_dim != D:
+        raise TypeError(f"q has heads of {D} elements, the cache of {cache.head_dim}")
+    qs = _rows_of(q, "q", B, n, Hq, D)
+    _ints(lens, "lens", B)
+    _ints(row, "row", B)
+    R = heads.numel()
+    _ints(heads, "heads", R)
+    _floats(lse, "lse", B, n, Hq)
+    as_ = _need(attn, torch.float32, "attn", 3)
+    if tuple(attn.shape[:2]) != (B, R):
+        raise TypeError(f"attn must be [B = {B}][R = {R}][n_keys], got {tuple(attn.shape)}")
+    return _run("pld_cache_attn_rows", (
+        cache, _ptr(q), qs[0], qs[1], _ptr(lens), _ptr(row), _ptr(heads), R, _ptr(lse), B, n, Hq,
+        D ** -0.5 if scale is None else float(scale), float(softcap), int(window), _ptr(attn),
+        as_[0], as_[1], attn.shape[2], _stream(stream)), prepare)
+
+
+def pld_token_logprobs(logits, tokens, logprob, workspace, count=None, temperature=1.0,
+                       entropy=None, top_ids=None, top_logprobs=None, stream=None, prepare=False):
+    """Log probabilities of tokens [B][n] under softmax(logits / temperature), rows i < count[b],
+    with the rows' entropy and their most likely tokens (top_ids, top_logprobs [B][n][top])."""
+    torch = _torch or _th()
+    _on_one_device(stream, logits=logits, tokens=tokens, logprob=logprob, workspace=workspace,
+                   count=count, entropy=entropy, top_ids=top_ids, top_logprobs=top_logprobs)
+    if logits.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("logits must be float32 or bfloat16")
+    ls = _need(logits, logits.dtype, "logits", 3)
+    B, n, V = logits.shape
+    _ints(tokens, "tokens", B, n)
+    _ints(count, "count", B)
+    _floats(logprob, "logprob", B, n)
+    _floats(entropy, "entropy", B, n)
+    if (top_ids is None) != (top_logprobs is None):
+        raise TypeError("top_ids and top_logprobs go together")
+    top = 0 if top_ids is None else top_ids.shape[-1]
+    if top:
+        _ints(top_ids, "top_ids", B, n, top)
+        _floats(top_logprobs, "top_logprobs", B, n, top)
+    dtype = PLD_F32 if logits.dtype == torch.float32 else PLD_BF16
+    return _run("pld_token_logprobs", (
+        _ptr(logits), dtype, ls[0], ls[1], V, n, _ptr(tokens), _ptr(count), B, float(temperature),
+        _ptr(logprob), _ptr(entropy), top, _ptr(top_ids) if top else None,
+        _ptr(top_logprobs) if top else None, _ptr(workspace), _nbytes(workspace),
+        _stream(stream)), prepare)

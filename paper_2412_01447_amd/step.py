@@ -13,7 +13,7 @@ from . import (DRAFT_MAX_PART, DRAFT_MAX_TOK_STRIDE, PLD_AGG_SUM, PLD_BF16, PLD_
                pld_draft_prefix, pld_draft_workspace_bytes, pld_emit_draft, pld_find_candidates,
                pld_find_scratch_bytes, pld_rank_attn, pld_rank_hidden, pld_score_attn,
                pld_score_both, pld_score_hidden, pld_select_best, pld_select_draft, pld_select_prefix,
-               pld_verify_accept,
+               pld_token_logprobs, pld_token_logprobs_workspace_bytes, pld_verify_accept,
                pld_verify_argmax, pld_verify_greedy, pld_verify_sample, pld_verify_sample_finish,
                pld_verify_sample_stats, pld_verify_sample_workspace_bytes, pld_workspace_bytes)
 
@@ -67,6 +67,10 @@ class DraftStep:
         self.temperature = None
         self.uniforms = None
         self.row_sample = None
+        # the emitted tokens' log probabilities (set_logprobs)
+        self.logprob = None
+        self.logprob_entropy = self.top_ids = self.top_logprobs = self.logprob_ws = None
+        self.logprob_temperature = 1.0
 
     def set_sampling(self, temperature, V, bf16, uniforms=None):
         """Verify by sampling at `temperature` (None: greedy again).  `uniforms` is a
@@ -85,6 +89,35 @@ class DraftStep:
         self.row_sample = torch.full((self.B, self.K + 1), -1, dtype=torch.int32,
                                      device=self.device)
         self.temperature = float(temperature)
+
+    def set_logprobs(self, V, bf16, top=0, temperature=1.0):
+        """From now on every step also gives its emitted tokens' log probabilities under
+        softmax(logits / temperature): self.logprob [B][K+1], self.logprob_entropy [B][K+1]
+        and, for top > 0, the rows' most likely tokens self.top_ids and self.top_logprobs
+        [B][K+1][top] (rows past out_count keep what they held).  V None: no longer."""
+        if V is None:
+            self.logprob = None
+            return
+        B, n = self.B, self.K + 1
+        f32 = dict(dtype=torch.float32, device=self.device)
+        need = pld_token_logprobs_workspace_bytes(B, n, V, PLD_BF16 if bf16 else PLD_F32, top)
+        if need == 0:
+            raise ValueError(f"no log probabilities for V = {V}, top = {top}")
+        self.logprob_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        self.logprob = torch.zeros((B, n), **f32)
+        self.logprob_entropy = torch.zeros((B, n), **f32)
+        self.top_ids = self.top_logprobs = None
+        if top:
+            self.top_ids = torch.full((B, n, top), -1, dtype=torch.int32, device=self.device)
+            self.top_logprobs = torch.zeros((B, n, top), **f32)
+        self.logprob_temperature = float(temperature)
+
+    def token_logprobs(self, logits, stream=None, prepare=False):
+        """The log probabilities of set_logprobs for out_tokens under `logits`."""
+        return pld_token_logprobs(logits, self.out_tokens, self.logprob, self.logprob_ws,
+                                  count=self.out_count, temperature=self.logprob_temperature,
+                                  entropy=self.logprob_entropy, top_ids=self.top_ids,
+                                  top_logprobs=self.top_logprobs, stream=stream, prepare=prepare)
 
     def min_split(self):
         """The fewest blocks per sequence the one-call drafting accepts."""
@@ -137,9 +170,11 @@ class DraftStep:
             pld_verify_sample(logits, self.draft, self.draft_len, self.temperature, self.uniforms,
                               self.accept_len, self.out_tokens, self.out_count, self.workspace,
                               row_sample=self.row_sample, stream=stream)
-            return
-        pld_verify_greedy(logits, self.draft, self.draft_len, self.accept_len, self.out_tokens,
-                          self.out_count, self.workspace, stream=stream)
+        else:
+            pld_verify_greedy(logits, self.draft, self.draft_len, self.accept_len,
+                              self.out_tokens, self.out_count, self.workspace, stream=stream)
+        if self.logprob is not None:
+            self.token_logprobs(logits, stream=stream)
 
     # the halves of the ranking and verification calls (same results, one kernel each)
     def score_hidden(self, hidden, lens, threshold=float("-inf"), stream=None):
@@ -322,7 +357,7 @@ class DraftStep:
         except where "find" (past 16384 tokens), the one-call "draft" past its team and
         prompt lookup's "draft" past one launch take several: the same work as run(),
         with every argument marshalled once so that issuing a step costs only the
-        launches.
+        launches.  After set_logprobs the last entry is the emitted tokens' log probabilities.
         commit=(limit, stats) adds the commit of the generation loop (with greedy
         verification, fused into the acceptance's launch: pld_accept_commit)."""
         P = dict(stream=stream, prepare=True)
@@ -368,6 +403,8 @@ class DraftStep:
             else:
                 ops.append(("commit", pld_commit(tokens, lens, self.out_tokens, self.out_count,
                                                  limit=limit, stats=stats, **P)))
+        if self.logprob is not None:
+            ops.append(("token_logprobs", self.token_logprobs(logits, **P)))
         return ops
 
     def host(self):
@@ -384,7 +421,7 @@ class DraftStep:
 
 def decode_loop(step, tokens, lens, limit, model, hidden=None, attn=None, ngram=(1, 1),
                 agg=PLD_AGG_SUM, threshold=float("-inf"), prefix_match=None, stats=None,
-                max_steps=1 << 20, check_every=4, stream=None, on_step=None):
+                max_steps=1 << 20, check_every=4, stream=None, on_step=None, refresh=None):
     """The generation loop around the drafting step, on the device: draft, verify
     against `model(step, lens)` (the target model's logits over context + draft),
     commit the emitted tokens; until every sequence has reached `limit` (checked
@@ -392,13 +429,18 @@ def decode_loop(step, tokens, lens, limit, model, hidden=None, attn=None, ngram=
     and `lens` [B] are updated in place; `stats` (int64 [B][2], optional)
     accumulates (emitted tokens, steps) per sequence, whose ratio is the paper's
     average acceptance length.  `on_step(i)` runs after each commit (tests use it
-    to compare every step).  Returns the number of steps run."""
+    to compare every step).  `refresh(step, lens)` runs between a step's verification
+    and its commit: the place to renew the ranking's artifact for the next step, e.g.
+    PagedCache.weights with row = step.accept_len into `attn`.  Returns the number of
+    steps run."""
     for i in range(max_steps):
         if i % check_every == 0 and bool((lens >= limit).all()):
             return i
         step.make_draft(tokens, lens, hidden, attn, ngram, agg, threshold, prefix_match,
                         stream=stream)
         step.verify(model(step, lens), stream=stream)
+        if refresh is not None:
+            refresh(step, lens)
         step.commit(tokens, lens, limit=limit, stats=stats, stream=stream)
         if on_step is not None:
             on_step(i)
