@@ -69,7 +69,8 @@ typedef struct pld_cache {
     float *v_scale;        /*   itself times scale[page*scale_page_stride +           */
     int64_t scale_page_stride; /* head*page_size + slot]; 16-byte aligned,            */
                            /*   scale_page_stride a multiple of 4                     */
-    int64_t page_stride, slot_stride, head_stride;   /* elements; multiples of 16 bytes */
+    int64_t page_stride, slot_stride, head_stride;   /* elements; multiples of 16 bytes; */
+                           /*   slot_stride <= 2^24                                   */
     const int32_t *table;  /* [B][table_stride]; an entry outside [0, num_pages) is a bad page */
     int64_t table_stride;  /* >= max_pages */
     int num_pages;         /* >= 1 */
@@ -131,7 +132,8 @@ int pld_cache_write(const pld_cache *cache, const uint16_t *q, int64_t q_seq_str
  *               time must not share it
  * Device-side rules: keys that a row does not see do not affect it, whatever
  * their slots hold; a row one of whose keys lies on a bad page or past the table
- * gets NaN in out and lse.
+ * gets NaN in out and lse.  Where a value that a row sees is not finite, that head
+ * of its out may be NaN as a whole.
  * Errors: PLD_ERR_INVALID, PLD_ERR_ALIGN, PLD_ERR_WORKSPACE, PLD_ERR_LAUNCH.
  */
 size_t pld_cache_attn_workspace_bytes(int B, int n, int Hq, int heads, int head_dim);

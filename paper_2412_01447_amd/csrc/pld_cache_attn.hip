@@ -10,11 +10,15 @@ struct AttnArgs {
     const uint16_t *q;
     int64_t qs, qr;
     int Hq;
-    float scale, cap, inv2_log2e;   // inv2_log2e = 2 log2(e) / cap
+    float scale, cap, inv2_log2e;   // inv2_log2e: of scores in the attention's units
+    float cap2;                     // cap in log2 units
     int window;
+    int G, groups;                  // query heads per key head; row groups per sequence
     uint16_t *out;
     int64_t os, orow;
     float *lse;
+    float *partials;
+    int4 *opened;                   // [blocks]: (entry, key head, last block) of an item that spans blocks
     // the chosen heads' weights
     const int32_t *row, *heads;
     int R;
@@ -41,60 +45,539 @@ __device__ __forceinline__ float score(const AttnArgs &a, const float *q, int pa
     for (int t = 0; t < D; ++t) s = fmaf(q[t], cache_get<kE4m3>(row, t), s);
     s *= a.scale;
     if (kE4m3) s *= a.c.ks[scale_at(a.c, page, j, kv)];
-    return a.cap > 0.f ? soft_cap(s, a.cap, a.inv2_log2e) : s;
+    return a.cap > 0.f ? soft_cap(s, a.cap, 2.f * kLog2E / a.cap) : s;
 }
 
-// One wave per row and head: 64 keys a round, a running maximum and sum.
-template <int D, bool kE4m3>
-__global__ __launch_bounds__(64) void cache_attn_kernel(AttnArgs a) {
-    const int h = blockIdx.x, i = blockIdx.y, b = blockIdx.z, lane = lane_id();
-    int pos0;
-    if (i >= row_count(a.r, b, pos0)) return;
-    __shared__ float q[D], p[64];
-    __shared__ int64_t at[64];
-    const uint16_t *qp = a.q + (int64_t)b * a.qs + (int64_t)i * a.qr + (int64_t)h * D;
-    for (int t = lane; t < D; t += 64) q[t] = __uint_as_float((uint32_t)qp[t] << 16);
-    __syncthreads();
-    const int kv = h / (a.Hq / a.c.heads);
-    const int64_t pos = (int64_t)pos0 + i, cap = (int64_t)a.c.max_pages << a.c.shift;
-    const int64_t lo = a.window && pos + 1 > a.window ? pos + 1 - a.window : 0;
-    bool bad = pos >= cap;
-    float m = -INFINITY, l = 0.f, o[D / 64] = {};
-    for (int64_t j0 = lo; !bad && j0 <= pos; j0 += 64) {
-        const int64_t j = j0 + lane;
-        float s = -INFINITY;
-        int page = 0;
-        if (j <= pos) {
-            page = page_of(a.c, b, j);
-            if (page >= 0) s = score<D, kE4m3>(a, q, page, j, kv);
-        }
-        if (__any(page < 0)) {
-            bad = true;
-            break;
-        }
-        const float mn = fmaxf(m, wave_max_f32(s));
-        const float e = __builtin_amdgcn_exp2f((s - mn) * kLog2E);
-        const float f = __builtin_amdgcn_exp2f((m - mn) * kLog2E);
-        m = mn;
-        l = l * f + wave_sum_f32(e);
-        p[lane] = kE4m3 && j <= pos ? e * a.c.vs[scale_at(a.c, page, j, kv)] : e;
-        at[lane] = slot_at(a.c, page, j, kv);
-        __syncthreads();
-        const int cnt = (int)min((int64_t)64, pos + 1 - j0);
-        for (int u = 0; u < D / 64; ++u) {
-            float s2 = o[u] * f;
-            for (int x = 0; x < cnt; ++x)
-                s2 = fmaf(p[x], cache_get<kE4m3>(a.c.v + at[x], lane + 64 * u), s2);
-            o[u] = s2;
-        }
-        __syncthreads();
+// ------------------------------------------------------------ matrix tiles
+// Everything is computed transposed, with v_mfma_f32_16x16x32_bf16: the scores
+// as K Q^T, whose result gives lane (g, c) = (lane / 16, lane % 16) the scores of
+// query c and keys 4g .. 4g+3 of a 16-key tile, and the output as V^T P^T.  The
+// second product sums over keys in any order, as long as both operands have the
+// same one, so its slot (g, e) is key 16 (e/4) + 4g + e%4 of a 32-key chunk: the
+// weights are then the second product's operand where they are, without a move
+// between lanes, and a lane's eight keys of V are eight row loads.  The rows of
+// V^T are dealt to the tiles so that a lane's eight loads are whole vectors
+// (D / 16 elements) of a V row and one byte permute a pair of keys makes an operand.
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ bf16x8_t as_bf16x8(uint4 v) { return __builtin_bit_cast(bf16x8_t, v); }
+__device__ __forceinline__ f32x4_t mfma(bf16x8_t a, bf16x8_t b, f32x4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+// Two of the four e4m3 values in v as bf16 (exact).
+template <bool kHi>
+__device__ __forceinline__ uint32_t e4m3_bf16(uint32_t v) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.f, kHi));
+}
+// A value that is the same in every lane, as a scalar.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+    return (int64_t)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
+}
+// Maximum over the four lanes of a query.
+__device__ __forceinline__ float query_max(float v) {
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float query_sum(float v) {
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+// --------------------------------------------------------------- the work
+// An item is one key head's rows of one sequence, up to 16 kMT of them (row m is
+// query head m % G of row m / G), over the units of 128 keys that they see.  All
+// items' units, in order of (sequence, row group, key head, unit), are dealt to the
+// blocks in equal contiguous ranges, whatever the sequences' lengths; an item that
+// spans blocks leaves one partial result per block, joined by a second launch.
+constexpr int kUnit = 128;        // keys
+constexpr int kAttnBlocks = 512;  // two per CU; nothing depends on their being resident at once
+
+struct Item {
+    int b, cnt, pos0, r0, rows;   // rows: of this group
+    int lo, hi;                   // keys that some row sees: [lo, hi)
+    int units;                    // 0: no rows
+};
+
+__device__ __forceinline__ Item item_of(const AttnArgs &a, int e, int R) {
+    Item it;
+    it.b = e / a.groups;
+    it.cnt = row_count(a.r, it.b, it.pos0);
+    it.r0 = (e - it.b * a.groups) * R;
+    it.rows = min(it.cnt * a.G - it.r0, R);
+    it.units = 0;
+    if (it.rows <= 0) return it;
+    const int64_t cap = (int64_t)a.c.max_pages << a.c.shift;
+    const int64_t p0 = (int64_t)it.pos0 + it.r0 / a.G;
+    const int64_t p1 = (int64_t)it.pos0 + (it.r0 + it.rows - 1) / a.G;
+    it.lo = a.window && p0 + 1 > a.window ? (int)min(p0 + 1 - a.window, cap) : 0;
+    it.hi = (int)min(p1 + 1, cap);
+    // rows past the table's end have no keys here, but are written
+    it.units = max(1, (it.hi + kUnit - 1) / kUnit - it.lo / kUnit);
+    return it;
+}
+
+// Where a partial result is: blocks keep one of an item that began before their
+// range (slot 0) and one of an item that ends after it (slot 1).
+template <int D>
+__device__ __forceinline__ float *partial_at(const AttnArgs &a, int block, int slot, int R) {
+    return a.partials + ((int64_t)block * 2 + slot) * R * (D + 2);
+}
+
+template <int D>
+__device__ __forceinline__ void put_row(const AttnArgs &a, const Item &it, int kv, int m, int64_t &o,
+                                        int64_t &l, bool &gone) {
+    const int i = (it.r0 + m) / a.G, h = kv * a.G + (it.r0 + m) % a.G;
+    o = (int64_t)it.b * a.os + (int64_t)i * a.orow + (int64_t)h * D;
+    l = ((int64_t)it.b * a.r.n + i) * a.Hq + h;
+    gone = (int64_t)it.pos0 + i >= ((int64_t)a.c.max_pages << a.c.shift);
+}
+
+// Four waves a block, each with all of the item's rows and 32 of a unit's keys.
+template <int D, bool kE4m3, int kMT>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnArgs a) {
+    constexpr int R = 16 * kMT;
+    constexpr int S = D / 32;            // products over a head's elements
+    constexpr int NJ = D / 16;           // output tiles
+    constexpr int NV = D > 128 ? 2 : 1;  // vector loads of a V row
+    constexpr int VE = D / 16 / NV;      // their elements
+    constexpr int KL = kE4m3 ? S / 2 : S;              // 16-byte loads of a key's row per lane
+    constexpr int VW = VE * (kE4m3 ? 1 : 2) / 4;       // words of a V load
+    __shared__ uint4 s_q[kMT][S][64];
+    __shared__ float s_ml[2][4][R];
+    __shared__ float s_o[4][kMT][NJ][64];
+    __shared__ int64_t s_w[8];
+    __shared__ int s_e;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+    const int g = lane >> 4, c = lane & 15;
+
+    // The block's range: the units of the entries before each thread's own.
+    const int entries = a.r.B * a.groups, per = (entries + 255) / 256;
+    const int e0 = min((int)threadIdx.x * per, entries), e1 = min(e0 + per, entries);
+    int64_t mine = 0;
+    for (int e = e0; e < e1; ++e) mine += item_of(a, e, R).units;
+    mine *= a.c.heads;
+    int64_t before = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const int64_t x = __shfl_up(before, o);
+        if (lane >= o) before += x;
     }
-    const float nan = __uint_as_float(0x7fc00000u);
-    uint16_t *out = a.out + (int64_t)b * a.os + (int64_t)i * a.orow + (int64_t)h * D;
-    for (int u = 0; u < D / 64; ++u)
-        out[lane + 64 * u] = (uint16_t)pack_bf16(bad ? nan : o[u] / l, 0.f);
-    if (a.lse && lane == 0)
-        a.lse[((int64_t)b * a.r.n + i) * a.Hq + h] = bad ? nan : m + logf(l);
+    if (lane == 63) s_w[wave] = before;
+    __syncthreads();
+    int64_t total = 0;
+    before -= mine;
+    for (int w = 0; w < 4; ++w) {
+        if (w < wave) before += s_w[w];
+        total += s_w[w];
+    }
+    total = uniform(total);
+    // (as many ranges as units where there are fewer: none between two others is empty)
+    const int64_t ranges = min(total, (int64_t)gridDim.x), block = min((int64_t)blockIdx.x, ranges);
+    const int64_t x0 = ranges ? total * block / ranges : 0;
+    const int64_t x1 = block < ranges ? total * (block + 1) / ranges : x0;
+    int4 opened = make_int4(-1, 0, 0, 0);   // the item that begins here and ends in a later block
+    if (x0 >= x1) {
+        if (threadIdx.x == 0) a.opened[blockIdx.x] = opened;
+        return;
+    }
+    if (before <= x0 && x0 < before + mine) {
+        s_e = e0;
+        s_w[4] = before;
+    }
+    __syncthreads();
+    int e = uniform(s_e);
+    int64_t x = x0, first = uniform(s_w[4]);     // first unit of entry e
+
+    const float c1 = a.scale * kLog2E;
+    while (x < x1) {
+        const Item it = item_of(a, e, R);
+        const int64_t span = (int64_t)it.units * a.c.heads;
+        if (x >= first + span) {
+            first += span;
+            ++e;
+            continue;
+        }
+        const int kv = (int)((x - first) / it.units);
+        const int u0 = (int)((x - first) - (int64_t)kv * it.units);
+        const int u1 = (int)min((int64_t)it.units, u0 + (x1 - x));
+        x += u1 - u0;
+
+        // The rows' queries, as operands in LDS (in registers they would cost a wave the
+        // room for its loads), and the keys that each lane's queries see.
+        int see_lo[kMT], see_hi[kMT];
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < kMT; ++t) {
+            const int m = min(16 * t + c, it.rows - 1);
+            const int i = (it.r0 + m) / a.G, h = kv * a.G + (it.r0 + m) % a.G;
+            const uint16_t *qp =
+                a.q + (int64_t)it.b * a.qs + (int64_t)i * a.qr + (int64_t)h * D;
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                const int d = kE4m3 ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
+                if ((t * S + s) % 4 == wave) s_q[t][s][lane] = *reinterpret_cast<const uint4 *>(qp + d);
+            }
+            const int64_t p = (int64_t)it.pos0 + i;
+            see_hi[t] = (int)min(p + 1, (int64_t)it.hi);
+            see_lo[t] = a.window && p + 1 > a.window ? (int)min(p + 1 - a.window, (int64_t)1 << 30) : 0;
+        }
+        __syncthreads();
+        // keys that every row sees: [all_lo, all_hi)
+        const int64_t pf = (int64_t)it.pos0 + it.r0 / a.G;
+        const int64_t pl = (int64_t)it.pos0 + (it.r0 + it.rows - 1) / a.G;
+        const int all_hi = (int)min(pf + 1, (int64_t)it.hi);
+        const int all_lo = a.window && pl + 1 > a.window ? (int)min(pl + 1 - a.window, (int64_t)1 << 30) : 0;
+
+        f32x4_t o[kMT][NJ];
+        float m[kMT], l[kMT];   // log2 units; l: of this lane's keys
+#pragma unroll
+        for (int t = 0; t < kMT; ++t) {
+            m[t] = -INFINITY;
+            l[t] = 0.f;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) o[t][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+
+        const int ubase = it.lo / kUnit;
+        const int kbase = (ubase + u0) * kUnit + 32 * wave, kend = (ubase + u1) * kUnit;
+        uint4 kr[2][KL];
+        uint32_t vr[8][NV][VW];
+        f32x4_t kf[2], vf[2];
+        int bad = 0;      // bit t: the page of 16-key tile t of the chunk
+
+        // A tile's page; one that cannot be read stands in for a bad one.
+        auto pages = [&](int k0, int (&pg)[2]) {
+            int flags = 0;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int p = k0 + 16 * t < it.hi ? page_of(a.c, it.b, k0 + 16 * t) : 0;
+                if (p < 0) flags |= 1 << t;
+                pg[t] = __builtin_amdgcn_readfirstlane(max(p, 0));
+            }
+            return __builtin_amdgcn_readfirstlane(flags);
+        };
+        // (uniform addresses and 32-bit offsets of the lanes)
+        const char *kh = a.c.k + (int64_t)kv * a.c.head, *vh = a.c.v + (int64_t)kv * a.c.head;
+        const uint32_t slot = (uint32_t)a.c.slot;
+        const uint32_t k_off = (uint32_t)c * slot + 16 * g, v_off = 4 * (uint32_t)g * slot + c * (4 * VW);
+        auto tile_at = [&](int page, int pos) {
+            return (int64_t)page * a.c.page + (int64_t)(pos & ((1 << a.c.shift) - 1)) * a.c.slot;
+        };
+        auto load_k = [&](int k0, const int (&pg)[2]) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const char *row = kh + tile_at(pg[t], k0 + 16 * t);
+#pragma unroll
+                for (int s = 0; s < KL; ++s) kr[t][s] = *reinterpret_cast<const uint4 *>(row + k_off + 64 * s);
+                if constexpr (kE4m3)
+                    kf[t] = *reinterpret_cast<const f32x4_t *>(a.c.ks + scale_at(a.c, pg[t], k0 + 16 * t, kv) + 4 * g);
+            }
+        };
+        auto load_v = [&](int k0, const int (&pg)[2]) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const char *row = vh + tile_at(pg[t], k0 + 16 * t);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int v = 0; v < NV; ++v)
+                        __builtin_memcpy(vr[4 * t + i][v], __builtin_assume_aligned(row + i * slot + v_off + v * (64 * VW), 4 * VW), 4 * VW);
+                if constexpr (kE4m3)
+                    vf[t] = *reinterpret_cast<const f32x4_t *>(a.c.vs + scale_at(a.c, pg[t], k0 + 16 * t, kv) + 4 * g);
+            }
+        };
+
+        int pg[2], bad_next = 0;
+        if (kbase < kend) {
+            bad_next = pages(kbase, pg);
+            load_k(kbase, pg);
+            load_v(kbase, pg);
+        }
+        for (int k0 = kbase; k0 < kend; k0 += kUnit) {
+            asm volatile("" ::: "memory");   // the queries are read from LDS anew
+            const bool more = k0 + kUnit < kend;
+            int pn[2] = {0, 0};
+            bad = bad_next;
+            if (more) bad_next = pages(k0 + kUnit, pn);
+            const bool plain = k0 >= all_lo && k0 + 32 <= all_hi && bad == 0;   // every row sees every key
+
+            f32x4_t x[kMT][2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int n = 0; n < kMT; ++n) x[n][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < S; ++s) {
+                    bf16x8_t k;
+                    if constexpr (kE4m3) {
+                        const uint32_t w0 = s & 1 ? kr[t][s / 2].z : kr[t][s / 2].x;
+                        const uint32_t w1 = s & 1 ? kr[t][s / 2].w : kr[t][s / 2].y;
+                        k = as_bf16x8(make_uint4(e4m3_bf16<false>(w0), e4m3_bf16<true>(w0),
+                                                 e4m3_bf16<false>(w1), e4m3_bf16<true>(w1)));
+                    } else {
+                        k = as_bf16x8(kr[t][s]);
+                    }
+#pragma unroll
+                    for (int n = 0; n < kMT; ++n) x[n][t] = mfma(k, as_bf16x8(s_q[n][s][lane]), x[n][t]);
+                }
+            }
+            f32x4_t kw[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                if constexpr (kE4m3)
+                    kw[t] = kf[t] * c1;
+                else
+                    kw[t] = f32x4_t{c1, c1, c1, c1};
+            }
+            if (more) load_k(k0 + kUnit, pn);
+
+            // Scores in log2 units, then the weights.
+#pragma unroll
+            for (int n = 0; n < kMT; ++n) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) x[n][t] *= kw[t];
+                if (a.cap > 0.f) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) x[n][t][r] = soft_cap(x[n][t][r], a.cap2, a.inv2_log2e);
+                }
+                if (!plain) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int j = k0 + 16 * t + 4 * g + r;
+                            const bool seen = j >= see_lo[n] && j < see_hi[n];
+                            const float v = (bad >> t) & 1 ? __uint_as_float(0x7fc00000u) : x[n][t][r];
+                            x[n][t][r] = seen ? v : -INFINITY;
+                        }
+                }
+                float mx = x[n][0][0];
+#pragma unroll
+                for (int r = 1; r < 8; ++r) mx = fmaxf(mx, x[n][r / 4][r % 4]);
+                if (__any(mx > m[n])) {
+                    const float mn = fmaxf(m[n], query_max(mx));
+                    const float f = m[n] > -INFINITY ? __builtin_amdgcn_exp2f(m[n] - mn) : 0.f;
+                    m[n] = mn;
+                    l[n] *= f;
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) o[n][j] *= f;
+                }
+                const float ms = m[n] > -INFINITY ? m[n] : 0.f;   // (nothing seen yet: weights of 0)
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        x[n][t][r] = __builtin_amdgcn_exp2f(x[n][t][r] - ms);
+                        l[n] += x[n][t][r];
+                    }
+                if constexpr (kE4m3) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            // (a key that is not seen may have any scale)
+                            const float w = x[n][t][r] * vf[t][r];
+                            x[n][t][r] = plain || x[n][t][r] != 0.f ? w : 0.f;
+                        }
+                }
+            }
+            // A product by a weight of 0 would let through what is not finite in a value that
+            // not every row sees.  It becomes 0, and where it was not finite, the weights of
+            // the rows that do see it become NaN.  vp: V as bf16 pairs, [key][element / 2].
+            auto mask_values = [&](uint32_t (&vp)[8][NV][VE / 2]) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int j = k0 + 16 * (i / 4) + 4 * g + i % 4;
+                    const bool any = j >= it.lo && j < it.hi, every = j >= all_lo && j < all_hi;
+                    bool odd = false;
+#pragma unroll
+                    for (int v = 0; v < NV; ++v)
+#pragma unroll
+                        for (int w = 0; w < VE / 2; ++w) {
+                            const uint32_t y = vp[i][v][w];
+                            odd |= (y & 0x7f80u) == 0x7f80u || (y & 0x7f800000u) == 0x7f800000u;
+                        }
+                    const bool row_odd = (__ballot(odd && any && !every) >> (16 * g) & 0xffff) != 0;
+#pragma unroll
+                    for (int v = 0; v < NV; ++v)
+#pragma unroll
+                        for (int w = 0; w < VE / 2; ++w)
+                            if (!any || row_odd) vp[i][v][w] = 0;
+#pragma unroll
+                    for (int n = 0; n < kMT; ++n)
+                        if (row_odd && j >= see_lo[n] && j < see_hi[n])
+                            x[n][i / 4][i % 4] = __uint_as_float(0x7fc00000u);
+                    __builtin_amdgcn_sched_barrier(0);   // key by key: all at once take too many registers
+                }
+            };
+            auto add_product = [&](const uint32_t (&vp)[8][NV][VE / 2]) {
+                // The weights as operands, rounded to bf16: the matrix product takes no wider
+                // ones, and half a step (2^-9) of each term is below the output's own rounding.
+                bf16x8_t p[kMT];
+#pragma unroll
+                for (int n = 0; n < kMT; ++n)
+                    p[n] = as_bf16x8(make_uint4(pack_bf16(x[n][0][0], x[n][0][1]), pack_bf16(x[n][0][2], x[n][0][3]),
+                                                pack_bf16(x[n][1][0], x[n][1][1]), pack_bf16(x[n][1][2], x[n][1][3])));
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    const int v = j / VE, w = j % VE / 2;
+                    const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
+                    uint32_t r[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_perm(vp[2 * i + 1][v][w], vp[2 * i][v][w], sel);
+                    const bf16x8_t vj = as_bf16x8(make_uint4(r[0], r[1], r[2], r[3]));
+#pragma unroll
+                    for (int n = 0; n < kMT; ++n) o[n][j] = mfma(vj, p[n], o[n][j]);
+                }
+            };
+            if constexpr (kE4m3) {
+                uint32_t vp[8][NV][VE / 2];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int v = 0; v < NV; ++v)
+#pragma unroll
+                        for (int w = 0; w < VE / 2; ++w)
+                            vp[i][v][w] = w & 1 ? e4m3_bf16<true>(vr[i][v][w / 2]) : e4m3_bf16<false>(vr[i][v][w / 2]);
+                if (!plain) mask_values(vp);
+                add_product(vp);
+            } else {
+                if (!plain) mask_values(vr);
+                add_product(vr);
+            }
+            if (more) load_v(k0 + kUnit, pn);
+        }
+
+        // The four waves' results joined: a common maximum, then, for each register r of
+        // the output tiles in turn, the sum by wave r (it holds whole vectors of a row).
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < kMT; ++t) {
+            const float lq = query_sum(l[t]);
+            if (g == 0) {
+                s_ml[0][wave][16 * t + c] = m[t];
+                s_ml[1][wave][16 * t + c] = lq;
+            }
+        }
+        __syncthreads();
+        const bool whole = u0 == 0 && u1 == it.units;
+        float *part = partial_at<D>(a, blockIdx.x, u0 == 0, R);
+        float mg[kMT], lg[kMT];
+#pragma unroll
+        for (int t = 0; t < kMT; ++t) {
+            const int r = 16 * t + c;
+            mg[t] = fmaxf(fmaxf(s_ml[0][0][r], s_ml[0][1][r]), fmaxf(s_ml[0][2][r], s_ml[0][3][r]));
+            const float ms = mg[t] > -INFINITY ? mg[t] : 0.f;
+            lg[t] = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) lg[t] += s_ml[1][w][r] * __builtin_amdgcn_exp2f(s_ml[0][w][r] - ms);
+            const float f = __builtin_amdgcn_exp2f(m[t] - ms);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) o[t][j] *= f;
+        }
+        const float nan = __uint_as_float(0x7fc00000u);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if (r) __syncthreads();
+#pragma unroll
+            for (int t = 0; t < kMT; ++t)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) s_o[wave][t][j][lane] = o[t][j][r];
+            __syncthreads();
+            if (wave != r) continue;
+#pragma unroll
+            for (int t = 0; t < kMT; ++t) {
+                const int row = 16 * t + c;
+                if (row >= it.rows) continue;
+                int64_t oat, lat;
+                bool gone;
+                put_row<D>(a, it, kv, row, oat, lat, gone);
+                const float inv = 1.f / lg[t];
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    float y[VE];
+#pragma unroll
+                    for (int j = 0; j < VE; ++j) {
+                        const int jj = v * VE + j;
+                        y[j] = (s_o[0][t][jj][lane] + s_o[1][t][jj][lane]) + (s_o[2][t][jj][lane] + s_o[3][t][jj][lane]);
+                    }
+                    const int d = (D / NV) * v + VE * (4 * g + r);
+                    if (whole) {
+                        uint32_t w[VE / 2];
+#pragma unroll
+                        for (int j = 0; j < VE / 2; ++j)
+                            w[j] = gone ? 0x7fc07fc0u : pack_bf16(y[2 * j] * inv, y[2 * j + 1] * inv);
+                        __builtin_memcpy(__builtin_assume_aligned(a.out + oat + d, 2 * VE), w, 2 * VE);
+                    } else {
+                        __builtin_memcpy(__builtin_assume_aligned(part + row * D + d, 16), y, 4 * VE);
+                    }
+                }
+                if (r == 0 && g == 0) {
+                    if (whole) {
+                        if (a.lse) a.lse[lat] = gone ? nan : (mg[t] + __log2f(lg[t])) * kLn2;
+                    } else {
+                        part[R * D + 2 * row] = mg[t];
+                        part[R * D + 2 * row + 1] = lg[t];
+                    }
+                }
+            }
+        }
+        if (u0 == 0 && !whole) {
+            const int64_t end = first + (int64_t)(kv + 1) * it.units;   // of the item
+            opened = make_int4(e, kv, (int)((end * ranges - 1) / total), 0);   // the last unit's block
+        }
+    }
+    if (threadIdx.x == 0) a.opened[blockIdx.x] = opened;
+}
+
+// One wave per row of an item that spans blocks, in the order of the blocks that open one: the parts' weights from their maxima
+// and sums, 64 parts a round, and the parts' rows added up in order.
+template <int D>
+__global__ __launch_bounds__(256) void cache_attn_join_kernel(AttnArgs a, int R) {
+    const int lane = lane_id(), row = blockIdx.y * 4 + (int)threadIdx.x / 64;
+    const int4 item = a.opened[blockIdx.x];
+    if (item.x < 0) return;
+    const int kv = item.y, parts = item.z - (int)blockIdx.x + 1;
+    const Item it = item_of(a, item.x, R);
+    if (row >= it.rows) return;
+    auto part = [&](int i) { return partial_at<D>(a, blockIdx.x + i, i == 0, R); };
+    float mg = -INFINITY;
+    for (int i = lane; i < parts; i += 64) mg = fmaxf(mg, part(i)[R * D + 2 * row]);
+    mg = wave_max_f32(mg);
+    if (!(mg > -INFINITY)) mg = 0.f;
+    float lg = 0.f, y[D / 64] = {};
+    for (int i0 = 0; i0 < parts; i0 += 64) {
+        float f = 0.f, lp = 0.f;
+        if (i0 + lane < parts) {
+            const float *ml = part(i0 + lane) + R * D + 2 * row;
+            f = __builtin_amdgcn_exp2f(ml[0] - mg);
+            lp = ml[1] * f;
+        }
+        lg += wave_sum_f32(lp);
+        const int n = min(64, parts - i0);
+        for (int i = 0; i < n; ++i) {
+            const float w = __shfl(f, i);
+            const float *p = part(i0 + i) + row * D + lane * (D / 64);
+#pragma unroll
+            for (int k = 0; k < D / 64; ++k) y[k] = fmaf(w, p[k], y[k]);
+        }
+    }
+    int64_t oat, lat;
+    bool gone;
+    put_row<D>(a, it, kv, row, oat, lat, gone);
+    const float inv = gone ? __uint_as_float(0x7fc00000u) : 1.f / lg;
+#pragma unroll
+    for (int k = 0; k < D / 64; ++k)
+        a.out[oat + lane * (D / 64) + k] = (uint16_t)pack_bf16(y[k] * inv, 0.f);
+    if (a.lse && lane == 0) a.lse[lat] = gone ? inv : (mg + __log2f(lg)) * kLn2;
 }
 
 // One thread per key and chosen head.
@@ -127,6 +610,36 @@ __global__ __launch_bounds__(256) void cache_attn_rows_kernel(AttnArgs a) {
     a.attn[(int64_t)b * a.as + (int64_t)r * a.ar + j] = w;
 }
 
+// Rows per item (16 tiles) and row groups per sequence, from the rows of a key head.
+struct AttnShape {
+    int tiles, groups;
+};
+static AttnShape attn_shape(int n, int G, int D) {
+    const int most = D == 256 ? 1 : 2;
+    const int64_t tiles = ((int64_t)n * G + 15) / 16;
+    AttnShape s;
+    s.groups = (int)((tiles + most - 1) / most);
+    s.tiles = (int)((tiles + s.groups - 1) / s.groups);
+    return s;
+}
+static size_t partials_bytes(const AttnShape &s, int D) {
+    return align_up((size_t)kAttnBlocks * 2 * 16 * s.tiles * (D + 2) * sizeof(float), 256);
+}
+
+template <int D, bool kE4m3>
+static void launch_attn(const AttnArgs &a, const AttnShape &sh, hipStream_t s) {
+    const int64_t units = (((int64_t)a.c.max_pages << a.c.shift) + kUnit - 1) / kUnit;
+    const int64_t most = units * a.r.B * sh.groups * a.c.heads;
+    const dim3 grid((unsigned)(most < kAttnBlocks ? most : kAttnBlocks));
+    const int R = 16 * sh.tiles;
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a); };
+    if (sh.tiles == 1)
+        go(cache_attn_kernel<D, kE4m3, 1>);
+    else if constexpr (D < 256)
+        go(cache_attn_kernel<D, kE4m3, 2>);
+    hipLaunchKernelGGL(cache_attn_join_kernel<D>, dim3(grid.x, (unsigned)(R / 4)), dim3(256), 0, s, a, R);
+}
+
 static int prep_attn(const pld_cache *cache, bool needs_v, const uint16_t *q, int64_t qs,
                      int64_t qr, const int32_t *lens, const int32_t *draft_len, int B, int n,
                      int Hq, float scale, float softcap, int window, AttnArgs &a) {
@@ -141,7 +654,9 @@ static int prep_attn(const pld_cache *cache, bool needs_v, const uint16_t *q, in
     a.q = q, a.qs = qs, a.qr = qr;
     a.Hq = Hq;
     a.scale = scale, a.cap = softcap;
-    a.inv2_log2e = softcap > 0.f ? 2.f * kLog2E / softcap : 0.f;
+    a.cap2 = softcap * kLog2E;
+    a.inv2_log2e = softcap > 0.f ? 2.f / softcap : 0.f;   // 2 log2(e) / (cap log2(e))
+    a.G = Hq / cache->heads;
     a.window = window;
     return PLD_OK;
 }
@@ -155,7 +670,8 @@ extern "C" size_t pld_cache_attn_workspace_bytes(int B, int n, int Hq, int heads
         Hq < 1 || Hq > 4096 || Hq % heads ||
         (head_dim != 64 && head_dim != 128 && head_dim != 256))
         return 0;
-    return 256;
+    const AttnShape sh = attn_shape(n, Hq / heads, head_dim);
+    return partials_bytes(sh, head_dim) + kAttnBlocks * sizeof(int4);
 }
 
 extern "C" int pld_cache_attn(const pld_cache *cache, const uint16_t *q, int64_t q_seq_stride,
@@ -174,19 +690,21 @@ extern "C" int pld_cache_attn(const pld_cache *cache, const uint16_t *q, int64_t
     if (!workspace || (uintptr_t)workspace % 16 ||
         workspace_bytes < pld_cache_attn_workspace_bytes(B, n, Hq, cache->heads, D))
         return PLD_ERR_WORKSPACE;
+    const AttnShape sh = attn_shape(n, a.G, D);
+    if ((int64_t)B * sh.groups > INT32_MAX / 2) return PLD_ERR_INVALID;
     a.out = out, a.os = o_seq_stride, a.orow = o_row_stride;
     a.lse = lse;
-    const dim3 grid((unsigned)Hq, (unsigned)n, (unsigned)B);
-    auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(64), 0, (hipStream_t)stream, a);
-    };
+    a.groups = sh.groups;
+    a.partials = static_cast<float *>(workspace);
+    a.opened = reinterpret_cast<int4 *>(static_cast<char *>(workspace) + partials_bytes(sh, D));
     const bool q8 = cache->dtype == PLD_E4M3;
+    const hipStream_t s = (hipStream_t)stream;
     if (D == 64)
-        q8 ? go(cache_attn_kernel<64, true>) : go(cache_attn_kernel<64, false>);
+        q8 ? launch_attn<64, true>(a, sh, s) : launch_attn<64, false>(a, sh, s);
     else if (D == 128)
-        q8 ? go(cache_attn_kernel<128, true>) : go(cache_attn_kernel<128, false>);
+        q8 ? launch_attn<128, true>(a, sh, s) : launch_attn<128, false>(a, sh, s);
     else
-        q8 ? go(cache_attn_kernel<256, true>) : go(cache_attn_kernel<256, false>);
+        q8 ? launch_attn<256, true>(a, sh, s) : launch_attn<256, false>(a, sh, s);
     return hipGetLastError() == hipSuccess ? PLD_OK : PLD_ERR_LAUNCH;
 }
 
