@@ -133,7 +133,7 @@ int pld_cache_write(const pld_cache *cache, const uint16_t *q, int64_t q_seq_str
  * Device-side rules: keys that a row does not see do not affect it, whatever
  * their slots hold; a row one of whose keys lies on a bad page or past the table
  * gets NaN in out and lse.  Where a value that a row sees is not finite, that head
- * of its out may be NaN as a whole.
+ * of its out, and its lse, may be NaN as a whole.
  * Errors: PLD_ERR_INVALID, PLD_ERR_ALIGN, PLD_ERR_WORKSPACE, PLD_ERR_LAUNCH.
  */
 size_t pld_cache_attn_workspace_bytes(int B, int n, int Hq, int heads, int head_dim);

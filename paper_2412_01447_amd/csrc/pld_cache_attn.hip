@@ -62,6 +62,7 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ bf16x8_t as_bf16x8(uint4 v) { return __builtin_bit_cast(bf16x8_t, v); }
+__device__ __forceinline__ bf16x8_t as_bf16x8(u32x4_t v) { return __builtin_bit_cast(bf16x8_t, v); }
 __device__ __forceinline__ f32x4_t mfma(bf16x8_t a, bf16x8_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
@@ -122,6 +123,55 @@ __device__ __forceinline__ Item item_of(const AttnArgs &a, int e, int R) {
     return it;
 }
 
+// The part of all units that is this block's, by each block from the lengths: there are
+// as many ranges as blocks, or as units where those are fewer, so that none between
+// two others is empty.
+struct Range {
+    int64_t x0, x1;          // [x0, x1) of `total`
+    int64_t total, ranges;
+    int e;                   // the entry (sequence and row group) of unit x0
+    int64_t first;           // its first unit
+};
+__device__ __forceinline__ Range block_range(const AttnArgs &a, int R, int64_t *s_w, int *s_e) {
+    const int lane = lane_id(), wave = uniform((int)threadIdx.x / 64);
+    const int entries = a.r.B * a.groups, per = (entries + 255) / 256;
+    const int e0 = min((int)threadIdx.x * per, entries), e1 = min(e0 + per, entries);
+    int64_t mine = 0;
+    for (int e = e0; e < e1; ++e) mine += item_of(a, e, R).units;
+    mine *= a.c.heads;
+    int64_t before = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const int64_t x = __shfl_up(before, o);
+        if (lane >= o) before += x;
+    }
+    if (lane == 63) s_w[wave] = before;
+    __syncthreads();
+    Range r;
+    r.total = 0;
+    before -= mine;
+    for (int w = 0; w < 4; ++w) {
+        if (w < wave) before += s_w[w];
+        r.total += s_w[w];
+    }
+    r.total = uniform(r.total);
+    r.ranges = min(r.total, (int64_t)gridDim.x);
+    const int64_t block = min((int64_t)blockIdx.x, r.ranges);
+    r.x0 = r.ranges ? r.total * block / r.ranges : 0;
+    r.x1 = block < r.ranges ? r.total * (block + 1) / r.ranges : r.x0;
+    if (before <= r.x0 && r.x0 < before + mine) {
+        // the thread whose entries hold x0 steps to the one that does
+        int e = e0;
+        for (int64_t u; r.x0 >= before + (u = (int64_t)item_of(a, e, R).units * a.c.heads); ++e) before += u;
+        *s_e = e;
+        s_w[4] = before;
+    }
+    __syncthreads();
+    r.e = uniform(*s_e);
+    r.first = uniform(s_w[4]);
+    return r;
+}
+
 // Where a partial result is: blocks keep one of an item that began before their
 // range (slot 0) and one of an item that ends after it (slot 1).
 template <int D>
@@ -136,6 +186,85 @@ __device__ __forceinline__ void put_row(const AttnArgs &a, const Item &it, int k
     o = (int64_t)it.b * a.os + (int64_t)i * a.orow + (int64_t)h * D;
     l = ((int64_t)it.b * a.r.n + i) * a.Hq + h;
     gone = (int64_t)it.pos0 + i >= ((int64_t)a.c.max_pages << a.c.shift);
+}
+
+// ------------------------------------------------- 32 keys against 16 queries
+// A lane's scores: x[t][r] of key 16 t + 4 g + r.
+__device__ __forceinline__ void scale_scores(const AttnArgs &a, f32x4_t (&x)[2], const f32x4_t (&kw)[2]) {
+    x[0] *= kw[0];
+    x[1] *= kw[1];
+    if (a.cap > 0.f) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[t][r] = soft_cap(x[t][r], a.cap2, a.inv2_log2e);
+    }
+}
+// Minus infinity for keys that the query does not see, NaN for those in `nan` (a bit per
+// key, this lane's first one lowest) that it does; j: the key of x[0][0].
+__device__ __forceinline__ void mask_scores(f32x4_t (&x)[2], int j, int lo, int hi, uint32_t nan) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int k = j + 16 * t + r;
+            const float v = (nan >> (16 * t + r)) & 1 ? __uint_as_float(0x7fc00000u) : x[t][r];
+            x[t][r] = k >= lo && k < hi ? v : -INFINITY;
+        }
+}
+// The keys of two tiles from the tiles on bad pages (bits 0 and 1).
+__device__ __forceinline__ uint32_t keys_of(int bad) {
+    return (bad & 1 ? 0xffffu : 0u) | (bad & 2 ? 0xffff0000u : 0u);
+}
+// Scores into weights 2^(x - m), with the running maximum m of the query (the same in its
+// four lanes) and the sum l of this lane's keys; output and sum are rescaled where the
+// maximum of any query of the tile grew.
+template <int NJ>
+__device__ __forceinline__ void weigh(f32x4_t (&x)[2], float &m, float &l, f32x4_t (&o)[NJ]) {
+    float mx = x[0][0];
+#pragma unroll
+    for (int r = 1; r < 8; ++r) mx = fmaxf(mx, x[r / 4][r % 4]);
+    if (__any(mx > m)) {
+        const float mn = fmaxf(m, query_max(mx));
+        const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - mn) : 0.f;
+        m = mn;
+        l *= f;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) o[j] *= f;
+    }
+    const float ms = m > -INFINITY ? m : 0.f;   // (nothing seen yet: weights of 0)
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            x[t][r] = __builtin_amdgcn_exp2f(x[t][r] - ms);
+            l += x[t][r];
+        }
+}
+// The weights times the values' scales (a key that is not seen may have any scale).
+__device__ __forceinline__ void scale_weights(f32x4_t (&x)[2], const f32x4_t (&vs)[2], bool plain) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float w = x[t][r] * vs[t][r];
+            x[t][r] = plain || x[t][r] != 0.f ? w : 0.f;
+        }
+}
+// The weights as an operand, rounded to bf16: the matrix product takes no wider ones, and
+// half a step (2^-8) of each term is no more than the output's own rounding.
+__device__ __forceinline__ bf16x8_t weight_operand(const f32x4_t (&x)[2]) {
+    return as_bf16x8(make_uint4(pack_bf16(x[0][0], x[0][1]), pack_bf16(x[0][2], x[0][3]),
+                                pack_bf16(x[1][0], x[1][1]), pack_bf16(x[1][2], x[1][3])));
+}
+// Eight values of an element of two bf16 (word w of each key's) as an operand.
+template <int N, int W>
+__device__ __forceinline__ bf16x8_t value_operand(const uint32_t (&vp)[8][N][W], int v, int w, bool hi) {
+    const uint32_t sel = hi ? 0x07060302u : 0x05040100u;
+    uint32_t r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_perm(vp[2 * i + 1][v][w], vp[2 * i][v][w], sel);
+    return as_bf16x8(make_uint4(r[0], r[1], r[2], r[3]));
 }
 
 // Four waves a block, each with all of the item's rows and 32 of a unit's keys.
@@ -156,46 +285,12 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
     const int g = lane >> 4, c = lane & 15;
 
-    // The block's range: the units of the entries before each thread's own.
-    const int entries = a.r.B * a.groups, per = (entries + 255) / 256;
-    const int e0 = min((int)threadIdx.x * per, entries), e1 = min(e0 + per, entries);
-    int64_t mine = 0;
-    for (int e = e0; e < e1; ++e) mine += item_of(a, e, R).units;
-    mine *= a.c.heads;
-    int64_t before = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        const int64_t x = __shfl_up(before, o);
-        if (lane >= o) before += x;
-    }
-    if (lane == 63) s_w[wave] = before;
-    __syncthreads();
-    int64_t total = 0;
-    before -= mine;
-    for (int w = 0; w < 4; ++w) {
-        if (w < wave) before += s_w[w];
-        total += s_w[w];
-    }
-    total = uniform(total);
-    // (as many ranges as units where there are fewer: none between two others is empty)
-    const int64_t ranges = min(total, (int64_t)gridDim.x), block = min((int64_t)blockIdx.x, ranges);
-    const int64_t x0 = ranges ? total * block / ranges : 0;
-    const int64_t x1 = block < ranges ? total * (block + 1) / ranges : x0;
+    const Range rg = block_range(a, R, s_w, &s_e);
+    int e = rg.e;
+    int64_t x = rg.x0, first = rg.first;    // first unit of entry e
     int4 opened = make_int4(-1, 0, 0, 0);   // the item that begins here and ends in a later block
-    if (x0 >= x1) {
-        if (threadIdx.x == 0) a.opened[blockIdx.x] = opened;
-        return;
-    }
-    if (before <= x0 && x0 < before + mine) {
-        s_e = e0;
-        s_w[4] = before;
-    }
-    __syncthreads();
-    int e = uniform(s_e);
-    int64_t x = x0, first = uniform(s_w[4]);     // first unit of entry e
-
     const float c1 = a.scale * kLog2E;
-    while (x < x1) {
+    while (x < rg.x1) {
         const Item it = item_of(a, e, R);
         const int64_t span = (int64_t)it.units * a.c.heads;
         if (x >= first + span) {
@@ -205,7 +300,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
         }
         const int kv = (int)((x - first) / it.units);
         const int u0 = (int)((x - first) - (int64_t)kv * it.units);
-        const int u1 = (int)min((int64_t)it.units, u0 + (x1 - x));
+        const int u1 = (int)min((int64_t)it.units, u0 + (rg.x1 - x));
         x += u1 - u0;
 
         // The rows' queries, as operands in LDS (in registers they would cost a wave the
@@ -337,57 +432,12 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
             }
             if (more) load_k(k0 + kUnit, pn);
 
-            // Scores in log2 units, then the weights.
 #pragma unroll
             for (int n = 0; n < kMT; ++n) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t) x[n][t] *= kw[t];
-                if (a.cap > 0.f) {
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) x[n][t][r] = soft_cap(x[n][t][r], a.cap2, a.inv2_log2e);
-                }
-                if (!plain) {
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const int j = k0 + 16 * t + 4 * g + r;
-                            const bool seen = j >= see_lo[n] && j < see_hi[n];
-                            const float v = (bad >> t) & 1 ? __uint_as_float(0x7fc00000u) : x[n][t][r];
-                            x[n][t][r] = seen ? v : -INFINITY;
-                        }
-                }
-                float mx = x[n][0][0];
-#pragma unroll
-                for (int r = 1; r < 8; ++r) mx = fmaxf(mx, x[n][r / 4][r % 4]);
-                if (__any(mx > m[n])) {
-                    const float mn = fmaxf(m[n], query_max(mx));
-                    const float f = m[n] > -INFINITY ? __builtin_amdgcn_exp2f(m[n] - mn) : 0.f;
-                    m[n] = mn;
-                    l[n] *= f;
-#pragma unroll
-                    for (int j = 0; j < NJ; ++j) o[n][j] *= f;
-                }
-                const float ms = m[n] > -INFINITY ? m[n] : 0.f;   // (nothing seen yet: weights of 0)
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        x[n][t][r] = __builtin_amdgcn_exp2f(x[n][t][r] - ms);
-                        l[n] += x[n][t][r];
-                    }
-                if constexpr (kE4m3) {
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            // (a key that is not seen may have any scale)
-                            const float w = x[n][t][r] * vf[t][r];
-                            x[n][t][r] = plain || x[n][t][r] != 0.f ? w : 0.f;
-                        }
-                }
+                scale_scores(a, x[n], kw);
+                if (!plain) mask_scores(x[n], k0 + 4 * g, see_lo[n], see_hi[n], keys_of(bad) >> (4 * g));
+                weigh<NJ>(x[n], m[n], l[n], o[n]);
+                if constexpr (kE4m3) scale_weights(x[n], vf, plain);
             }
             // A product by a weight of 0 would let through what is not finite in a value that
             // not every row sees.  It becomes 0, and where it was not finite, the weights of
@@ -419,21 +469,12 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
                 }
             };
             auto add_product = [&](const uint32_t (&vp)[8][NV][VE / 2]) {
-                // The weights as operands, rounded to bf16: the matrix product takes no wider
-                // ones, and half a step (2^-9) of each term is below the output's own rounding.
                 bf16x8_t p[kMT];
 #pragma unroll
-                for (int n = 0; n < kMT; ++n)
-                    p[n] = as_bf16x8(make_uint4(pack_bf16(x[n][0][0], x[n][0][1]), pack_bf16(x[n][0][2], x[n][0][3]),
-                                                pack_bf16(x[n][1][0], x[n][1][1]), pack_bf16(x[n][1][2], x[n][1][3])));
+                for (int n = 0; n < kMT; ++n) p[n] = weight_operand(x[n]);
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) {
-                    const int v = j / VE, w = j % VE / 2;
-                    const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
-                    uint32_t r[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_perm(vp[2 * i + 1][v][w], vp[2 * i][v][w], sel);
-                    const bf16x8_t vj = as_bf16x8(make_uint4(r[0], r[1], r[2], r[3]));
+                    const bf16x8_t vj = value_operand(vp, j / VE, j % VE / 2, j & 1);
 #pragma unroll
                     for (int n = 0; n < kMT; ++n) o[n][j] = mfma(vj, p[n], o[n][j]);
                 }
@@ -532,7 +573,313 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
         }
         if (u0 == 0 && !whole) {
             const int64_t end = first + (int64_t)(kv + 1) * it.units;   // of the item
-            opened = make_int4(e, kv, (int)((end * ranges - 1) / total), 0);   // the last unit's block
+            opened = make_int4(e, kv, (int)((end * rg.ranges - 1) / rg.total), 0);   // the last unit's block
+        }
+    }
+    if (threadIdx.x == 0) a.opened[blockIdx.x] = opened;
+}
+
+// More rows: a block's waves share the keys and each has tiles of 16 rows of its own,
+// wave w the tiles w, w+4, w+8.  Keys and values of 64 positions go through LDS once,
+// as operands: each wave fetches a 16-key tile of K and, of 32 keys, half the elements
+// of V, into registers while the block works on the 64 before, and turns them (e4m3 to
+// bf16, V to pairs of keys) once for all waves on the way to LDS.
+constexpr int kStep = 64;   // keys
+template <int D>
+struct WideLds {
+    u32x4_t k[2][4][D / 32][64], v[2][2][D / 16][64];   // operands of two steps
+    u32x4_t q[3][D / 32][64];                           // the queries of tiles 8 .. 10
+    f32x4_t scale[2][2][kStep / 4];
+    uint32_t odd[2][2][2];                              // [step][32 keys][half]: keys not finite
+};
+
+// A wave's whole work on an item, with NT tiles of its own (from tile0 on, every fourth):
+// a block's waves meet at the same barriers whatever their NT.
+template <int D, bool kE4m3, int NT>
+__device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds, const Item &it, int kv,
+                                             int u0, int u1, int tile0, int R) {
+    constexpr int S = D / 32, NJ = D / 16, NA = NT ? NT : 1;
+    constexpr int KL = kE4m3 ? S / 2 : S;           // 16-byte loads of a key's row per lane
+    constexpr int VE = NJ / 2;                      // elements of a wave's V loads
+    constexpr int VB = VE * (kE4m3 ? 1 : 2);        // their bytes: 2 .. 16
+    constexpr int VW = (VB + 3) / 4;
+    const int lane = lane_id(), wave = uniform((int)threadIdx.x / 64);
+    const int g = lane >> 4, c = lane & 15;
+    const float c1 = a.scale * kLog2E;
+    constexpr int kQ = NT > 2 ? 2 : NT;   // tiles whose queries stay in registers
+    bf16x8_t q[NT > 2 ? 2 : NA][S];
+    int see_lo[NA], see_hi[NA];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int m = min(16 * (tile0 + 4 * t) + c, it.rows - 1);
+        const int i = (it.r0 + m) / a.G, h = kv * a.G + (it.r0 + m) % a.G;
+        const uint16_t *qp = a.q + (int64_t)it.b * a.qs + (int64_t)i * a.qr + (int64_t)h * D;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const int d = kE4m3 ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
+            const u32x4_t v = *reinterpret_cast<const u32x4_t *>(qp + d);
+            if (t < kQ)
+                q[t][s] = as_bf16x8(v);
+            else if (tile0 < 3)
+                lds.q[tile0][s][lane] = v;   // read by this wave alone
+        }
+        const int64_t p = (int64_t)it.pos0 + i;
+        see_hi[t] = (int)min(p + 1, (int64_t)it.hi);
+        see_lo[t] = a.window && p + 1 > a.window ? (int)min(p + 1 - a.window, (int64_t)1 << 30) : 0;
+    }
+    const int64_t pf = (int64_t)it.pos0 + it.r0 / a.G;
+    const int64_t pl = (int64_t)it.pos0 + (it.r0 + it.rows - 1) / a.G;
+    const int all_hi = (int)min(pf + 1, (int64_t)it.hi);
+    const int all_lo = a.window && pl + 1 > a.window ? (int)min(pl + 1 - a.window, (int64_t)1 << 30) : 0;
+
+    f32x4_t o[NA][NJ];
+    float m[NA], l[NA];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        m[t] = -INFINITY;
+        l[t] = 0.f;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) o[t][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+
+    const int kbase = (it.lo / kUnit + u0) * kUnit, kend = (it.lo / kUnit + u1) * kUnit;
+    const char *kh = a.c.k + (int64_t)kv * a.c.head, *vh = a.c.v + (int64_t)kv * a.c.head;
+    const uint32_t slot = (uint32_t)a.c.slot;
+    const uint32_t k_off = (uint32_t)c * slot + 16 * g;
+    const uint32_t v_off = 4 * (uint32_t)g * slot + (16 * (wave & 1) + c) * VB;
+    u32x4_t kr[KL];
+    uint32_t vr[8][1][VW];
+    float sc = 0.f;
+    int bad_next = 0;
+    auto fetch = [&](int k0) {
+        int pg[4];
+        bad_next = 0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int p = k0 + 16 * t < it.hi ? page_of(a.c, it.b, k0 + 16 * t) : 0;
+            if (p < 0) bad_next |= 1 << t;
+            pg[t] = uniform(max(p, 0));
+        }
+        bad_next = uniform(bad_next);
+        auto tile_at = [&](int page, int pos) {
+            return (int64_t)page * a.c.page + (int64_t)(pos & ((1 << a.c.shift) - 1)) * a.c.slot;
+        };
+        const int kp = wave == 0 ? pg[0] : wave == 1 ? pg[1] : wave == 2 ? pg[2] : pg[3];
+        const char *row = kh + tile_at(kp, k0 + 16 * wave);
+#pragma unroll
+        for (int s = 0; s < KL; ++s) kr[s] = *reinterpret_cast<const u32x4_t *>(row + k_off + 64 * s);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int vt = 2 * (wave >> 1) + t;
+            const char *vrow = vh + tile_at(wave >> 1 ? pg[2 + t] : pg[t], k0 + 16 * vt);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                vr[4 * t + i][0][0] = 0;
+                __builtin_memcpy(vr[4 * t + i][0], __builtin_assume_aligned(vrow + i * slot + v_off, VB), VB);
+            }
+        }
+        if constexpr (kE4m3) {
+            // wave 0: the keys' scales, wave 1: the values'
+            if (wave < 2) {
+                const int p = lane < 16 ? pg[0] : lane < 32 ? pg[1] : lane < 48 ? pg[2] : pg[3];
+                sc = (wave ? a.c.vs : a.c.ks)[scale_at(a.c, p, k0 + lane, kv)];
+            }
+        }
+    };
+    // What was fetched for the keys from k0 on, as operands in LDS.
+    auto stage = [&](int k0, int buf) {
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            if constexpr (kE4m3) {
+                const uint32_t w0 = s & 1 ? kr[s / 2].z : kr[s / 2].x, w1 = s & 1 ? kr[s / 2].w : kr[s / 2].y;
+                lds.k[buf][wave][s][lane] = u32x4_t{e4m3_bf16<false>(w0), e4m3_bf16<true>(w0),
+                                                  e4m3_bf16<false>(w1), e4m3_bf16<true>(w1)};
+            } else {
+                lds.k[buf][wave][s][lane] = kr[s];
+            }
+        }
+        uint32_t vp[8][1][VE / 2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int w = 0; w < VE / 2; ++w) {
+                if constexpr (kE4m3)
+                    vp[i][0][w] = w & 1 ? e4m3_bf16<true>(vr[i][0][w / 2]) : e4m3_bf16<false>(vr[i][0][w / 2]);
+                else
+                    vp[i][0][w] = vr[i][0][w];
+            }
+        uint32_t odd_keys = 0;
+        if (!(k0 >= all_lo && k0 + kStep <= all_hi)) {
+            // values that not every row sees (see mask_values above)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int kk = 16 * (i / 4) + 4 * g + i % 4, j = k0 + 32 * (wave >> 1) + kk;
+                const bool any = j >= it.lo && j < it.hi, every = j >= all_lo && j < all_hi;
+                bool odd = false;
+#pragma unroll
+                for (int w = 0; w < VE / 2; ++w) {
+                    const uint32_t y = vp[i][0][w];
+                    odd |= (y & 0x7f80u) == 0x7f80u || (y & 0x7f800000u) == 0x7f800000u;
+                }
+                const uint64_t ball = __ballot(odd && any && !every);
+                const bool row_odd = (ball >> (16 * g) & 0xffff) != 0;
+#pragma unroll
+                for (int gg = 0; gg < 4; ++gg)
+                    if (ball >> (16 * gg) & 0xffff) odd_keys |= 1u << (16 * (i / 4) + 4 * gg + i % 4);
+#pragma unroll
+                for (int w = 0; w < VE / 2; ++w)
+                    if (!any || row_odd) vp[i][0][w] = 0;
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if (lane == 0) lds.odd[buf][wave >> 1][wave & 1] = odd_keys;
+#pragma unroll
+        for (int j = 0; j < VE; ++j)
+            lds.v[buf][wave >> 1][VE * (wave & 1) + j][lane] = __builtin_bit_cast(u32x4_t, value_operand(vp, 0, j / 2, j & 1));
+        if constexpr (kE4m3)
+            if (wave < 2) reinterpret_cast<float *>(lds.scale[buf][wave])[lane] = sc;
+    };
+
+    fetch(kbase);
+    int bad = bad_next, buf = 0;
+    __syncthreads();   // the item before is done with LDS
+    stage(kbase, 0);
+    __syncthreads();
+    for (int k0 = kbase; k0 < kend; k0 += kStep) {
+        const bool more = k0 + kStep < kend;
+        if (more) fetch(k0 + kStep);
+        if constexpr (NT > 0) {
+#pragma unroll 1
+            for (int hh = 0; hh < 2; ++hh) {
+                const int j0 = k0 + 32 * hh;
+                asm volatile("" ::: "memory");   // operands are read from LDS anew
+                const bool plain = k0 >= all_lo && k0 + kStep <= all_hi && bad == 0;
+                f32x4_t sx[NT][2];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) sx[n][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int s = 0; s < S; ++s) {
+                        const bf16x8_t k = as_bf16x8(lds.k[buf][2 * hh + t][s][lane]);
+#pragma unroll
+                        for (int n = 0; n < kQ; ++n) sx[n][t] = mfma(k, q[n][s], sx[n][t]);
+                        if constexpr (NT > 2) sx[2][t] = mfma(k, as_bf16x8(lds.q[tile0][s][lane]), sx[2][t]);
+                    }
+                }
+                f32x4_t kw[2];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    kw[t] = f32x4_t{c1, c1, c1, c1};
+                    if constexpr (kE4m3) kw[t] = lds.scale[buf][0][8 * hh + 4 * t + g] * c1;
+                }
+                bf16x8_t p[NT];
+                // (a value that is not finite: as if its key's page were bad)
+                const uint32_t nan = plain ? 0 : (keys_of(bad >> (2 * hh)) | lds.odd[buf][hh][0] | lds.odd[buf][hh][1]) >> (4 * g);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    scale_scores(a, sx[n], kw);
+                    if (!plain) mask_scores(sx[n], j0 + 4 * g, see_lo[n], see_hi[n], nan);
+                    weigh<NJ>(sx[n], m[n], l[n], o[n]);
+                    if constexpr (kE4m3) {
+                        const f32x4_t vs[2] = {lds.scale[buf][1][8 * hh + g], lds.scale[buf][1][8 * hh + 4 + g]};
+                        scale_weights(sx[n], vs, plain);
+                    }
+                    p[n] = weight_operand(sx[n]);
+                }
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    const bf16x8_t v = as_bf16x8(lds.v[buf][hh][j][lane]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) o[n][j] = mfma(v, p[n], o[n][j]);
+                }
+            }
+        }
+        if (more) stage(k0 + kStep, buf ^ 1);
+        bad = bad_next;
+        buf ^= 1;
+        __syncthreads();
+    }
+
+    const bool whole = u0 == 0 && u1 == it.units;
+    float *part = partial_at<D>(a, blockIdx.x, u0 == 0, R);
+    const float nan = __uint_as_float(0x7fc00000u);
+    int first_tile = tile0;   // (what follows is not computed ahead of the loop)
+    asm volatile("" : "+s"(first_tile));
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const float lg = query_sum(l[n]);
+        const int row = 16 * (first_tile + 4 * n) + c;
+        if (row >= it.rows) continue;
+        int64_t oat, lat;
+        bool gone;
+        put_row<D>(a, it, kv, row, oat, lat, gone);
+        const float inv = 1.f / lg;
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = (D / 2) * v + VE * (4 * g + r);
+                if (whole) {
+                    uint32_t w[VE / 2];
+#pragma unroll
+                    for (int j = 0; j < VE / 2; ++j)
+                        w[j] = gone ? 0x7fc07fc0u
+                                    : pack_bf16(o[n][VE * v + 2 * j][r] * inv, o[n][VE * v + 2 * j + 1][r] * inv);
+                    __builtin_memcpy(__builtin_assume_aligned(a.out + oat + d, 2 * VE), w, 2 * VE);
+                } else {
+                    float y[VE];
+#pragma unroll
+                    for (int j = 0; j < VE; ++j) y[j] = o[n][VE * v + j][r];
+                    __builtin_memcpy(__builtin_assume_aligned(part + row * D + d, VE < 4 ? 8 : 16), y, 4 * VE);
+                }
+            }
+        if (g == 0) {
+            if (whole) {
+                if (a.lse) a.lse[lat] = gone ? nan : (m[n] + __log2f(lg)) * kLn2;
+            } else {
+                part[R * D + 2 * row] = m[n];
+                part[R * D + 2 * row + 1] = lg;
+            }
+        }
+    }
+}
+
+template <int D, bool kE4m3, int kMT>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_wide_kernel(AttnArgs a, int R) {
+    __shared__ WideLds<D> lds;
+    __shared__ int64_t s_w[8];
+    __shared__ int s_e;
+    const int wave = uniform((int)threadIdx.x / 64);
+    const Range rg = block_range(a, R, s_w, &s_e);
+    int e = rg.e;
+    int64_t x = rg.x0, first = rg.first;
+    int4 opened = make_int4(-1, 0, 0, 0);
+    while (x < rg.x1) {
+        const Item it = item_of(a, e, R);
+        const int64_t span = (int64_t)it.units * a.c.heads;
+        if (x >= first + span) {
+            first += span;
+            ++e;
+            continue;
+        }
+        const int kv = (int)((x - first) / it.units);
+        const int u0 = (int)((x - first) - (int64_t)kv * it.units);
+        const int u1 = (int)min((int64_t)it.units, u0 + (rg.x1 - x));
+        x += u1 - u0;
+
+        const int tiles = (it.rows + 15) / 16;
+        // (the waves that have a tile more are others in every other block, and so on other SIMDs)
+        const int tile0 = (wave + blockIdx.x) & 3;
+        if (tile0 + 4 * (kMT - 1) < tiles)
+            wide_segment<D, kE4m3, kMT>(a, lds, it, kv, u0, u1, tile0, R);
+        else if (tile0 >= tiles)
+            wide_segment<D, kE4m3, 0>(a, lds, it, kv, u0, u1, tile0, R);
+        else   // (or fewer, in an item of few rows)
+            wide_segment<D, kE4m3, kMT - 1>(a, lds, it, kv, u0, u1, tile0, R);
+        if (u0 == 0 && u1 < it.units) {
+            const int64_t end = first + (int64_t)(kv + 1) * it.units;
+            opened = make_int4(e, kv, (int)((end * rg.ranges - 1) / rg.total), 0);
         }
     }
     if (threadIdx.x == 0) a.opened[blockIdx.x] = opened;
@@ -610,12 +957,15 @@ __global__ __launch_bounds__(256) void cache_attn_rows_kernel(AttnArgs a) {
     a.attn[(int64_t)b * a.as + (int64_t)r * a.ar + j] = w;
 }
 
-// Rows per item (16 tiles) and row groups per sequence, from the rows of a key head.
+// Tiles of 16 rows per item, and row groups per sequence, from a key head's rows.
+// Up to 2 tiles (1 for heads of 256) a wave has all of an item's rows; past that a wave has
+// up to three tiles (two) of its own.  Eleven and not twelve: the third tiles' queries are in
+// LDS, where two blocks a CU leave room for three.
 struct AttnShape {
     int tiles, groups;
 };
 static AttnShape attn_shape(int n, int G, int D) {
-    const int most = D == 256 ? 1 : 2;
+    const int most = D == 256 ? 8 : 11;
     const int64_t tiles = ((int64_t)n * G + 15) / 16;
     AttnShape s;
     s.groups = (int)((tiles + most - 1) / most);
@@ -633,10 +983,17 @@ static void launch_attn(const AttnArgs &a, const AttnShape &sh, hipStream_t s) {
     const dim3 grid((unsigned)(most < kAttnBlocks ? most : kAttnBlocks));
     const int R = 16 * sh.tiles;
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a); };
+    auto go_wide = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a, R); };
     if (sh.tiles == 1)
         go(cache_attn_kernel<D, kE4m3, 1>);
+    else if (D < 256 && sh.tiles == 2)
+        go(cache_attn_kernel<D, kE4m3, D < 256 ? 2 : 1>);
+    else if (sh.tiles <= 4)
+        go_wide(cache_attn_wide_kernel<D, kE4m3, 1>);
+    else if (sh.tiles <= 8)
+        go_wide(cache_attn_wide_kernel<D, kE4m3, 2>);
     else if constexpr (D < 256)
-        go(cache_attn_kernel<D, kE4m3, 2>);
+        go_wide(cache_attn_wide_kernel<D, kE4m3, 3>);
     hipLaunchKernelGGL(cache_attn_join_kernel<D>, dim3(grid.x, (unsigned)(R / 4)), dim3(256), 0, s, a, R);
 }
 

@@ -124,6 +124,13 @@ ATTEND = [
     ([200, 130], 2, 10, 2, 256, 64, "e4m3", "pairs", 20.0, 0, None),
     ([90, 4], 71, 8, 2, 128, 16, "bf16", "slots", 0, 0, [70, 64]),
     ([2049], 33, 16, 1, 128, 4096, "bf16", "slots", 0, 0, None),
+    ([300, 64, 1], 9, 8, 1, 128, 16, "bf16", "heads", 0, 0, [8, 3, 8]),     # 5 tiles of 16 rows
+    ([300, 90], 17, 16, 2, 128, 16, "e4m3", "pairs", 0, 70, [16, 4]),       # 9 and 3
+    ([140], 22, 8, 1, 64, 16, "e4m3", "slots", 25.0, 0, None),              # 11
+    ([140, 20], 23, 8, 1, 64, 32, "bf16", "slots", 0, 0, [22, 1]),          # 12: two groups
+    ([150, 33], 17, 16, 2, 256, 16, "bf16", "slots", 0, 40, None),          # 9, of heads of 256
+    ([150, 33], 8, 8, 1, 256, 16, "e4m3", "slots", 0, 0, [7, 5]),
+    ([600], 200, 4, 2, 128, 64, "bf16", "slots", 0, 100, None),             # a prompt's chunk
 ]
 
 
@@ -142,7 +149,9 @@ def test_attend(lens, n, Hq, heads, D, page, dtype, layout, softcap, window, dl)
 
 
 @pytest.mark.parametrize("D,heads,G,dtype", [(128, 8, 4, "bf16"), (64, 2, 8, "e4m3"),
-                                             (128, 1, 16, "e4m3"), (256, 1, 1, "bf16")])
+                                             (128, 1, 16, "e4m3"), (256, 1, 1, "bf16"),
+                                             (128, 2, 36, "bf16"), (128, 1, 44, "e4m3"),
+                                             (64, 1, 24, "bf16"), (256, 1, 24, "e4m3")])
 def test_attend_long(D, heads, G, dtype):
     """Tens of thousands of keys split over many blocks beside short sequences; a sample of
     the rows is checked, all of them for being written."""
@@ -176,11 +185,12 @@ def test_attend_spread_scores():
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
 @pytest.mark.parametrize("window", [0, 20])
 @pytest.mark.parametrize("poison", [NAN, math.inf, -math.inf])
-def test_attend_masked_places(dtype, window, poison):
+@pytest.mark.parametrize("G", [1, 4, 12])        # 5, 20 and 60 rows a key head
+def test_attend_masked_places(dtype, window, poison, G):
     """What stands in slots that a row does not see -- past its position (other rows' slots
     among them), before its window, on unused pages -- does not reach it."""
     lens, n = [37, 1, 130], 5
-    c = Case(lens, n, 8, 2, 64, 16, E4M3 if dtype == "e4m3" else torch.bfloat16, [4, 2, 4], seed=11)
+    c = Case(lens, n, 2 * G, 2, 64, 16, E4M3 if dtype == "e4m3" else torch.bfloat16, [4, 2, 4], seed=11)
     P = c.k.shape[0]
     used = np.zeros((P, 16), bool)
     for b, T in enumerate(lens):
@@ -225,10 +235,11 @@ def test_attend_masked_places(dtype, window, poison):
             assert np.array_equal(bits(got[0, i]), bits(out[0, i])), i
 
 
-def test_attend_bad_pages_and_ends():
+@pytest.mark.parametrize("G", [4, 12])
+def test_attend_bad_pages_and_ends(G):
     """A bad page gives NaN to the rows that see it and to no others; rows past the table are
     NaN; sequences without rows are left alone."""
-    c = Case([100, 100, 100, 0, 50, 31], 4, 8, 2, 64, 16, draft_len=[3, 3, 3, 3, 4, -1], seed=2)
+    c = Case([100, 100, 100, 0, 50, 31], 4, 2 * G, 2, 64, 16, draft_len=[3, 3, 3, 3, 4, -1], seed=2)
     c.table[0, 3] = -1
     c.table[1, 0] = c.k.shape[0]
     c.t = d_i32(c.table)
@@ -241,7 +252,7 @@ def test_attend_bad_pages_and_ends():
     c.check_attend(out, L, window=30)
     assert not torch.isnan(out.float()).any()
     # a table that ends inside the rows, or before them
-    c = Case([30, 30, 30, 30], 4, 4, 2, 64, 16, seed=2)
+    c = Case([30, 30, 30, 30], 4, 2 * G, 2, 64, 16, seed=2)
     c.lens = [30, 47, 200, 2 ** 31 - 1]
     c.d_lens = d_i32(c.lens)
     out, L = c.attend()
