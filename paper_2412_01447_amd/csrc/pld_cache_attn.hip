@@ -172,6 +172,23 @@ __device__ __forceinline__ Range block_range(const AttnArgs &a, int R, int64_t *
     return r;
 }
 
+// The table's entry for 16-key tile (lane % T) of the keys from k0 on, as loaded (the last
+// tile that has keys stands in for those past the end), and the pages from it: those that
+// cannot be read are 0, with a bit in `bad` where the tile has keys.
+template <int T>
+__device__ __forceinline__ int load_pages(const AttnArgs &a, const Item &it, int k0) {
+    const int j = min(k0 + 16 * (lane_id() & (T - 1)), it.hi - 1);
+    return a.c.table[(int64_t)it.b * a.c.table_stride + (j >> a.c.shift)];
+}
+template <int T>
+__device__ __forceinline__ int take_pages(const AttnArgs &a, const Item &it, int k0, int entry, int (&pg)[T]) {
+    const bool ok = (uint32_t)entry < (uint32_t)a.c.num_pages;
+    const int page = ok ? entry : 0;
+#pragma unroll
+    for (int t = 0; t < T; ++t) pg[t] = __builtin_amdgcn_readlane(page, t);
+    return (int)__ballot(!ok && k0 + 16 * (lane_id() & (T - 1)) < it.hi) & ((1 << T) - 1);
+}
+
 // Where a partial result is: blocks keep one of an item that began before their
 // range (slot 0) and one of an item that ends after it (slot 1).
 template <int D>
@@ -189,66 +206,75 @@ __device__ __forceinline__ void put_row(const AttnArgs &a, const Item &it, int k
 }
 
 // ------------------------------------------------- 32 keys against 16 queries
-// A lane's scores: x[t][r] of key 16 t + 4 g + r.
-__device__ __forceinline__ void scale_scores(const AttnArgs &a, f32x4_t (&x)[2], const f32x4_t (&kw)[2]) {
-    x[0] *= kw[0];
-    x[1] *= kw[1];
-    if (a.cap > 0.f) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) x[t][r] = soft_cap(x[t][r], a.cap2, a.inv2_log2e);
-    }
-}
-// Minus infinity for keys that the query does not see, NaN for those in `nan` (a bit per
-// key, this lane's first one lowest) that it does; j: the key of x[0][0].
-__device__ __forceinline__ void mask_scores(f32x4_t (&x)[2], int j, int lo, int hi, uint32_t nan) {
+// A lane's products q.k: x[t][r] of key 16 t + 4 g + r.  What a query sees of the keys, where
+// it may not be all of them: j0 <= j < j1 counted from x[0][0]'s key, and the keys (a bit
+// each, this lane's first one lowest) that turn what sees them into NaN.
+struct Seen {
+    int j0, j1;
+    uint32_t nan;
+};
+__device__ __forceinline__ void mask_scores(f32x4_t (&x)[2], const Seen &see) {
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int k = j + 16 * t + r;
-            const float v = (nan >> (16 * t + r)) & 1 ? __uint_as_float(0x7fc00000u) : x[t][r];
-            x[t][r] = k >= lo && k < hi ? v : -INFINITY;
+            const int j = 16 * t + r;
+            const float v = (see.nan >> j) & 1 ? __uint_as_float(0x7fc00000u) : x[t][r];
+            x[t][r] = j >= see.j0 && j < see.j1 ? v : -INFINITY;
         }
 }
 // The keys of two tiles from the tiles on bad pages (bits 0 and 1).
 __device__ __forceinline__ uint32_t keys_of(int bad) {
     return (bad & 1 ? 0xffffu : 0u) | (bad & 2 ? 0xffff0000u : 0u);
 }
-// Scores into weights 2^(x - m), with the running maximum m of the query (the same in its
-// four lanes) and the sum l of this lane's keys; output and sum are rescaled where the
-// maximum of any query of the tile grew.
-template <int NJ>
-__device__ __forceinline__ void weigh(f32x4_t (&x)[2], float &m, float &l, f32x4_t (&o)[NJ]) {
-    float mx = x[0][0];
+__device__ __forceinline__ float max_of(const f32x4_t (&x)[2]) {
+    return fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])),
+                 fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
+}
+
+// Products into scores; returns the factor that is left to log2 units (the scale, where it
+// is the same for all keys and no cap comes between).
+template <bool kE4m3>
+__device__ __forceinline__ float scale_scores(const AttnArgs &a, f32x4_t (&x)[2], float c1, f32x4_t ks0,
+                                              f32x4_t ks1) {
+    if constexpr (kE4m3) {
+        x[0] *= ks0 * c1;
+        x[1] *= ks1 * c1;
+        c1 = 1.f;
+    }
+    if (a.cap > 0.f) {
 #pragma unroll
-    for (int r = 1; r < 8; ++r) mx = fmaxf(mx, x[r / 4][r % 4]);
-    if (__any(mx > m)) {
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[t][r] = soft_cap(x[t][r] * c1, a.cap2, a.inv2_log2e);
+        c1 = 1.f;
+    }
+    return c1;
+}
+// Scores into weights 2^(x c - m), with the running maximum m of the query (the same in its
+// four lanes) and the sum l of this lane's keys.  The maximum is raised, and output and sum
+// are rescaled, only where a score of any query of the tile is kSlack above it: weights of
+// up to 2^kSlack lose nothing in fp32 and bf16, and what random scores still grow by after a
+// few keys seldom comes that far.
+constexpr float kSlack = 8.f;
+constexpr float kNoMax = -1e30f;   // of a query that has seen no key
+template <int NJ>
+__device__ __forceinline__ void weigh(f32x4_t (&x)[2], float c, float &m, float &l, f32x4_t (&o)[NJ]) {
+    const float mx = max_of(x) * c;
+    if (__any(mx > m + kSlack)) {
         const float mn = fmaxf(m, query_max(mx));
-        const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - mn) : 0.f;
+        const float f = __builtin_amdgcn_exp2f(m - mn);
         m = mn;
         l *= f;
 #pragma unroll
         for (int j = 0; j < NJ; ++j) o[j] *= f;
     }
-    const float ms = m > -INFINITY ? m : 0.f;   // (nothing seen yet: weights of 0)
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            x[t][r] = __builtin_amdgcn_exp2f(x[t][r] - ms);
+            x[t][r] = __builtin_amdgcn_exp2f(fmaf(x[t][r], c, -m));
             l += x[t][r];
-        }
-}
-// The weights times the values' scales (a key that is not seen may have any scale).
-__device__ __forceinline__ void scale_weights(f32x4_t (&x)[2], const f32x4_t (&vs)[2], bool plain) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float w = x[t][r] * vs[t][r];
-            x[t][r] = plain || x[t][r] != 0.f ? w : 0.f;
         }
 }
 // The weights as an operand, rounded to bf16: the matrix product takes no wider ones, and
@@ -333,7 +359,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
         float m[kMT], l[kMT];   // log2 units; l: of this lane's keys
 #pragma unroll
         for (int t = 0; t < kMT; ++t) {
-            m[t] = -INFINITY;
+            m[t] = kNoMax;
             l[t] = 0.f;
 #pragma unroll
             for (int j = 0; j < NJ; ++j) o[t][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -346,17 +372,6 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
         f32x4_t kf[2], vf[2];
         int bad = 0;      // bit t: the page of 16-key tile t of the chunk
 
-        // A tile's page; one that cannot be read stands in for a bad one.
-        auto pages = [&](int k0, int (&pg)[2]) {
-            int flags = 0;
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const int p = k0 + 16 * t < it.hi ? page_of(a.c, it.b, k0 + 16 * t) : 0;
-                if (p < 0) flags |= 1 << t;
-                pg[t] = __builtin_amdgcn_readfirstlane(max(p, 0));
-            }
-            return __builtin_amdgcn_readfirstlane(flags);
-        };
         // (uniform addresses and 32-bit offsets of the lanes)
         const char *kh = a.c.k + (int64_t)kv * a.c.head, *vh = a.c.v + (int64_t)kv * a.c.head;
         const uint32_t slot = (uint32_t)a.c.slot;
@@ -388,18 +403,20 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
             }
         };
 
-        int pg[2], bad_next = 0;
-        if (kbase < kend) {
-            bad_next = pages(kbase, pg);
-            load_k(kbase, pg);
-            load_v(kbase, pg);
-        }
+        int pg[2], entry = load_pages<2>(a, it, kbase);
+        int bad_next = take_pages<2>(a, it, kbase, entry, pg);
+        entry = load_pages<2>(a, it, kbase + kUnit);   // ahead of the loads that go by it
+        load_k(kbase, pg);
+        load_v(kbase, pg);
         for (int k0 = kbase; k0 < kend; k0 += kUnit) {
             asm volatile("" ::: "memory");   // the queries are read from LDS anew
             const bool more = k0 + kUnit < kend;
             int pn[2] = {0, 0};
             bad = bad_next;
-            if (more) bad_next = pages(k0 + kUnit, pn);
+            if (more) {
+                bad_next = take_pages<2>(a, it, k0 + kUnit, entry, pn);
+                entry = load_pages<2>(a, it, k0 + 2 * kUnit);
+            }
             const bool plain = k0 >= all_lo && k0 + 32 <= all_hi && bad == 0;   // every row sees every key
 
             f32x4_t x[kMT][2];
@@ -422,22 +439,35 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
                     for (int n = 0; n < kMT; ++n) x[n][t] = mfma(k, as_bf16x8(s_q[n][s][lane]), x[n][t]);
                 }
             }
-            f32x4_t kw[2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                if constexpr (kE4m3)
-                    kw[t] = kf[t] * c1;
-                else
-                    kw[t] = f32x4_t{c1, c1, c1, c1};
-            }
+            f32x4_t ks[2];
+            if constexpr (kE4m3) ks[0] = kf[0], ks[1] = kf[1];
             if (more) load_k(k0 + kUnit, pn);
 
 #pragma unroll
             for (int n = 0; n < kMT; ++n) {
-                scale_scores(a, x[n], kw);
-                if (!plain) mask_scores(x[n], k0 + 4 * g, see_lo[n], see_hi[n], keys_of(bad) >> (4 * g));
-                weigh<NJ>(x[n], m[n], l[n], o[n]);
-                if constexpr (kE4m3) scale_weights(x[n], vf, plain);
+                const float sc = scale_scores<kE4m3>(a, x[n], c1, ks[0], ks[1]);
+                const int j = k0 + 4 * g;
+                if (!plain) mask_scores(x[n], Seen{see_lo[n] - j, see_hi[n] - j, keys_of(bad) >> (4 * g)});
+                weigh<NJ>(x[n], sc, m[n], l[n], o[n]);
+            }
+            if constexpr (kE4m3) {
+                if (!plain) {
+                    // a scale that is not finite, as with the values below
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        if (fabsf(vf[i / 4][i % 4]) < INFINITY) continue;
+                        const int j = k0 + 16 * (i / 4) + 4 * g + i % 4;
+                        vf[i / 4][i % 4] = 0.f;
+#pragma unroll
+                        for (int n = 0; n < kMT; ++n)
+                            if (j >= see_lo[n] && j < see_hi[n]) x[n][i / 4][i % 4] = __uint_as_float(0x7fc00000u);
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < kMT; ++n) {
+                    x[n][0] *= vf[0];
+                    x[n][1] *= vf[1];
+                }
             }
             // A product by a weight of 0 would let through what is not finite in a value that
             // not every row sees.  It becomes 0, and where it was not finite, the weights of
@@ -516,11 +546,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
         for (int t = 0; t < kMT; ++t) {
             const int r = 16 * t + c;
             mg[t] = fmaxf(fmaxf(s_ml[0][0][r], s_ml[0][1][r]), fmaxf(s_ml[0][2][r], s_ml[0][3][r]));
-            const float ms = mg[t] > -INFINITY ? mg[t] : 0.f;
             lg[t] = 0.f;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) lg[t] += s_ml[1][w][r] * __builtin_amdgcn_exp2f(s_ml[0][w][r] - ms);
-            const float f = __builtin_amdgcn_exp2f(m[t] - ms);
+            for (int w = 0; w < 4; ++w) lg[t] += s_ml[1][w][r] * __builtin_amdgcn_exp2f(s_ml[0][w][r] - mg[t]);
+            const float f = __builtin_amdgcn_exp2f(m[t] - mg[t]);
 #pragma unroll
             for (int j = 0; j < NJ; ++j) o[t][j] *= f;
         }
@@ -590,7 +619,7 @@ struct WideLds {
     u32x4_t k[2][4][D / 32][64], v[2][2][D / 16][64];   // operands of two steps
     u32x4_t q[3][D / 32][64];                           // the queries of tiles 8 .. 10
     f32x4_t scale[2][2][kStep / 4];
-    uint32_t odd[2][2][2];                              // [step][32 keys][half]: keys not finite
+    uint32_t odd[2][2][3];                              // [step][32 keys][half; scales]: not finite
 };
 
 // A wave's whole work on an item, with NT tiles of its own (from tile0 on, every fourth):
@@ -636,7 +665,7 @@ __device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds,
     float m[NA], l[NA];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        m[t] = -INFINITY;
+        m[t] = kNoMax;
         l[t] = 0.f;
 #pragma unroll
         for (int j = 0; j < NJ; ++j) o[t][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -650,17 +679,11 @@ __device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds,
     u32x4_t kr[KL];
     uint32_t vr[8][1][VW];
     float sc = 0.f;
-    int bad_next = 0;
+    int bad_next = 0, entry = load_pages<4>(a, it, kbase);
     auto fetch = [&](int k0) {
         int pg[4];
-        bad_next = 0;
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int p = k0 + 16 * t < it.hi ? page_of(a.c, it.b, k0 + 16 * t) : 0;
-            if (p < 0) bad_next |= 1 << t;
-            pg[t] = uniform(max(p, 0));
-        }
-        bad_next = uniform(bad_next);
+        bad_next = take_pages<4>(a, it, k0, entry, pg);
+        entry = load_pages<4>(a, it, k0 + kStep);   // ahead of the loads that go by it
         auto tile_at = [&](int page, int pos) {
             return (int64_t)page * a.c.page + (int64_t)(pos & ((1 << a.c.shift) - 1)) * a.c.slot;
         };
@@ -736,8 +759,15 @@ __device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds,
 #pragma unroll
         for (int j = 0; j < VE; ++j)
             lds.v[buf][wave >> 1][VE * (wave & 1) + j][lane] = __builtin_bit_cast(u32x4_t, value_operand(vp, 0, j / 2, j & 1));
-        if constexpr (kE4m3)
+        if constexpr (kE4m3) {
+            if (wave == 1) {
+                // a scale that is not finite, as with the values
+                const uint64_t ball = __ballot(!(fabsf(sc) < INFINITY));
+                if (!(fabsf(sc) < INFINITY)) sc = 0.f;
+                if (lane < 2) lds.odd[buf][lane][2] = (uint32_t)(ball >> (32 * lane));
+            }
             if (wave < 2) reinterpret_cast<float *>(lds.scale[buf][wave])[lane] = sc;
+        }
     };
 
     fetch(kbase);
@@ -767,23 +797,25 @@ __device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds,
                         if constexpr (NT > 2) sx[2][t] = mfma(k, as_bf16x8(lds.q[tile0][s][lane]), sx[2][t]);
                     }
                 }
-                f32x4_t kw[2];
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    kw[t] = f32x4_t{c1, c1, c1, c1};
-                    if constexpr (kE4m3) kw[t] = lds.scale[buf][0][8 * hh + 4 * t + g] * c1;
-                }
                 bf16x8_t p[NT];
                 // (a value that is not finite: as if its key's page were bad)
-                const uint32_t nan = plain ? 0 : (keys_of(bad >> (2 * hh)) | lds.odd[buf][hh][0] | lds.odd[buf][hh][1]) >> (4 * g);
+                uint32_t nan = 0;
+                if (!plain) {
+                    nan = keys_of(bad >> (2 * hh)) | lds.odd[buf][hh][0] | lds.odd[buf][hh][1];
+                    if constexpr (kE4m3) nan |= lds.odd[buf][hh][2];
+                    nan >>= 4 * g;
+                }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    scale_scores(a, sx[n], kw);
-                    if (!plain) mask_scores(sx[n], j0 + 4 * g, see_lo[n], see_hi[n], nan);
-                    weigh<NJ>(sx[n], m[n], l[n], o[n]);
+                    f32x4_t ks[2];
+                    if constexpr (kE4m3) ks[0] = lds.scale[buf][0][8 * hh + g], ks[1] = lds.scale[buf][0][8 * hh + 4 + g];
+                    const float sc = scale_scores<kE4m3>(a, sx[n], c1, ks[0], ks[1]);
+                    const int j = j0 + 4 * g;
+                    if (!plain) mask_scores(sx[n], Seen{see_lo[n] - j, see_hi[n] - j, nan});
+                    weigh<NJ>(sx[n], sc, m[n], l[n], o[n]);
                     if constexpr (kE4m3) {
-                        const f32x4_t vs[2] = {lds.scale[buf][1][8 * hh + g], lds.scale[buf][1][8 * hh + 4 + g]};
-                        scale_weights(sx[n], vs, plain);
+                        sx[n][0] *= lds.scale[buf][1][8 * hh + g];
+                        sx[n][1] *= lds.scale[buf][1][8 * hh + 4 + g];
                     }
                     p[n] = weight_operand(sx[n]);
                 }
@@ -899,7 +931,6 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(AttnArgs a, int R)
     float mg = -INFINITY;
     for (int i = lane; i < parts; i += 64) mg = fmaxf(mg, part(i)[R * D + 2 * row]);
     mg = wave_max_f32(mg);
-    if (!(mg > -INFINITY)) mg = 0.f;
     float lg = 0.f, y[D / 64] = {};
     for (int i0 = 0; i0 < parts; i0 += 64) {
         float f = 0.f, lp = 0.f;
