@@ -172,21 +172,59 @@ __device__ __forceinline__ Range block_range(const AttnArgs &a, int R, int64_t *
     return r;
 }
 
-// The table's entry for 16-key tile (lane % T) of the keys from k0 on, as loaded (the last
-// tile that has keys stands in for those past the end), and the pages from it: those that
-// cannot be read are 0, with a bit in `bad` where the tile has keys.
+// Loads at a uniform address plus 32-bit offsets, a lane's and a scalar one: no vector
+// arithmetic for addresses.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void *p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, 0x7fffffff, 0x00027000);
+}
+__device__ __forceinline__ u32x4_t buffer_load16(__amdgpu_buffer_rsrc_t b, uint32_t off, uint32_t soff) {
+    return __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(b, off, soff, 0));
+}
+template <int kBytes, int W>
+__device__ __forceinline__ void buffer_load(uint32_t (&v)[W], __amdgpu_buffer_rsrc_t b, uint32_t off, uint32_t soff) {
+    if constexpr (kBytes == 2) {
+        v[0] = __builtin_amdgcn_raw_buffer_load_b16(b, off, soff, 0);
+    } else if constexpr (kBytes == 4) {
+        v[0] = __builtin_amdgcn_raw_buffer_load_b32(b, off, soff, 0);
+    } else if constexpr (kBytes == 8) {
+        const auto w = __builtin_amdgcn_raw_buffer_load_b64(b, off, soff, 0);
+        v[0] = w[0], v[1] = w[1];
+    } else {
+        const auto w = __builtin_amdgcn_raw_buffer_load_b128(b, off, soff, 0);
+        v[0] = w[0], v[1] = w[1], v[2] = w[2], v[3] = w[3];
+    }
+}
+
+// The pages of T tiles of 16 keys: lane l stands for key l % (16 T) of those from k0 on.
+// load_entry takes the table's entries (the last key's page stands in for keys past the
+// end), a step ahead; take_tiles makes addresses of them.  A page that cannot be read is 0,
+// with a bit in `bad` for each of its keys that the item has.
 template <int T>
-__device__ __forceinline__ int load_pages(const AttnArgs &a, const Item &it, int k0) {
-    const int j = min(k0 + 16 * (lane_id() & (T - 1)), it.hi - 1);
+__device__ __forceinline__ int load_entry(const AttnArgs &a, const Item &it, int k0) {
+    const int j = min(k0 + (lane_id() & (16 * T - 1)), it.hi - 1);
     return a.c.table[(int64_t)it.b * a.c.table_stride + (j >> a.c.shift)];
 }
 template <int T>
-__device__ __forceinline__ int take_pages(const AttnArgs &a, const Item &it, int k0, int entry, int (&pg)[T]) {
+struct Tiles {
+    int64_t at[T];   // of a tile's first row, in bytes
+    int64_t scale;   // of this lane's key
+    uint64_t bad;
+};
+__device__ __forceinline__ int64_t readlane(int64_t v, int l) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), l) << 32 |
+                     (uint32_t)__builtin_amdgcn_readlane((int)v, l));
+}
+template <int T, bool kScales>
+__device__ __forceinline__ Tiles<T> take_tiles(const AttnArgs &a, const Item &it, int k0, int entry, int kv) {
+    Tiles<T> r;
     const bool ok = (uint32_t)entry < (uint32_t)a.c.num_pages;
-    const int page = ok ? entry : 0;
+    const int page = ok ? entry : 0, j = k0 + (lane_id() & (16 * T - 1)), mask = (1 << a.c.shift) - 1;
+    const int64_t at = (int64_t)page * a.c.page + (int64_t)(j & mask & ~15) * a.c.slot;
 #pragma unroll
-    for (int t = 0; t < T; ++t) pg[t] = __builtin_amdgcn_readlane(page, t);
-    return (int)__ballot(!ok && k0 + 16 * (lane_id() & (T - 1)) < it.hi) & ((1 << T) - 1);
+    for (int t = 0; t < T; ++t) r.at[t] = readlane(at, 16 * t);
+    if constexpr (kScales) r.scale = (int64_t)page * a.c.spage + ((int64_t)kv << a.c.shift) + (j & mask);
+    r.bad = __ballot(!ok && j < it.hi);
+    return r;
 }
 
 // Where a partial result is: blocks keep one of an item that began before their
@@ -223,23 +261,19 @@ __device__ __forceinline__ void mask_scores(f32x4_t (&x)[2], const Seen &see) {
             x[t][r] = j >= see.j0 && j < see.j1 ? v : -INFINITY;
         }
 }
-// The keys of two tiles from the tiles on bad pages (bits 0 and 1).
-__device__ __forceinline__ uint32_t keys_of(int bad) {
-    return (bad & 1 ? 0xffffu : 0u) | (bad & 2 ? 0xffff0000u : 0u);
-}
 __device__ __forceinline__ float max_of(const f32x4_t (&x)[2]) {
     return fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])),
                  fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
 }
 
-// Products into scores; returns the factor that is left to log2 units (the scale, where it
-// is the same for all keys and no cap comes between).
+// Products into scores; returns the factor that is left to log2 units (c1, where it is the
+// same for all keys and no cap comes between).  ks: the keys' scales times c1.
 template <bool kE4m3>
 __device__ __forceinline__ float scale_scores(const AttnArgs &a, f32x4_t (&x)[2], float c1, f32x4_t ks0,
                                               f32x4_t ks1) {
     if constexpr (kE4m3) {
-        x[0] *= ks0 * c1;
-        x[1] *= ks1 * c1;
+        x[0] *= ks0;
+        x[1] *= ks1;
         c1 = 1.f;
     }
     if (a.cap > 0.f) {
@@ -367,55 +401,50 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
 
         const int ubase = it.lo / kUnit;
         const int kbase = (ubase + u0) * kUnit + 32 * wave, kend = (ubase + u1) * kUnit;
-        uint4 kr[2][KL];
+        u32x4_t kr[2][KL];
         uint32_t vr[8][NV][VW];
         f32x4_t kf[2], vf[2];
-        int bad = 0;      // bit t: the page of 16-key tile t of the chunk
+        uint32_t bad = 0;   // the chunk's keys on bad pages
 
-        // (uniform addresses and 32-bit offsets of the lanes)
         const char *kh = a.c.k + (int64_t)kv * a.c.head, *vh = a.c.v + (int64_t)kv * a.c.head;
         const uint32_t slot = (uint32_t)a.c.slot;
         const uint32_t k_off = (uint32_t)c * slot + 16 * g, v_off = 4 * (uint32_t)g * slot + c * (4 * VW);
-        auto tile_at = [&](int page, int pos) {
-            return (int64_t)page * a.c.page + (int64_t)(pos & ((1 << a.c.shift) - 1)) * a.c.slot;
-        };
-        auto load_k = [&](int k0, const int (&pg)[2]) {
+        auto load_k = [&](const Tiles<2> &tl) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const char *row = kh + tile_at(pg[t], k0 + 16 * t);
+                const auto buf = buffer_at(kh + tl.at[t]);
 #pragma unroll
-                for (int s = 0; s < KL; ++s) kr[t][s] = *reinterpret_cast<const uint4 *>(row + k_off + 64 * s);
+                for (int s = 0; s < KL; ++s) kr[t][s] = buffer_load16(buf, k_off + 64 * s, 0);
                 if constexpr (kE4m3)
-                    kf[t] = *reinterpret_cast<const f32x4_t *>(a.c.ks + scale_at(a.c, pg[t], k0 + 16 * t, kv) + 4 * g);
+                    kf[t] = __builtin_bit_cast(f32x4_t, buffer_load16(buffer_at(a.c.ks + readlane(tl.scale, 16 * t)), 16 * g, 0));
             }
         };
-        auto load_v = [&](int k0, const int (&pg)[2]) {
+        auto load_v = [&](const Tiles<2> &tl) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const char *row = vh + tile_at(pg[t], k0 + 16 * t);
+                const auto buf = buffer_at(vh + tl.at[t]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int v = 0; v < NV; ++v)
-                        __builtin_memcpy(vr[4 * t + i][v], __builtin_assume_aligned(row + i * slot + v_off + v * (64 * VW), 4 * VW), 4 * VW);
+                        buffer_load<4 * VW>(vr[4 * t + i][v], buf, v_off + v * (64 * VW), i * slot);
                 if constexpr (kE4m3)
-                    vf[t] = *reinterpret_cast<const f32x4_t *>(a.c.vs + scale_at(a.c, pg[t], k0 + 16 * t, kv) + 4 * g);
+                    vf[t] = __builtin_bit_cast(f32x4_t, buffer_load16(buffer_at(a.c.vs + readlane(tl.scale, 16 * t)), 16 * g, 0));
             }
         };
 
-        int pg[2], entry = load_pages<2>(a, it, kbase);
-        int bad_next = take_pages<2>(a, it, kbase, entry, pg);
-        entry = load_pages<2>(a, it, kbase + kUnit);   // ahead of the loads that go by it
-        load_k(kbase, pg);
-        load_v(kbase, pg);
+        int entry = load_entry<2>(a, it, kbase);
+        Tiles<2> tl = take_tiles<2, kE4m3>(a, it, kbase, entry, kv);
+        entry = load_entry<2>(a, it, kbase + kUnit);   // ahead of the loads that go by it
+        load_k(tl);
+        load_v(tl);
         for (int k0 = kbase; k0 < kend; k0 += kUnit) {
             asm volatile("" ::: "memory");   // the queries are read from LDS anew
             const bool more = k0 + kUnit < kend;
-            int pn[2] = {0, 0};
-            bad = bad_next;
+            bad = (uint32_t)tl.bad;
             if (more) {
-                bad_next = take_pages<2>(a, it, k0 + kUnit, entry, pn);
-                entry = load_pages<2>(a, it, k0 + 2 * kUnit);
+                tl = take_tiles<2, kE4m3>(a, it, k0 + kUnit, entry, kv);
+                entry = load_entry<2>(a, it, k0 + 2 * kUnit);
             }
             const bool plain = k0 >= all_lo && k0 + 32 <= all_hi && bad == 0;   // every row sees every key
 
@@ -440,14 +469,14 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
                 }
             }
             f32x4_t ks[2];
-            if constexpr (kE4m3) ks[0] = kf[0], ks[1] = kf[1];
-            if (more) load_k(k0 + kUnit, pn);
+            if constexpr (kE4m3) ks[0] = kf[0] * c1, ks[1] = kf[1] * c1;
+            if (more) load_k(tl);
 
 #pragma unroll
             for (int n = 0; n < kMT; ++n) {
                 const float sc = scale_scores<kE4m3>(a, x[n], c1, ks[0], ks[1]);
                 const int j = k0 + 4 * g;
-                if (!plain) mask_scores(x[n], Seen{see_lo[n] - j, see_hi[n] - j, keys_of(bad) >> (4 * g)});
+                if (!plain) mask_scores(x[n], Seen{see_lo[n] - j, see_hi[n] - j, bad >> (4 * g)});
                 weigh<NJ>(x[n], sc, m[n], l[n], o[n]);
             }
             if constexpr (kE4m3) {
@@ -524,7 +553,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
                 if (!plain) mask_values(vr);
                 add_product(vr);
             }
-            if (more) load_v(k0 + kUnit, pn);
+            if (more) load_v(tl);
         }
 
         // The four waves' results joined: a common maximum, then, for each register r of
@@ -679,35 +708,24 @@ __device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds,
     u32x4_t kr[KL];
     uint32_t vr[8][1][VW];
     float sc = 0.f;
-    int bad_next = 0, entry = load_pages<4>(a, it, kbase);
+    uint64_t bad_next = 0;
+    int entry = load_entry<4>(a, it, kbase);
     auto fetch = [&](int k0) {
-        int pg[4];
-        bad_next = take_pages<4>(a, it, k0, entry, pg);
-        entry = load_pages<4>(a, it, k0 + kStep);   // ahead of the loads that go by it
-        auto tile_at = [&](int page, int pos) {
-            return (int64_t)page * a.c.page + (int64_t)(pos & ((1 << a.c.shift) - 1)) * a.c.slot;
-        };
-        const int kp = wave == 0 ? pg[0] : wave == 1 ? pg[1] : wave == 2 ? pg[2] : pg[3];
-        const char *row = kh + tile_at(kp, k0 + 16 * wave);
+        const Tiles<4> tl = take_tiles<4, kE4m3>(a, it, k0, entry, kv);
+        bad_next = tl.bad;
+        entry = load_entry<4>(a, it, k0 + kStep);   // ahead of the loads that go by it
+        const auto kb = buffer_at(kh + (wave == 0 ? tl.at[0] : wave == 1 ? tl.at[1] : wave == 2 ? tl.at[2] : tl.at[3]));
 #pragma unroll
-        for (int s = 0; s < KL; ++s) kr[s] = *reinterpret_cast<const u32x4_t *>(row + k_off + 64 * s);
+        for (int s = 0; s < KL; ++s) kr[s] = buffer_load16(kb, k_off + 64 * s, 0);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int vt = 2 * (wave >> 1) + t;
-            const char *vrow = vh + tile_at(wave >> 1 ? pg[2 + t] : pg[t], k0 + 16 * vt);
+            const auto vb = buffer_at(vh + (wave >> 1 ? tl.at[2 + t] : tl.at[t]));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                vr[4 * t + i][0][0] = 0;
-                __builtin_memcpy(vr[4 * t + i][0], __builtin_assume_aligned(vrow + i * slot + v_off, VB), VB);
-            }
+            for (int i = 0; i < 4; ++i) buffer_load<VB>(vr[4 * t + i][0], vb, v_off, i * slot);
         }
-        if constexpr (kE4m3) {
-            // wave 0: the keys' scales, wave 1: the values'
-            if (wave < 2) {
-                const int p = lane < 16 ? pg[0] : lane < 32 ? pg[1] : lane < 48 ? pg[2] : pg[3];
-                sc = (wave ? a.c.vs : a.c.ks)[scale_at(a.c, p, k0 + lane, kv)];
-            }
-        }
+        // The keys' scales for wave 0, the values' for wave 1 (and 2 and 3, which have no use
+        // for them: a branch here had the compiler wait for all loads before it).
+        if constexpr (kE4m3) sc = (wave ? a.c.vs : a.c.ks)[tl.scale];
     };
     // What was fetched for the keys from k0 on, as operands in LDS.
     auto stage = [&](int k0, int buf) {
@@ -760,6 +778,7 @@ __device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds,
         for (int j = 0; j < VE; ++j)
             lds.v[buf][wave >> 1][VE * (wave & 1) + j][lane] = __builtin_bit_cast(u32x4_t, value_operand(vp, 0, j / 2, j & 1));
         if constexpr (kE4m3) {
+            if (wave == 0) sc *= c1;
             if (wave == 1) {
                 // a scale that is not finite, as with the values
                 const uint64_t ball = __ballot(!(fabsf(sc) < INFINITY));
@@ -771,7 +790,8 @@ __device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds,
     };
 
     fetch(kbase);
-    int bad = bad_next, buf = 0;
+    uint64_t bad = bad_next;
+    int buf = 0;
     __syncthreads();   // the item before is done with LDS
     stage(kbase, 0);
     __syncthreads();
@@ -801,7 +821,7 @@ __device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds,
                 // (a value that is not finite: as if its key's page were bad)
                 uint32_t nan = 0;
                 if (!plain) {
-                    nan = keys_of(bad >> (2 * hh)) | lds.odd[buf][hh][0] | lds.odd[buf][hh][1];
+                    nan = (uint32_t)(bad >> (32 * hh)) | lds.odd[buf][hh][0] | lds.odd[buf][hh][1];
                     if constexpr (kE4m3) nan |= lds.odd[buf][hh][2];
                     nan >>= 4 * g;
                 }
