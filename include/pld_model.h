@@ -68,9 +68,9 @@ typedef struct pld_cache {
     float *k_scale;        /* PLD_E4M3 only, else NULL: a stored element stands for   */
     float *v_scale;        /*   itself times scale[page*scale_page_stride +           */
     int64_t scale_page_stride; /* head*page_size + slot]; 16-byte aligned,            */
-                           /*   scale_page_stride a multiple of 4                     */
+                           /*   scale_page_stride a multiple of 4, <= 2^31            */
     int64_t page_stride, slot_stride, head_stride;   /* elements; multiples of 16 bytes; */
-                           /*   slot_stride <= 2^24                                   */
+                           /*   slot_stride <= 2^24, page_stride <= 2^34              */
     const int32_t *table;  /* [B][table_stride]; an entry outside [0, num_pages) is a bad page */
     int64_t table_stride;  /* >= max_pages */
     int num_pages;         /* >= 1 */

@@ -64,13 +64,14 @@ inline int prep_cache(const pld_cache *c, bool needs_v, CacheView &o) {
     const int64_t spage = c->num_pages > 1 ? c->scale_page_stride : (int64_t)c->heads * ps;
     if (c->slot_stride < c->head_dim || head < c->head_dim || page < c->head_dim)
         return PLD_ERR_INVALID;
-    if (c->slot_stride > 1 << 24) return PLD_ERR_INVALID;   // a tile's offsets are 32-bit
+    // a tile's offsets, and a page's stride in 16 bytes, are 32-bit
+    if (c->slot_stride > 1 << 24 || page > (int64_t)1 << 34) return PLD_ERR_INVALID;
     const int64_t esz = q8 ? 1 : 2;
     if ((uintptr_t)c->k % 16 || (needs_v && (uintptr_t)c->v % 16) || (uintptr_t)c->table % 4 ||
         page * esz % 16 || c->slot_stride * esz % 16 || head * esz % 16)
         return PLD_ERR_ALIGN;
     if (q8) {
-        if (spage < (int64_t)c->heads * ps) return PLD_ERR_INVALID;
+        if (spage < (int64_t)c->heads * ps || spage > (int64_t)1 << 31) return PLD_ERR_INVALID;
         if ((uintptr_t)c->k_scale % 16 || (needs_v && (uintptr_t)c->v_scale % 16) ||
             spage % 4)
             return PLD_ERR_ALIGN;

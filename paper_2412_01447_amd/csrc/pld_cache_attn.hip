@@ -14,6 +14,8 @@ struct AttnArgs {
     float cap2;                     // cap in log2 units
     int window;
     int G, groups;                  // query heads per key head; row groups per sequence
+    uint32_t page16, slot16;        // strides of a page and a slot in 16 bytes
+    uint32_t spage32;               // scale stride of a page
     uint16_t *out;
     int64_t os, orow;
     float *lse;
@@ -204,25 +206,26 @@ __device__ __forceinline__ int load_entry(const AttnArgs &a, const Item &it, int
     const int j = min(k0 + (lane_id() & (16 * T - 1)), it.hi - 1);
     return a.c.table[(int64_t)it.b * a.c.table_stride + (j >> a.c.shift)];
 }
-template <int T>
 struct Tiles {
-    int64_t at[T];   // of a tile's first row, in bytes
-    int64_t scale;   // of this lane's key
+    uint64_t at;       // of the first row of this lane's tile, in 16 bytes
+    int64_t scale;     // of this lane's key
     uint64_t bad;
+    // Tile t's first row in bytes, from a uniform t.
+    __device__ __forceinline__ int64_t row(int t) const { return (int64_t)(read(at, 16 * t) << 4); }
+    __device__ __forceinline__ int64_t first_scale(int t) const { return (int64_t)read((uint64_t)scale, 16 * t); }
+    __device__ __forceinline__ static uint64_t read(uint64_t v, int l) {
+        return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), l) << 32 |
+               (uint32_t)__builtin_amdgcn_readlane((int)v, l);
+    }
 };
-__device__ __forceinline__ int64_t readlane(int64_t v, int l) {
-    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), l) << 32 |
-                     (uint32_t)__builtin_amdgcn_readlane((int)v, l));
-}
 template <int T, bool kScales>
-__device__ __forceinline__ Tiles<T> take_tiles(const AttnArgs &a, const Item &it, int k0, int entry, int kv) {
-    Tiles<T> r;
+__device__ __forceinline__ Tiles take_tiles(const AttnArgs &a, const Item &it, int k0, int entry, int kv) {
+    Tiles r;
     const bool ok = (uint32_t)entry < (uint32_t)a.c.num_pages;
-    const int page = ok ? entry : 0, j = k0 + (lane_id() & (16 * T - 1)), mask = (1 << a.c.shift) - 1;
-    const int64_t at = (int64_t)page * a.c.page + (int64_t)(j & mask & ~15) * a.c.slot;
-#pragma unroll
-    for (int t = 0; t < T; ++t) r.at[t] = readlane(at, 16 * t);
-    if constexpr (kScales) r.scale = (int64_t)page * a.c.spage + ((int64_t)kv << a.c.shift) + (j & mask);
+    const uint32_t page = ok ? entry : 0, mask = (1u << a.c.shift) - 1;
+    const int j = k0 + (lane_id() & (16 * T - 1));
+    r.at = (uint64_t)page * a.page16 + ((uint32_t)j & mask & ~15u) * a.slot16;
+    if constexpr (kScales) r.scale = (int64_t)((uint64_t)page * a.spage32 + (((uint32_t)kv << a.c.shift) + ((uint32_t)j & mask)));
     r.bad = __ballot(!ok && j < it.hi);
     return r;
 }
@@ -409,32 +412,32 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
         const char *kh = a.c.k + (int64_t)kv * a.c.head, *vh = a.c.v + (int64_t)kv * a.c.head;
         const uint32_t slot = (uint32_t)a.c.slot;
         const uint32_t k_off = (uint32_t)c * slot + 16 * g, v_off = 4 * (uint32_t)g * slot + c * (4 * VW);
-        auto load_k = [&](const Tiles<2> &tl) {
+        auto load_k = [&](const Tiles &tl) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const auto buf = buffer_at(kh + tl.at[t]);
+                const auto buf = buffer_at(kh + tl.row(t));
 #pragma unroll
                 for (int s = 0; s < KL; ++s) kr[t][s] = buffer_load16(buf, k_off + 64 * s, 0);
                 if constexpr (kE4m3)
-                    kf[t] = __builtin_bit_cast(f32x4_t, buffer_load16(buffer_at(a.c.ks + readlane(tl.scale, 16 * t)), 16 * g, 0));
+                    kf[t] = __builtin_bit_cast(f32x4_t, buffer_load16(buffer_at(a.c.ks + tl.first_scale(t)), 16 * g, 0));
             }
         };
-        auto load_v = [&](const Tiles<2> &tl) {
+        auto load_v = [&](const Tiles &tl) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const auto buf = buffer_at(vh + tl.at[t]);
+                const auto buf = buffer_at(vh + tl.row(t));
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int v = 0; v < NV; ++v)
                         buffer_load<4 * VW>(vr[4 * t + i][v], buf, v_off + v * (64 * VW), i * slot);
                 if constexpr (kE4m3)
-                    vf[t] = __builtin_bit_cast(f32x4_t, buffer_load16(buffer_at(a.c.vs + readlane(tl.scale, 16 * t)), 16 * g, 0));
+                    vf[t] = __builtin_bit_cast(f32x4_t, buffer_load16(buffer_at(a.c.vs + tl.first_scale(t)), 16 * g, 0));
             }
         };
 
         int entry = load_entry<2>(a, it, kbase);
-        Tiles<2> tl = take_tiles<2, kE4m3>(a, it, kbase, entry, kv);
+        Tiles tl = take_tiles<2, kE4m3>(a, it, kbase, entry, kv);
         entry = load_entry<2>(a, it, kbase + kUnit);   // ahead of the loads that go by it
         load_k(tl);
         load_v(tl);
@@ -711,15 +714,15 @@ __device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds,
     uint64_t bad_next = 0;
     int entry = load_entry<4>(a, it, kbase);
     auto fetch = [&](int k0) {
-        const Tiles<4> tl = take_tiles<4, kE4m3>(a, it, k0, entry, kv);
+        const Tiles tl = take_tiles<4, kE4m3>(a, it, k0, entry, kv);
         bad_next = tl.bad;
         entry = load_entry<4>(a, it, k0 + kStep);   // ahead of the loads that go by it
-        const auto kb = buffer_at(kh + (wave == 0 ? tl.at[0] : wave == 1 ? tl.at[1] : wave == 2 ? tl.at[2] : tl.at[3]));
+        const auto kb = buffer_at(kh + tl.row(wave));
 #pragma unroll
         for (int s = 0; s < KL; ++s) kr[s] = buffer_load16(kb, k_off + 64 * s, 0);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const auto vb = buffer_at(vh + (wave >> 1 ? tl.at[2 + t] : tl.at[t]));
+            const auto vb = buffer_at(vh + tl.row(2 * (wave >> 1) + t));
 #pragma unroll
             for (int i = 0; i < 4; ++i) buffer_load<VB>(vr[4 * t + i][0], vb, v_off, i * slot);
         }
@@ -1065,6 +1068,8 @@ static int prep_attn(const pld_cache *cache, bool needs_v, const uint16_t *q, in
     a.cap2 = softcap * kLog2E;
     a.inv2_log2e = softcap > 0.f ? 2.f / softcap : 0.f;   // 2 log2(e) / (cap log2(e))
     a.G = Hq / cache->heads;
+    a.page16 = (uint32_t)(a.c.page / 16), a.slot16 = (uint32_t)(a.c.slot / 16);
+    a.spage32 = (uint32_t)a.c.spage;
     a.window = window;
     return PLD_OK;
 }
