@@ -19,21 +19,25 @@ struct LogprobArgs {
     int32_t *top_ids;
     float *top_lp;
     int segs;           // segments per row
-    int4 *opened;       // [waves]: (sequence, row, last wave, -) of a row that spans waves
-    float *partials;    // [waves][2]: maximum, mass, mass times exponent, -, then `top` keys
+    int2 *parts;        // [B][n]: first and last wave of a row
+    float4 *masses;     // [waves][2]: reference, mass, mass times exponent of a wave's part of a row
+    void *maxima;       // [B][n][segs][64], the logits' type: each lane's largest value of a segment
 };
 
 // A segment of a row is 32 elements a lane, one wave's work at a time, in 16-byte vectors:
 // lane l has the vectors l, l + 64, ...  The segments of all rows that exist, in order, are
-// dealt to the waves in equal contiguous ranges; a row that spans waves leaves one partial
-// result per wave (slot 0 of a wave: a row that began before it, slot 1: one that ends
-// after it), joined by a second launch.
+// dealt to the waves in equal contiguous ranges.  A wave sums up the masses of its part of a
+// row (slot 0: a row that began before it, slot 1: one that begins in it) and, where
+// alternatives are asked for, keeps each lane's largest value of a segment: 1/32 of the
+// logits, which tell a second launch, a wave per row, where the row's best elements are.
+// (Kept by the first pass itself, the best twenty cost as much as the pass: 95 us, and 46
+// without them, for 64 x 17 rows of 128256 in bf16.)
 constexpr int kLogElems = 32;
 template <int P>
 constexpr int kLogLoads = kLogElems / P;
 constexpr int kLogBlocks = 1024, kLogWaves = 4;   // 16 waves a CU
-constexpr int kKeys = 512;                        // keys a wave keeps at most before it sorts them out
-constexpr int kHits = 32;
+constexpr int kKeys = 256;                        // keys a wave keeps at most before it sorts them out
+constexpr int kGroups = 128;                      // (segment, lane) groups of elements to look at
 
 // A mass is 2^x with x = z k - c for a c near the largest z k: one fused multiply-add whose
 // only error is x's own rounding, whatever c is.  s sums 2^x, t sums 2^x x (the entropy is
@@ -55,6 +59,12 @@ struct Mass {
         s += e;
         t = fmaf(e, x, t);
     }
+    // all lanes' masses together, in every lane
+    __device__ __forceinline__ void join_lanes() {
+        raise(wave_max_f32(c));
+        s = wave_sum_f32(s);
+        t = wave_sum_f32(t);
+    }
 };
 // The reference of a largest value z (finite, also where z k is not).
 __device__ __forceinline__ float reference(float z, float k) { return fminf(fmaxf(z * k, kNoMass), FLT_MAX); }
@@ -70,17 +80,11 @@ __device__ __forceinline__ float next_up(float v) {
 // below `at`, cannot be among them.
 struct Best {
     uint64_t *buf, *sorted;   // [kKeys], [PLD_MAX_TOP]
-    int N, cnt;
-    uint64_t floor;
-    float at;
-    bool full;   // N keys at or above `at` are there
+    int N, cnt = 0;
+    uint64_t floor = 0;
+    float at = -INFINITY;
+    bool full = false;        // N keys at or above `at` are there
 
-    __device__ __forceinline__ void reset() {
-        cnt = 0;
-        full = false;
-        floor = 0;
-        at = -INFINITY;
-    }
     // Ranks by counting: the keys are distinct.
     __device__ __forceinline__ void compress() {
         const int lane = lane_id();
@@ -111,82 +115,39 @@ struct Best {
         asm volatile("" ::: "memory");
         if (cnt > kKeys - kWave) compress();
     }
+    // As append(), for up to kEach keys a lane (key(e) where `mask` has bit e): in one go
+    // where there is room, which there is but for rows of many equal values.
+    template <int kEach, class Key>
+    __device__ __forceinline__ void append_some(uint32_t mask, Key key) {
+        int total;
+        int to = cnt + wave_excl_scan(__popc(mask), total);
+        if (total == 0) return;
+        if (cnt + total <= kKeys) {
+            cnt += total;
+            for (; mask; mask &= mask - 1) buf[to++] = key(__ffs(mask) - 1);
+            asm volatile("" ::: "memory");
+            if (cnt > kKeys - kWave) compress();
+        } else {
+            for (int e = 0; e < kEach; ++e) append(key(e), (mask >> e) & 1);
+        }
+    }
     // The N-th best of the lanes' own best values (`own`, as ord_f32 has them; 0: none) is a
-    // floor; where more lanes than are needed have it, the indexes (`index`, called then)
-    // decide.  Of a bf16 value the upper half of ord_f32 says all.
-    template <bool kBf16, class Index>
-    __device__ __forceinline__ void raise_floor(uint32_t own, Index index) {
-        uint32_t v = 0, w = 0;
+    // floor of the values.  Of a bf16 value the upper half of ord_f32 says all.
+    template <bool kBf16>
+    __device__ __forceinline__ void raise_floor(uint32_t own) {
+        uint32_t v = 0;
         for (uint32_t bit = 1u << 31; bit > (kBf16 ? 0x8000u : 0u); bit >>= 1)
             if (__popcll(__ballot(own >= (v | bit))) >= N) v |= bit;
         if (v == 0) return;   // fewer than N lanes have one
         if (kBf16 && !(v >> 31)) v |= 0xffffu;
-        const int need = N - __popcll(__ballot(own > v));
-        if (__popcll(__ballot(own == v)) > need) {
-            const uint32_t lo = own == v ? 0xffffffffu - index() : 0;
-            for (uint32_t bit = 1u << 31; bit; bit >>= 1)
-                if (__popcll(__ballot(lo >= (w | bit))) >= need) w |= bit;
-        }
-        floor = max(floor, (uint64_t)v << 32 | w);
+        floor = max(floor, (uint64_t)v << 32);
         at = fmaxf(at, unord_f32(v));
     }
 };
 
-// What a row's results come from: its mass over all lanes or waves, and its best keys.
-template <int kBf16>
-__device__ __forceinline__ void put_row(const LogprobArgs &a, int b, int i, Mass w, const Best &best) {
-    using E = Elem<kBf16>;
-    using T = typename E::T;
-    const T *z = reinterpret_cast<const T *>(a.logits) + (int64_t)b * a.ls + (int64_t)i * a.lr;
-    const int lane = lane_id();
-    const int64_t at = (int64_t)b * a.n + i;
-    // No mass: only -inf, or logits so low (a mask of the type's lowest value) that times k
-    // they overflow: then relative to their own maximum m.
-    bool none = false;
-    float m = 0.f;
-    if (!(w.s > 0.f)) {
-        m = -INFINITY;
-        for (int v = lane; v < a.V; v += kWave) m = fmaxf(m, E::get(z, v));
-        m = wave_max_f32(m);
-        none = !(m > -INFINITY);
-        w = Mass{0.f, 0.f, 0.f};
-        for (int v = lane; v < a.V && !none; v += kWave) w.add(E::get(z, v) - m, a.k);
-        w.s = wave_sum_f32(w.s);
-        w.t = wave_sum_f32(w.t);
-    }
-    const float log2_s = __builtin_amdgcn_logf(w.s);
-    auto logprob = [&](float x) { return none ? -INFINITY : (fmaf(x - m, a.k, -w.c) - log2_s) * 0.6931471805599453f; };
-    if (lane == 0) {
-        const int tok = a.tokens[at];
-        a.logprob[at] = tok >= 0 && tok < a.V ? logprob(E::get(z, tok)) : __uint_as_float(0x7fc00000u);
-        if (a.entropy) a.entropy[at] = none ? 0.f : fmaxf((log2_s - w.t / w.s) * 0.6931471805599453f, 0.f);
-    }
-    if (lane < a.top) {
-        const bool have = lane < best.cnt;
-        const uint64_t key = have ? best.buf[lane] : 0;
-        a.top_ids[at * a.top + lane] = have ? (int)argmax_key_index(key) : -1;
-        a.top_lp[at * a.top + lane] = have ? logprob(unord_f32((uint32_t)(key >> 32))) : -INFINITY;
-    }
-}
-
-// (whole 16-byte vectors)
-__host__ __device__ inline int part_floats(int top) { return 4 + 4 * ((top + 1) / 2); }
-__device__ __forceinline__ float *partial_at(const LogprobArgs &a, int wave, int slot) {
-    return a.partials + ((int64_t)wave * 2 + slot) * part_floats(a.top);
-}
-
 __device__ __forceinline__ int rows_of(const LogprobArgs &a, int b) {
     const int c = a.count ? a.count[b] : a.n;
     return c < 0 || c > a.n ? 0 : c;
-}
-
-// A vector's elements back together (exact).
-__device__ __forceinline__ uint4 pack(const float (&z)[4]) {
-    return make_uint4(__float_as_uint(z[0]), __float_as_uint(z[1]), __float_as_uint(z[2]), __float_as_uint(z[3]));
-}
-__device__ __forceinline__ uint4 pack(const float (&z)[8]) {
-    auto two = [&](int i) { return __float_as_uint(z[i]) >> 16 | __float_as_uint(z[i + 1]); };
-    return make_uint4(two(0), two(2), two(4), two(6));
 }
 
 template <int kBf16, bool kTop>
@@ -196,8 +157,6 @@ __global__ __launch_bounds__(kLogWaves * 64, 4) void token_logprobs_kernel(Logpr
     constexpr int P = E::kPerVec;
     constexpr uint32_t kNegInf2 = kBf16 ? 0xff80ff80u : 0xff800000u;
     constexpr int L = kLogLoads<P>, kVecs = L * kWave;
-    __shared__ uint64_t s_keys[kTop ? kLogWaves : 1][kTop ? kKeys + PLD_MAX_TOP : 1];
-    __shared__ uint4 s_hits[kTop ? kLogWaves : 1][kTop ? kHits : 1][L];
     __shared__ int64_t s_w[kLogWaves], s_first[kLogWaves];
     __shared__ int s_b[kLogWaves];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
@@ -236,22 +195,17 @@ __global__ __launch_bounds__(kLogWaves * 64, 4) void token_logprobs_kernel(Logpr
     }
     __syncthreads();
     const int id = (int)blockIdx.x * kLogWaves + wave;
-    int4 opened = make_int4(-1, 0, 0, 0);
-    if (id >= ranges) {
-        if (lane == 0) a.opened[id] = opened;
-        return;
-    }
+    if (id >= ranges) return;
     int64_t x = total * id / ranges;
     const int64_t x1 = total * (id + 1) / ranges;
     int b = __builtin_amdgcn_readfirstlane(s_b[wave]), cnt = rows_of(a, b);
     int i = (int)(x / a.segs - s_first[wave]), g = (int)(x % a.segs);
-    Best best{s_keys[kTop ? wave : 0], s_keys[kTop ? wave : 0] + (kTop ? kKeys : 0), a.top, 0, 0, -INFINITY, false};
 
     while (x < x1) {
         const RowView<T, P> rv = row_view<T, P>(a.logits, a.ls, a.lr, b, i, a.V);
+        const int64_t row = (int64_t)b * a.n + i;
         const int g0 = g, g1 = (int)min((int64_t)a.segs, g + (x1 - x));
         Mass w;
-        best.reset();
         uint4 r[L];
         auto load = [&](int seg) {
             const int64_t v0 = (int64_t)seg * kVecs + lane;
@@ -263,11 +217,13 @@ __global__ __launch_bounds__(kLogWaves * 64, 4) void token_logprobs_kernel(Logpr
         };
         load(g);
         for (; g < g1; ++g) {
-            const int64_t v0 = (int64_t)g * kVecs + lane;
-            const bool head = g == 0 && lane < rv.head;
-            const bool tail = g == a.segs - 1 && rv.body_end + lane < a.V;
-            const float zh = head ? E::get(rv.row, lane) : -INFINITY;
-            const float zt = tail ? E::get(rv.row, rv.body_end + lane) : -INFINITY;
+            // elements before the first whole vector, or after the last one
+            float zh = -INFINITY, zt = -INFINITY;
+            const bool ends = (g == 0 && rv.head) || (g == a.segs - 1 && rv.body_end < a.V);
+            if (ends) {
+                if (g == 0 && lane < rv.head) zh = E::get(rv.row, lane);
+                if (g == a.segs - 1 && rv.body_end + lane < a.V) zt = E::get(rv.row, rv.body_end + lane);
+            }
             float z[L][P], top = fmaxf(zh, zt);
 #pragma unroll
             for (int u = 0; u < L; ++u) {
@@ -276,89 +232,28 @@ __global__ __launch_bounds__(kLogWaves * 64, 4) void token_logprobs_kernel(Logpr
                 for (int e = 0; e < P; ++e) top = fmaxf(top, z[u][e]);
             }
             if (g + 1 < g1) load(g + 1);   // under this segment's work
+            if constexpr (kTop) {
+                const int64_t at = (row * a.segs + g) * kWave + lane;
+                if constexpr (kBf16)
+                    static_cast<uint16_t *>(a.maxima)[at] = (uint16_t)(__float_as_uint(top) >> 16);
+                else
+                    static_cast<float *>(a.maxima)[at] = top;
+            }
             w.raise(fmaxf(w.c, reference(top, a.k)));
-            w.add(zh, a.k);
-            w.add(zt, a.k);
+            if (ends) {
+                w.add(zh, a.k);
+                w.add(zt, a.k);
+            }
 #pragma unroll
             for (int u = 0; u < L; ++u)
 #pragma unroll
                 for (int e = 0; e < P; ++e) w.add(z[u][e], a.k);
-            if constexpr (kTop) {
-                // Values from `gate` on are looked at.  With N keys already, a later equal
-                // value loses to them; before that, the lanes' own maxima give a floor.
-                const bool boot = !best.full;
-                if (boot)
-                    best.raise_floor<kBf16>(head || tail || v0 < rv.nvec ? ord_f32(top) : 0, [&] {
-                        // this lane's lowest index of `top`
-                        uint32_t idx = 0xffffffffu;
-                        if (zt == top && tail) idx = (uint32_t)(rv.body_end + lane);
-#pragma unroll
-                        for (int u = L - 1; u >= 0; --u) {
-                            const bool in = v0 + u * kWave < rv.nvec;
-#pragma unroll
-                            for (int e = P - 1; e >= 0; --e)
-                                if (in && z[u][e] == top) idx = (uint32_t)(rv.head + (v0 + u * kWave) * P + e);
-                        }
-                        if (zh == top && head) idx = (uint32_t)lane;
-                        return idx;
-                    });
-                const float gate = boot ? best.at : next_up(best.at);
-                uint64_t hits = __ballot(top >= gate);
-                if (hits) {
-                    best.append(argmax_key(zh, (uint32_t)lane), head && zh >= gate);
-                    // The lanes with such values put their vectors into LDS, kHits at a time,
-                    // and the wave reads a lane's elements side by side.
-                    while (hits) {
-                        const int slot = __popcll(hits & lanemask_lt());
-                        if (((hits >> lane) & 1) && slot < kHits) {
-#pragma unroll
-                            for (int u = 0; u < L; ++u) s_hits[wave][slot][u] = pack(z[u]);
-                        }
-                        asm volatile("" ::: "memory");
-                        // two lanes' elements side by side
-                        const int e = lane & (kLogElems - 1), half = lane / kLogElems;
-                        constexpr int kAhead = kBf16 ? 2 : 1;
-                        for (int h = 0; hits && h < kHits; h += 2 * kAhead) {
-                            float y[kAhead];
-#pragma unroll
-                            for (int q = 0; q < kAhead; ++q)
-                                y[q] = E::get(reinterpret_cast<const T *>(s_hits[wave][h + 2 * q + half]), e);
-#pragma unroll
-                            for (int q = 0; q < kAhead; ++q) {
-                                if (hits == 0) break;
-                                const int l0 = __ffsll((unsigned long long)hits) - 1;
-                                hits &= hits - 1;
-                                const int l1 = __ffsll((unsigned long long)hits) - 1;   // -1: none
-                                hits &= hits - 1;
-                                const int from = half ? l1 : l0;
-                                const int64_t vi = (int64_t)g * kVecs + from + (e / P) * kWave;
-                                best.append(argmax_key(y[q], (uint32_t)(rv.head + vi * P + e % P)),
-                                            from >= 0 && vi < rv.nvec && y[q] >= gate);
-                            }
-                        }
-                        asm volatile("" ::: "memory");
-                    }
-                    best.append(argmax_key(zt, (uint32_t)(rv.body_end + lane)), tail && zt >= gate);
-                    if (boot || best.cnt > 2 * kWave) best.compress();
-                }
-            }
         }
-        if constexpr (kTop) best.compress();
         x += g1 - g0;
-        // the lanes' masses to a common maximum
-        w.raise(wave_max_f32(w.c));
-        w.s = wave_sum_f32(w.s);
-        w.t = wave_sum_f32(w.t);
-        if (g0 == 0 && g1 == a.segs) {
-            put_row<kBf16>(a, b, i, w, best);
-        } else {
-            float *part = partial_at(a, id, g0 == 0);
-            if (lane == 0) *reinterpret_cast<float4 *>(part) = make_float4(w.c, w.s, w.t, 0.f);
-            if (kTop && lane < a.top) reinterpret_cast<uint64_t *>(part + 4)[lane] = lane < best.cnt ? best.buf[lane] : 0;
-            if (g0 == 0) {
-                const int64_t end = x + (a.segs - g1);   // of the row
-                opened = make_int4(b, i, (int)((end * ranges - 1) / total), 0);
-            }
+        w.join_lanes();
+        if (lane == 0) {
+            a.masses[(int64_t)id * 2 + (g0 == 0)] = make_float4(w.c, w.s, w.t, 0.f);
+            if (g0 == 0) a.parts[row] = make_int2(id, (int)(((x + (a.segs - g1)) * ranges - 1) / total));
         }
         g = 0;
         if (x < x1 && ++i >= cnt) {
@@ -367,22 +262,27 @@ __global__ __launch_bounds__(kLogWaves * 64, 4) void token_logprobs_kernel(Logpr
             while (cnt == 0);
         }
     }
-    if (lane == 0) a.opened[id] = opened;
 }
 
-// A wave per row that spans waves, in the order of the waves that open one.
+// A wave per row: the masses of its parts joined, and its best elements.
 template <int kBf16, bool kTop>
-__global__ __launch_bounds__(kLogWaves * 64) void token_logprobs_join_kernel(LogprobArgs a) {
+__global__ __launch_bounds__(kLogWaves * 64) void token_logprobs_finish_kernel(LogprobArgs a) {
+    using E = Elem<kBf16>;
+    using T = typename E::T;
+    constexpr int P = E::kPerVec, L = kLogLoads<P>, kVecs = L * kWave;
     __shared__ uint64_t s_keys[kTop ? kLogWaves : 1][kTop ? kKeys + PLD_MAX_TOP : 1];
+    __shared__ int s_groups[kTop ? kLogWaves : 1][kTop ? kGroups : 1];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
-    const int id = (int)blockIdx.x * kLogWaves + wave;
-    const int4 row = a.opened[id];
-    if (row.x < 0) return;
-    const int parts = row.z - id + 1;
-    auto part = [&](int p) { return partial_at(a, id + p, p == 0); };
+    const int b = blockIdx.y, i = (int)blockIdx.x * kLogWaves + wave;
+    if (i >= rows_of(a, b)) return;
+    const int64_t row = (int64_t)b * a.n + i;
+    const RowView<T, P> rv = row_view<T, P>(a.logits, a.ls, a.lr, b, i, a.V);
+    const int2 part = a.parts[row];
+    const int tok = a.tokens[row];
+    const float z_tok = E::get(rv.row, tok >= 0 && tok < a.V ? tok : 0);
     Mass w;
-    for (int p = lane; p < parts; p += 64) {
-        const float4 v = *reinterpret_cast<const float4 *>(part(p));
+    for (int p = part.x + lane; p <= part.y; p += kWave) {
+        const float4 v = a.masses[(int64_t)p * 2 + (p == part.x)];
         Mass o;
         o.c = v.x, o.s = v.y, o.t = v.z;
         const float cn = fmaxf(w.c, o.c);
@@ -391,45 +291,160 @@ __global__ __launch_bounds__(kLogWaves * 64) void token_logprobs_join_kernel(Log
         w.s += o.s;
         w.t += o.t;
     }
-    w.raise(wave_max_f32(w.c));
-    w.s = wave_sum_f32(w.s);
-    w.t = wave_sum_f32(w.t);
-    Best best{s_keys[kTop ? wave : 0], s_keys[kTop ? wave : 0] + (kTop ? kKeys : 0), a.top, 0, 0, -INFINITY, false};
+
+    Best best{s_keys[kTop ? wave : 0], s_keys[kTop ? wave : 0] + (kTop ? kKeys : 0), a.top};
     if constexpr (kTop) {
-        best.reset();
-        // sorted lists: 64 of them at a time, to the depth at which none has a key in reach
-        for (int p0 = 0; p0 < parts; p0 += 64) {
-            const bool in = p0 + lane < parts;
-            const uint64_t *list = reinterpret_cast<const uint64_t *>(part(in ? p0 + lane : 0) + 4);
-            constexpr int kAhead = 4;
-            for (int k0 = 0; k0 < a.top; k0 += kAhead) {
-                uint64_t key[kAhead];
+        // Each lane's largest of the maxima; the top-th largest of those is a floor.
+        const uint4 *maxima = reinterpret_cast<const uint4 *>(static_cast<const T *>(a.maxima) + row * a.segs * kWave);
+        constexpr int kChunk = 8;   // vectors a lane: a bf16 row of up to 131072 at once
+        const int vecs = a.segs * (kWave / P);
+        uint4 m[kChunk];
+        auto load = [&](int v0) {
 #pragma unroll
-                for (int k = 0; k < kAhead; ++k) key[k] = in && k0 + k < a.top ? list[k0 + k] : 0;
-                if (k0 == 0 && !best.full)
-                    best.raise_floor<false>((uint32_t)(key[0] >> 32), [&] { return argmax_key_index(key[0]); });
-                bool any = false;
+            for (int q = 0; q < kChunk; ++q) m[q] = maxima[min(v0 + q * kWave + lane, vecs - 1)];
+        };
+        float own = -INFINITY;
+        for (int v0 = 0; v0 < vecs; v0 += kChunk * kWave) {
+            load(v0);
+            // (no other lane's vector in place of an absent one: the floor counts lanes)
 #pragma unroll
-                for (int k = 0; k < kAhead; ++k) {
-                    any = __any(key[k] != 0 && key[k] >= best.floor);
-                    if (any) best.append(key[k], key[k] != 0);
-                }
-                if (!any) break;
-            }
-            best.compress();
+            for (int q = 0; q < kChunk; ++q)
+                if (v0 + q * kWave + lane < vecs) own = fmaxf(own, E::vmax(m[q]));
         }
+        best.raise_floor<kBf16>(lane < vecs ? ord_f32(own) : 0);
+
+        // The groups of a list of (segment, lane), L lanes each: a vector a lane.
+        int *groups = s_groups[wave];
+        int listed = 0;
+        auto look = [&] {
+            asm volatile("" ::: "memory");
+            constexpr int kEach = kWave / L, kRounds = 4;   // groups a round, rounds in flight
+            for (int q0 = 0; q0 < listed; q0 += kEach * kRounds) {
+            uint4 vec[kRounds];
+            int at_group[kRounds];
+#pragma unroll
+            for (int t = 0; t < kRounds; ++t) {
+                at_group[t] = groups[min(q0 + t * kEach + lane / L, listed - 1)];
+                const int64_t vi = (int64_t)(at_group[t] / kWave) * kVecs + at_group[t] % kWave + lane % L * kWave;
+                vec[t] = rv.nvec ? rv.vec[min(vi, (int64_t)rv.nvec - 1)] : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int t = 0; t < kRounds; ++t) {
+                const int q = q0 + t * kEach + lane / L, u = lane % L;
+                if (q0 + t * kEach >= listed) continue;
+                const int seg = at_group[t] / kWave, l = at_group[t] % kWave;
+                const int64_t vi = (int64_t)seg * kVecs + l + u * kWave;
+                float z[P];
+                E::unpack(vec[t], z);
+                uint32_t mask = 0;
+                auto key = [&](int e) {
+                    float y = z[0];
+#pragma unroll
+                    for (int f = 1; f < P; ++f) y = e == f ? z[f] : y;
+                    return argmax_key(y, (uint32_t)(rv.head + vi * P + e));
+                };
+#pragma unroll
+                for (int e = 0; e < P; ++e)
+                    if (z[e] >= best.at && argmax_key(z[e], (uint32_t)(rv.head + vi * P + e)) >= best.floor) mask |= 1u << e;
+                best.append_some<P>(q < listed && vi < rv.nvec ? mask : 0, key);
+                const bool first = q < listed && u == 0;
+                if (rv.head) {
+                    const bool h = first && seg == 0 && l < rv.head;
+                    best.append(argmax_key(h ? E::get(rv.row, l) : 0.f, (uint32_t)l), h);
+                }
+                if (rv.body_end < a.V) {
+                    const bool t = first && seg == a.segs - 1 && rv.body_end + l < a.V;
+                    best.append(argmax_key(t ? E::get(rv.row, rv.body_end + l) : 0.f, (uint32_t)(rv.body_end + l)), t);
+                }
+            }
+            }
+            listed = 0;
+            best.compress();
+            asm volatile("" ::: "memory");
+        };
+        // All of the row's groups from the floor on at once, where they are few.
+        bool done = false;
+        if (vecs <= kChunk * kWave) {
+            uint64_t mask = 0;
+#pragma unroll
+            for (int q = 0; q < kChunk; ++q) {
+                float y[P];
+                E::unpack(m[q], y);
+#pragma unroll
+                for (int e = 0; e < P; ++e) mask |= (uint64_t)(q * kWave + lane < vecs && y[e] >= best.at) << (q * P + e);
+            }
+            int to = wave_excl_scan(__popcll(mask), listed);
+            done = listed <= kGroups;
+            if (done)
+                for (; mask; mask &= mask - 1) {
+                    const int bit = __ffsll((unsigned long long)mask) - 1;
+                    groups[to++] = (bit / P * kWave + lane) * P + bit % P;
+                }
+            else
+                listed = 0;
+        }
+        // Else in order of the vectors, that is of the segments: once there are `top` keys, an
+        // equal value of a later segment loses to them, and only larger ones are of interest.
+        // (64 vectors are whole segments.)
+        float gate = best.at;
+        for (int v0 = 0; v0 < vecs && !done; v0 += kWave) {
+            const int v = v0 + lane;
+            float y[P];
+            E::unpack(maxima[min(v, vecs - 1)], y);
+            for (int e = 0; e < P; ++e) {
+                const uint64_t hits = __ballot(v < vecs && y[0] >= gate);
+                if (hits) {
+                    if ((hits >> lane) & 1) groups[listed + __popcll(hits & lanemask_lt())] = v * P + e;
+                    listed += __popcll(hits);
+                }
+                // all that is listed, where no more has room or where these segments end
+                if (listed > kGroups - kWave || (e == P - 1 && listed >= kWave / L)) look();
+#pragma unroll
+                for (int f = 0; f + 1 < P; ++f) y[f] = y[f + 1];
+            }
+            if (best.full && listed == 0) gate = next_up(best.at);
+        }
+        if (listed) look();
     }
-    put_row<kBf16>(a, row.x, row.y, w, best);
+
+    w.join_lanes();
+    // No mass: only -inf, or logits so low (a mask of the type's lowest value) that times k
+    // they overflow: then relative to their own maximum m.
+    bool none = false;
+    float m = 0.f;
+    if (!(w.s > 0.f)) {
+        m = -INFINITY;
+        for (int v = lane; v < a.V; v += kWave) m = fmaxf(m, E::get(rv.row, v));
+        m = wave_max_f32(m);
+        none = !(m > -INFINITY);
+        w = Mass{0.f, 0.f, 0.f};
+        for (int v = lane; v < a.V && !none; v += kWave) w.add(E::get(rv.row, v) - m, a.k);
+        w.s = wave_sum_f32(w.s);
+        w.t = wave_sum_f32(w.t);
+    }
+    const float log2_s = __builtin_amdgcn_logf(w.s);
+    auto logprob = [&](float x) { return none ? -INFINITY : (fmaf(x - m, a.k, -w.c) - log2_s) * 0.6931471805599453f; };
+    if (lane == 0) {
+        a.logprob[row] = tok >= 0 && tok < a.V ? logprob(z_tok) : __uint_as_float(0x7fc00000u);
+        if (a.entropy) a.entropy[row] = none ? 0.f : fmaxf((log2_s - w.t / w.s) * 0.6931471805599453f, 0.f);
+    }
+    if (kTop && lane < a.top) {
+        const bool have = lane < best.cnt;
+        const uint64_t key = have ? best.buf[lane] : 0;
+        a.top_ids[row * a.top + lane] = have ? (int)argmax_key_index(key) : -1;
+        a.top_lp[row * a.top + lane] = have ? logprob(unord_f32((uint32_t)(key >> 32))) : -INFINITY;
+    }
 }
 
-static int log_segs(int V) {
-    const int64_t per = kLogElems * kWave;
-    return (int)((V + per - 1) / per);
-}
+static int log_segs(int V) { return (int)((V + (int64_t)kLogElems * kWave - 1) / (kLogElems * kWave)); }
 static int log_blocks(int B, int n, int segs) {
     const int64_t waves = (int64_t)B * n * segs, blocks = (waves + kLogWaves - 1) / kLogWaves;
     return (int)(blocks < kLogBlocks ? blocks : kLogBlocks);
 }
+static size_t log_masses_bytes(int B, int n, int segs) {
+    return (size_t)log_blocks(B, n, segs) * kLogWaves * 2 * sizeof(float4);
+}
+static size_t log_parts_bytes(int B, int n) { return align_up((size_t)B * n * sizeof(int2), 256); }
 
 }  // namespace pld
 
@@ -439,8 +454,9 @@ extern "C" size_t pld_token_logprobs_workspace_bytes(int B, int n, int V, int dt
     if (B < 1 || B > 65535 || n < 1 || n > 65535 || V < 1 || (dtype != PLD_F32 && dtype != PLD_BF16) ||
         top < 0 || top > PLD_MAX_TOP)
         return 0;
-    const size_t waves = (size_t)log_blocks(B, n, log_segs(V)) * kLogWaves;
-    return waves * (sizeof(int4) + 2 * (size_t)part_floats(top) * sizeof(float));
+    const int segs = log_segs(V);
+    const size_t maxima = top ? (size_t)B * n * segs * kWave * (dtype == PLD_F32 ? 4 : 2) : 0;
+    return log_masses_bytes(B, n, segs) + log_parts_bytes(B, n) + maxima;
 }
 
 extern "C" int pld_token_logprobs(const void *logits, int dtype, int64_t l_seq_stride,
@@ -465,20 +481,22 @@ extern "C" int pld_token_logprobs(const void *logits, int dtype, int64_t l_seq_s
     a.logprob = logprob, a.entropy = entropy;
     a.top = top, a.top_ids = top_ids, a.top_lp = top_logprobs;
     a.segs = log_segs(V);
-    const int blocks = log_blocks(B, n, a.segs);
-    a.opened = static_cast<int4 *>(workspace);
-    a.partials = reinterpret_cast<float *>(a.opened + (size_t)blocks * kLogWaves);
-    auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kLogWaves * 64), 0, (hipStream_t)stream, a);
-    };
+    char *ws = static_cast<char *>(workspace);
+    a.masses = reinterpret_cast<float4 *>(ws);
+    ws += log_masses_bytes(B, n, a.segs);
+    a.parts = reinterpret_cast<int2 *>(ws);
+    a.maxima = ws + log_parts_bytes(B, n);
+    const dim3 block(kLogWaves * 64), grid((unsigned)log_blocks(B, n, a.segs));
+    const dim3 finish((unsigned)((n + kLogWaves - 1) / kLogWaves), (unsigned)B);
+    const hipStream_t st = (hipStream_t)stream;
     auto both = [&](auto bf16) {
         constexpr int kBf16 = decltype(bf16)::value;
         if (top > 0) {
-            go(token_logprobs_kernel<kBf16, true>);
-            go(token_logprobs_join_kernel<kBf16, true>);
+            hipLaunchKernelGGL((token_logprobs_kernel<kBf16, true>), grid, block, 0, st, a);
+            hipLaunchKernelGGL((token_logprobs_finish_kernel<kBf16, true>), finish, block, 0, st, a);
         } else {
-            go(token_logprobs_kernel<kBf16, false>);
-            go(token_logprobs_join_kernel<kBf16, false>);
+            hipLaunchKernelGGL((token_logprobs_kernel<kBf16, false>), grid, block, 0, st, a);
+            hipLaunchKernelGGL((token_logprobs_finish_kernel<kBf16, false>), finish, block, 0, st, a);
         }
     };
     if (dtype == PLD_F32)
