@@ -161,7 +161,8 @@ int pld_cache_attn(const pld_cache *cache, const uint16_t *q, int64_t q_seq_stri
  *   lse         fp32 [B][n][Hq] from pld_cache_attn of the same rows
  *   attn        fp32; (b, r, j) at b*a_seq_stride + r*a_row_stride + j
  * Device-side rule: a key on a bad page or past the table gets NaN.
- * Errors: PLD_ERR_INVALID (also R outside [1, 65535], n_keys < 1), PLD_ERR_ALIGN,
+ * Errors: PLD_ERR_INVALID (also R outside [1, 65535], n_keys < 1 or
+ * past 2^31 - 65537), PLD_ERR_ALIGN,
  * PLD_ERR_LAUNCH.
  */
 int pld_cache_attn_rows(const pld_cache *cache, const uint16_t *q, int64_t q_seq_stride,

@@ -28,28 +28,6 @@ struct AttnArgs {
     int64_t as, ar, n_keys;
 };
 
-// Element t of a head's row.
-template <bool kE4m3>
-__device__ __forceinline__ float cache_get(const char *row, int t) {
-    if constexpr (kE4m3) {
-        return __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t *)row)[t], 0);
-    } else {
-        return __uint_as_float((uint32_t)((const uint16_t *)row)[t] << 16);
-    }
-}
-
-// Score of key j (on page `page`) against the query row in `q`.
-template <int D, bool kE4m3>
-__device__ __forceinline__ float score(const AttnArgs &a, const float *q, int page, int64_t j,
-                                       int kv) {
-    const char *row = a.c.k + slot_at(a.c, page, j, kv);
-    float s = 0.f;
-    for (int t = 0; t < D; ++t) s = fmaf(q[t], cache_get<kE4m3>(row, t), s);
-    s *= a.scale;
-    if (kE4m3) s *= a.c.ks[scale_at(a.c, page, j, kv)];
-    return a.cap > 0.f ? soft_cap(s, a.cap, 2.f * kLog2E / a.cap) : s;
-}
-
 // ------------------------------------------------------------ matrix tiles
 // Everything is computed transposed, with v_mfma_f32_16x16x32_bf16: the scores
 // as K Q^T, whose result gives lane (g, c) = (lane / 16, lane % 16) the scores of
@@ -179,20 +157,28 @@ __device__ __forceinline__ Range block_range(const AttnArgs &a, int R, int64_t *
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void *p) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, 0x7fffffff, 0x00027000);
 }
+template <int kAux = 0>
 __device__ __forceinline__ u32x4_t buffer_load16(__amdgpu_buffer_rsrc_t b, uint32_t off, uint32_t soff) {
-    return __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(b, off, soff, 0));
+    return __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(b, off, soff, kAux));
 }
-template <int kBytes, int W>
+// kAux of rows that one block reads once: without it the caches keep what nobody asks for
+// again (64 sequences of 8192 tokens, 8 heads of 128 in bf16: 383 us without, 347 with it).
+// Not for rows of half a 128-byte line, whose other half is the next head's and would be
+// fetched twice (32 heads of 64 in e4m3: 201 without, 225 with it), and not in the wide form,
+// whose keys other row groups read too (a 2048-token prefill: 489 without, 581 with it).
+template <int D, bool kE4m3>
+constexpr int kOnce = D * (kE4m3 ? 1 : 2) >= 128 ? 2 : 0;
+template <int kBytes, int kAux = 0, int W>
 __device__ __forceinline__ void buffer_load(uint32_t (&v)[W], __amdgpu_buffer_rsrc_t b, uint32_t off, uint32_t soff) {
     if constexpr (kBytes == 2) {
-        v[0] = __builtin_amdgcn_raw_buffer_load_b16(b, off, soff, 0);
+        v[0] = __builtin_amdgcn_raw_buffer_load_b16(b, off, soff, kAux);
     } else if constexpr (kBytes == 4) {
-        v[0] = __builtin_amdgcn_raw_buffer_load_b32(b, off, soff, 0);
+        v[0] = __builtin_amdgcn_raw_buffer_load_b32(b, off, soff, kAux);
     } else if constexpr (kBytes == 8) {
-        const auto w = __builtin_amdgcn_raw_buffer_load_b64(b, off, soff, 0);
+        const auto w = __builtin_amdgcn_raw_buffer_load_b64(b, off, soff, kAux);
         v[0] = w[0], v[1] = w[1];
     } else {
-        const auto w = __builtin_amdgcn_raw_buffer_load_b128(b, off, soff, 0);
+        const auto w = __builtin_amdgcn_raw_buffer_load_b128(b, off, soff, kAux);
         v[0] = w[0], v[1] = w[1], v[2] = w[2], v[3] = w[3];
     }
 }
@@ -228,6 +214,53 @@ __device__ __forceinline__ Tiles take_tiles(const AttnArgs &a, const Item &it, i
     if constexpr (kScales) r.scale = (int64_t)((uint64_t)page * a.spage32 + (((uint32_t)kv << a.c.shift) + ((uint32_t)j & mask)));
     r.bad = __ballot(!ok && j < it.hi);
     return r;
+}
+
+// The keys of T 16-key tiles on their way to being operands.  As an operand a lane has one
+// key's row in pieces of 16 bytes, g of each four; loaded like that, an instruction reads 64
+// bytes of each of 16 rows, and a read of a large cache reaches 5.1 TB/s where whole rows
+// side by side reach 6.3.  So rows are loaded whole, kLanes lanes each, and turned in LDS,
+// in a part of a wave's own.  Piece p of key k goes to unit 16 p + (k ^ p % 16) of its
+// tile: neither side meets a bank twice.
+template <int D, bool kE4m3, int T>
+struct KeyRows {
+    static constexpr int kLanes = D * (kE4m3 ? 1 : 2) / 16;    // lanes of a row: 4 .. 32
+    static constexpr int kRows = kWave / kLanes;               // rows of a load
+    static constexpr int kLoads = 16 * T / kRows;
+    static constexpr int kPieces = kLanes / 4;                 // operand pieces a lane
+    u32x4_t r[kLoads];
+
+    __device__ __forceinline__ static int row() { return lane_id() / kLanes; }
+    __device__ __forceinline__ static int piece() { return lane_id() % kLanes; }
+    // off: row() slot + 16 piece(); at(t): tile t's address
+    template <class At>
+    __device__ __forceinline__ void load(uint32_t off, uint32_t slot, At at) {
+        __amdgpu_buffer_rsrc_t buf;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            if (i * kRows % 16 == 0) buf = buffer_at(at(i * kRows / 16));
+            r[i] = buffer_load16<kOnce<D, kE4m3>>(buf, off, i * kRows % 16 * slot);
+        }
+    }
+    __device__ __forceinline__ static int unit(int key, int piece) { return 16 * piece + ((key ^ piece) & 15); }
+    __device__ __forceinline__ void store(u32x4_t (*lds)[kPieces * kWave]) const {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) lds[i * kRows / 16][unit(i * kRows + row(), piece())] = r[i];
+    }
+    // Piece f of this lane's key of tile t: key lane % 16, bytes 64 f + 16 (lane / 16) on.
+    __device__ __forceinline__ static u32x4_t read(const u32x4_t (*lds)[kPieces * kWave], int t, int f) {
+        return lds[t][unit(lane_id() & 15, 4 * f + (lane_id() >> 4))];
+    }
+};
+// Operand s of a head's row from its pieces: bf16 has one a piece, e4m3 two.
+template <bool kE4m3>
+__device__ __forceinline__ bf16x8_t key_operand(u32x4_t piece, int s) {
+    if constexpr (kE4m3) {
+        const uint32_t w0 = s & 1 ? piece.z : piece.x, w1 = s & 1 ? piece.w : piece.y;
+        return as_bf16x8(u32x4_t{e4m3_bf16<false>(w0), e4m3_bf16<true>(w0), e4m3_bf16<false>(w1), e4m3_bf16<true>(w1)});
+    } else {
+        return as_bf16x8(piece);
+    }
 }
 
 // Where a partial result is: blocks keep one of an item that began before their
@@ -338,9 +371,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
     constexpr int NJ = D / 16;           // output tiles
     constexpr int NV = D > 128 ? 2 : 1;  // vector loads of a V row
     constexpr int VE = D / 16 / NV;      // their elements
-    constexpr int KL = kE4m3 ? S / 2 : S;              // 16-byte loads of a key's row per lane
     constexpr int VW = VE * (kE4m3 ? 1 : 2) / 4;       // words of a V load
+    using Keys = KeyRows<D, kE4m3, 2>;
     __shared__ uint4 s_q[kMT][S][64];
+    __shared__ u32x4_t s_keys[4][2][Keys::kPieces * 64];
     __shared__ float s_ml[2][4][R];
     __shared__ float s_o[4][kMT][NJ][64];
     __shared__ int64_t s_w[8];
@@ -404,23 +438,20 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
 
         const int ubase = it.lo / kUnit;
         const int kbase = (ubase + u0) * kUnit + 32 * wave, kend = (ubase + u1) * kUnit;
-        u32x4_t kr[2][KL];
+        Keys kr;
         uint32_t vr[8][NV][VW];
         f32x4_t kf[2], vf[2];
         uint32_t bad = 0;   // the chunk's keys on bad pages
 
         const char *kh = a.c.k + (int64_t)kv * a.c.head, *vh = a.c.v + (int64_t)kv * a.c.head;
         const uint32_t slot = (uint32_t)a.c.slot;
-        const uint32_t k_off = (uint32_t)c * slot + 16 * g, v_off = 4 * (uint32_t)g * slot + c * (4 * VW);
+        const uint32_t k_off = (uint32_t)Keys::row() * slot + 16 * Keys::piece(), v_off = 4 * (uint32_t)g * slot + c * (4 * VW);
         auto load_k = [&](const Tiles &tl) {
+            kr.load(k_off, slot, [&](int t) { return kh + tl.row(t); });
+            if constexpr (kE4m3)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const auto buf = buffer_at(kh + tl.row(t));
-#pragma unroll
-                for (int s = 0; s < KL; ++s) kr[t][s] = buffer_load16(buf, k_off + 64 * s, 0);
-                if constexpr (kE4m3)
+                for (int t = 0; t < 2; ++t)
                     kf[t] = __builtin_bit_cast(f32x4_t, buffer_load16(buffer_at(a.c.ks + tl.first_scale(t)), 16 * g, 0));
-            }
         };
         auto load_v = [&](const Tiles &tl) {
 #pragma unroll
@@ -430,7 +461,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int v = 0; v < NV; ++v)
-                        buffer_load<4 * VW>(vr[4 * t + i][v], buf, v_off + v * (64 * VW), i * slot);
+                        buffer_load<4 * VW, kOnce<D, kE4m3>>(vr[4 * t + i][v], buf, v_off + v * (64 * VW), i * slot);
                 if constexpr (kE4m3)
                     vf[t] = __builtin_bit_cast(f32x4_t, buffer_load16(buffer_at(a.c.vs + tl.first_scale(t)), 16 * g, 0));
             }
@@ -451,6 +482,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
             }
             const bool plain = k0 >= all_lo && k0 + 32 <= all_hi && bad == 0;   // every row sees every key
 
+            kr.store(s_keys[wave]);
+            f32x4_t ks[2];
+            if constexpr (kE4m3) ks[0] = kf[0] * c1, ks[1] = kf[1] * c1;
+            asm volatile("" ::: "memory");
+            if (more) load_k(tl);
             f32x4_t x[kMT][2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
@@ -458,22 +494,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
                 for (int n = 0; n < kMT; ++n) x[n][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int s = 0; s < S; ++s) {
-                    bf16x8_t k;
-                    if constexpr (kE4m3) {
-                        const uint32_t w0 = s & 1 ? kr[t][s / 2].z : kr[t][s / 2].x;
-                        const uint32_t w1 = s & 1 ? kr[t][s / 2].w : kr[t][s / 2].y;
-                        k = as_bf16x8(make_uint4(e4m3_bf16<false>(w0), e4m3_bf16<true>(w0),
-                                                 e4m3_bf16<false>(w1), e4m3_bf16<true>(w1)));
-                    } else {
-                        k = as_bf16x8(kr[t][s]);
-                    }
+                    const bf16x8_t k = key_operand<kE4m3>(Keys::read(s_keys[wave], t, kE4m3 ? s / 2 : s), s);
 #pragma unroll
                     for (int n = 0; n < kMT; ++n) x[n][t] = mfma(k, as_bf16x8(s_q[n][s][lane]), x[n][t]);
                 }
             }
-            f32x4_t ks[2];
-            if constexpr (kE4m3) ks[0] = kf[0] * c1, ks[1] = kf[1] * c1;
-            if (more) load_k(tl);
 
 #pragma unroll
             for (int n = 0; n < kMT; ++n) {
@@ -981,34 +1006,216 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(AttnArgs a, int R)
     if (a.lse && lane == 0) a.lse[lat] = gone ? inv : (mg + __log2f(lg)) * kLn2;
 }
 
-// One thread per key and chosen head.
+// ------------------------------------------------ chosen heads at one row
+// The keys of a sequence once per key head that has chosen query heads, as the first
+// operand, against up to 16 of those as the second: with the log sums known a weight is
+// final at once, and a lane stores its four keys of a row together.  The units of all
+// (sequence, used key head) pairs are dealt to the blocks as in the attention; a block's
+// four waves have 32 of a unit's keys each.
+constexpr int kRowsBlocks = 1024;   // four per CU
+
 template <int D, bool kE4m3>
-__global__ __launch_bounds__(256) void cache_attn_rows_kernel(AttnArgs a) {
-    const int r = blockIdx.y, b = blockIdx.z, T = a.r.lens[b], i = a.row[b];
-    if (T < 1 || i < 0 || i >= a.r.n) return;
-    const int64_t pos = (int64_t)T - 1 + i, end = min(pos + 1, a.n_keys);
-    const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (j - threadIdx.x >= end) return;
-    __shared__ float q[D];
-    const int h = a.heads[r];
-    const bool known = h >= 0 && h < a.Hq;
-    if (known) {
-        const uint16_t *qp = a.q + (int64_t)b * a.qs + (int64_t)i * a.qr + (int64_t)h * D;
-        for (int t = threadIdx.x; t < D; t += 256) q[t] = __uint_as_float((uint32_t)qp[t] << 16);
+__global__ __launch_bounds__(256, D == 256 ? 2 : 3) void cache_attn_rows_kernel(AttnArgs a) {
+    constexpr int S = D / 32;
+    using Keys = KeyRows<D, kE4m3, 2>;
+    __shared__ u32x4_t s_keys[4][2][Keys::kPieces * 64];
+    constexpr int kHeadList = 512;   // chosen heads that are kept in LDS
+    __shared__ int s_used[1024], s_heads[kHeadList], s_list[256], s_cnt[4];
+    __shared__ int64_t s_w[5];
+    __shared__ int s_b;
+    const int lane = lane_id(), wave = uniform((int)threadIdx.x / 64), tid = threadIdx.x;
+    const int g = lane >> 4, c = lane & 15;
+
+    // A sequence's keys to write, and its units.
+    auto keys_of = [&](int b) {
+        const int T = a.r.lens[b], i = a.row[b];
+        return T >= 1 && i >= 0 && i < a.r.n ? min((int64_t)T + i, a.n_keys) : 0;
+    };
+    auto units_of = [&](int b) { return (keys_of(b) + kUnit - 1) / kUnit; };
+    const int per = (a.r.B + 255) / 256, b0 = min(tid * per, a.r.B), b1 = min(b0 + per, a.r.B);
+    int64_t mine = 0;
+    const int head0 = tid < a.R ? a.heads[tid] : -1;   // (asked for together with the lengths)
+    for (int b = b0; b < b1; ++b) mine += units_of(b);
+
+    // The key heads that are used, in order, and a place after them for chosen heads that do
+    // not exist: their rows are NaN.
+    for (int h = tid; h < a.c.heads; h += 256) s_used[h] = 0;
+    __syncthreads();
+    bool unknown = false;
+    for (int r = tid; r < a.R; r += 256) {
+        const int h = r == tid ? head0 : a.heads[r];
+        if (r < kHeadList) s_heads[r] = h;
+        if (h >= 0 && h < a.Hq)
+            s_used[h / a.G] = 1;
+        else
+            unknown = true;
+    }
+    unknown = __syncthreads_or(unknown);
+    if (wave == 0) {
+        int n = 0;
+        for (int h0 = 0; h0 < a.c.heads; h0 += 64) {
+            const bool in = h0 + lane < a.c.heads && s_used[h0 + lane];
+            const uint64_t m = __ballot(in);
+            asm volatile("" ::: "memory");
+            if (in) s_used[n + __popcll(m & lanemask_lt())] = h0 + lane;   // (never past h0)
+            n += __popcll(m);
+        }
+        if (lane == 0) s_cnt[0] = n;
+    }
+    // the waves' sums go through LDS at the same barrier
+    int64_t before = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const int64_t x = __shfl_up(before, o);
+        if (lane >= o) before += x;
+    }
+    if (lane == 63) s_w[wave] = before;
+    __syncthreads();
+    const int used = uniform(s_cnt[0]), heads = used + unknown;
+
+    int64_t total = 0;
+    before -= mine;
+    for (int w = 0; w < 4; ++w) {
+        if (w < wave) before += s_w[w];
+        total += s_w[w];
+    }
+    total = uniform(total) * heads;
+    before *= heads;
+    mine *= heads;
+    int64_t x = total * blockIdx.x / gridDim.x;
+    const int64_t x1 = total * (blockIdx.x + 1) / gridDim.x;
+    if (x >= x1) return;
+    if (before <= x && x < before + mine) {
+        int b = b0;
+        for (int64_t u; x >= before + (u = units_of(b) * heads); ++b) before += u;
+        s_b = b;
+        s_w[4] = before;
     }
     __syncthreads();
-    if (j >= end) return;
-    float w = __uint_as_float(0x7fc00000u);
-    if (known) {
-        const int page = page_of(a.c, b, j);
-        if (a.window && j <= pos - a.window)
-            w = 0.f;
-        else if (page >= 0)
-            w = __builtin_amdgcn_exp2f((score<D, kE4m3>(a, q, page, j, h / (a.Hq / a.c.heads)) -
-                                        a.lse[((int64_t)b * a.r.n + i) * a.Hq + h]) *
-                                       kLog2E);
+    int b = uniform(s_b);
+    int64_t first = uniform(s_w[4]);
+
+    const float c1 = a.scale * kLog2E, nan = __uint_as_float(0x7fc00000u);
+    const int64_t cap = (int64_t)a.c.max_pages << a.c.shift;
+    while (x < x1) {
+        const int64_t units = uniform(units_of(b)), span = units * heads;
+        if (x >= first + span) {
+            first += span;
+            ++b;
+            continue;
+        }
+        const int ki = (int)((x - first) / units);
+        const int u0 = (int)((x - first) - ki * units), u1 = (int)min(units, u0 + (x1 - x));
+        x += u1 - u0;
+        const int kv = ki < used ? uniform(s_used[ki]) : -1;
+        const int row = uniform(a.row[b]);
+        const int64_t pos = (int64_t)uniform(a.r.lens[b]) - 1 + row;
+        const int end = (int)min(keys_of(b), (int64_t)u1 * kUnit);      // of what is written here
+        const int lo = a.window && pos + 1 > a.window ? (int)min(pos + 1 - a.window, (int64_t)1 << 30) : 0;
+        Item it;
+        it.b = b;
+        it.hi = (int)min(min(pos + 1, a.n_keys), cap);
+
+        for (int r0 = 0; r0 < a.R; r0 += 256) {
+            // the rows r of this key head among 256, in order
+            const int h = r0 + tid >= a.R ? 0 : r0 + tid < kHeadList ? s_heads[r0 + tid] : a.heads[r0 + tid];
+            const bool known = h >= 0 && h < a.Hq;
+            const bool in = r0 + tid < a.R && (known ? h / a.G == kv : kv < 0);
+            const uint64_t m = __ballot(in);
+            __syncthreads();
+            if (lane == 0) s_cnt[wave] = __popcll(m);
+            __syncthreads();
+            int to = __popcll(m & lanemask_lt()), cnt = 0;
+            for (int w = 0; w < 4; ++w) {
+                if (w < wave) to += s_cnt[w];
+                cnt += s_cnt[w];
+            }
+            cnt = uniform(cnt);
+            if (in) s_list[to] = r0 + tid;
+            __syncthreads();
+
+            for (int t0 = 0; t0 < cnt; t0 += 16) {
+                const bool own = t0 + c < cnt;
+                const int r = s_list[min(t0 + c, cnt - 1)];
+                const int head = kv < 0 ? 0 : r < kHeadList ? s_heads[r] : a.heads[r];
+                const uint16_t *qp = a.q + (int64_t)b * a.qs + (int64_t)row * a.qr + (int64_t)head * D;
+                bf16x8_t q[S];
+#pragma unroll
+                for (int s = 0; s < S; ++s) {
+                    const int d = kE4m3 ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
+                    q[s] = as_bf16x8(*reinterpret_cast<const u32x4_t *>(qp + d));
+                }
+                const float lse2 = a.lse[((int64_t)b * a.r.n + row) * a.Hq + head] * kLog2E;
+                float *dst = a.attn + (int64_t)b * a.as + (int64_t)r * a.ar;
+                const bool vec = ((uintptr_t)dst & 15) == 0;
+
+                const char *kh = a.c.k + (int64_t)max(kv, 0) * a.c.head;
+                const uint32_t slot = (uint32_t)a.c.slot, k_off = (uint32_t)Keys::row() * slot + 16 * Keys::piece();
+                Keys kr;
+                f32x4_t kf[2];
+                auto load_k = [&](const Tiles &tl) {
+                    kr.load(k_off, slot, [&](int t) { return kh + tl.row(t); });
+                    if constexpr (kE4m3)
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+                            kf[t] = __builtin_bit_cast(f32x4_t, buffer_load16(buffer_at(a.c.ks + tl.first_scale(t)), 16 * g, 0));
+                };
+                const int kbase = u0 * kUnit + 32 * wave;
+                int entry = load_entry<2>(a, it, kbase);
+                Tiles tl = take_tiles<2, kE4m3>(a, it, kbase, entry, max(kv, 0));
+                entry = load_entry<2>(a, it, kbase + kUnit);
+                // (keys before the window are written, not read)
+                if (kbase < end && kbase + 32 > lo) load_k(tl);
+                for (int k0 = kbase; k0 < end; k0 += kUnit) {
+                    const uint32_t bad = (uint32_t)tl.bad;
+                    kr.store(s_keys[wave]);
+                    f32x4_t w[2], ks[2];
+                    if constexpr (kE4m3) ks[0] = kf[0] * c1, ks[1] = kf[1] * c1;
+                    asm volatile("" ::: "memory");
+                    if (k0 + kUnit < end) {
+                        tl = take_tiles<2, kE4m3>(a, it, k0 + kUnit, entry, max(kv, 0));
+                        entry = load_entry<2>(a, it, k0 + 2 * kUnit);
+                        if (k0 + kUnit + 32 > lo) load_k(tl);
+                    }
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        w[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int s = 0; s < S; ++s)
+                            w[t] = mfma(key_operand<kE4m3>(Keys::read(s_keys[wave], t, kE4m3 ? s / 2 : s), s), q[s], w[t]);
+                    }
+                    const float sc = scale_scores<kE4m3>(a, w, c1, ks[0], ks[1]);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[t][e] = __builtin_amdgcn_exp2f(fmaf(w[t][e], sc, -lse2));
+                    if (bad || kv < 0 || k0 < lo || k0 + 32 > it.hi) {
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int j = k0 + 16 * t + 4 * g + e;
+                                if ((bad >> (16 * t + 4 * g + e)) & 1 || j >= cap) w[t][e] = nan;
+                                if (j < lo) w[t][e] = 0.f;
+                                if (kv < 0) w[t][e] = nan;
+                            }
+                    }
+                    if (!own) continue;
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        const int j = k0 + 16 * t + 4 * g;
+                        if (vec && j + 4 <= end) {
+                            *reinterpret_cast<f32x4_t *>(dst + j) = w[t];
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (j + e < end) dst[j + e] = w[t][e];
+                        }
+                    }
+                }
+            }
+        }
     }
-    a.attn[(int64_t)b * a.as + (int64_t)r * a.ar + j] = w;
 }
 
 // Tiles of 16 rows per item, and row groups per sequence, from a key head's rows.
@@ -1131,7 +1338,8 @@ extern "C" int pld_cache_attn_rows(const pld_cache *cache, const uint16_t *q,
     int rc = prep_attn(cache, false, q, q_seq_stride, q_row_stride, lens, nullptr, B, n, Hq, scale,
                        softcap, window, a);
     if (rc != PLD_OK) return rc;
-    if (!row || !heads || !lse || !attn || R < 1 || R > 65535 || n_keys < 1)
+    if (!row || !heads || !lse || !attn || R < 1 || R > 65535 || n_keys < 1 ||
+        n_keys > INT32_MAX - 65536)
         return PLD_ERR_INVALID;
     if ((B > 1 && a_seq_stride < n_keys) || (R > 1 && a_row_stride < n_keys))
         return PLD_ERR_INVALID;
@@ -1139,10 +1347,8 @@ extern "C" int pld_cache_attn_rows(const pld_cache *cache, const uint16_t *q,
     a.row = row, a.heads = heads, a.R = R;
     a.lse = const_cast<float *>(lse);
     a.attn = attn, a.as = a_seq_stride, a.ar = a_row_stride, a.n_keys = n_keys;
-    // positions past the table have no page: more keys than it holds (and a page's
-    // worth, for rows past its end) are of no use
-    const int64_t keys = n_keys < kMaxTokStride ? n_keys : kMaxTokStride;
-    const dim3 grid((unsigned)((keys + 255) / 256), (unsigned)R, (unsigned)B);
+    const int64_t most = (n_keys / kUnit + 1) * B * (cache->heads + 1);   // units
+    const dim3 grid((unsigned)(most < kRowsBlocks ? most : kRowsBlocks));
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, a);
     };
