@@ -581,39 +581,35 @@ def pld_verify_accept(draft, draft_len, accept_len, out_tokens, out_count, works
 
 
 # ------------------------------------------------- the verification pass's model side
-def _on_one_device(stream, **tensors):
+def _on_one_device(stream, *tensors):
     """The calls of include/pld_model.h take many tensors at once: all of them on one
     device, which is the current one (the kernels run there)."""
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise TypeError("tensors on several devices: " + ", ".join(
+                str(t.device) for t in tensors if t is not None))
+    if dev < 0:
+        raise TypeError("expected device tensors")
     torch = _torch or _th()
-    dev = None
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise TypeError(f"{name}: expected a device tensor, got one on {t.device}")
-        if dev is None:
-            dev = t.get_device()
-        elif t.get_device() != dev:
-            raise TypeError(f"{name} is on cuda:{t.get_device()}, the other tensors on cuda:{dev}")
-    if dev != torch.cuda.current_device():
-        raise TypeError(f"the tensors are on cuda:{dev}, the current device is "
-                        f"cuda:{torch.cuda.current_device()}")
-    sd = getattr(stream, "device_index", dev)
-    if sd != dev:
-        raise TypeError(f"the stream is on cuda:{sd}, the tensors on cuda:{dev}")
+    # (torch.cuda.current_device(), without its check that CUDA is initialised)
+    if dev != (getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device)():
+        raise TypeError(f"the tensors are on cuda:{dev}, which is not the current device")
+    if getattr(stream, "device_index", dev) != dev:
+        raise TypeError(f"the stream is on cuda:{stream.device_index}, the tensors on cuda:{dev}")
 
 
 def _ints(t, name, *shape):
     """A contiguous int32 tensor of `shape` (None: absent)."""
     torch = _torch or _th()
-    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != shape
+    if t is not None and (t.dtype != torch.int32 or t.shape != shape
                           or not t.is_contiguous()):
         raise TypeError(f"{name} must be a contiguous int32 tensor of shape {shape}")
 
 
 def _floats(t, name, *shape):
     torch = _torch or _th()
-    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != shape
+    if t is not None and (t.dtype != torch.float32 or t.shape != shape
                           or not t.is_contiguous()):
         raise TypeError(f"{name} must be a contiguous float32 tensor of shape {shape}")
 
@@ -621,7 +617,7 @@ def _floats(t, name, *shape):
 def _rows_of(t, name, B, n, heads, D):
     """Strides (sequence, row) of a bf16 [B][n][heads][D] tensor whose heads follow each other."""
     torch = _torch or _th()
-    if t.dtype != torch.bfloat16 or tuple(t.shape) != (B, n, heads, D):
+    if t.dtype != torch.bfloat16 or t.shape != (B, n, heads, D):
         raise TypeError(f"{name}: expected bfloat16 {(B, n, heads, D)}, got {t.dtype} "
                         f"{tuple(t.shape)}")
     st = t.stride()
@@ -642,26 +638,30 @@ def _cache_of(k_cache, v_cache, table, k_scale, v_scale, B):
     if v_cache is not None and (v_cache.dtype != k_cache.dtype or v_cache.shape != k_cache.shape
                                 or v_cache.stride() != ks):
         raise TypeError("v_cache must have k_cache's type, shape and strides")
-    _need(table, torch.int32, "table", 2)
-    if table.shape[0] != B:
+    ts = _need(table, torch.int32, "table", 2)
+    rows, per = table.shape
+    if rows != B:
         raise TypeError(f"table must be [B = {B}][pages], got {tuple(table.shape)}")
     q8 = k_cache.dtype == torch.float8_e4m3fn
     sp = 0
-    for t, name, used in ((k_scale, "k_scale", True), (v_scale, "v_scale", v_cache is not None)):
-        if not q8:
-            if t is not None:
-                raise TypeError(f"{name}: a bfloat16 cache has no scales")
-        elif used or t is not None:
-            if t is None or t.dtype != torch.float32 or tuple(t.shape) != (P, heads, page):
+    if not q8:
+        if k_scale is not None or v_scale is not None:
+            raise TypeError("a bfloat16 cache has no scales")
+    else:
+        for t, name, used in ((k_scale, "k_scale", True), (v_scale, "v_scale", v_cache is not None)):
+            if not used and t is None:
+                continue
+            if t is None or t.dtype != torch.float32 or t.shape != (P, heads, page):
                 raise TypeError(f"{name} must be a float32 [pages][heads][slots] tensor")
-            if t.stride(2) != 1 or (heads > 1 and t.stride(1) != page):
+            st = t.stride()
+            if st[2] != 1 or (heads > 1 and st[1] != page):
                 raise TypeError(f"{name}: a page's scales must follow each other")
-            if sp and t.stride(0) != sp:
+            if sp and st[0] != sp:
                 raise TypeError("k_scale and v_scale must have the same strides")
-            sp = t.stride(0)
+            sp = st[0]
     return _Cache(_ptr(k_cache), _ptr(v_cache), PLD_E4M3 if q8 else PLD_BF16, _ptr(k_scale),
-                  _ptr(v_scale), sp, ks[0], ks[1], ks[2], _ptr(table), table.stride(0), P, page,
-                  table.shape[1], heads, D)
+                  _ptr(v_scale), sp, ks[0], ks[1], ks[2], _ptr(table), ts[0], P, page,
+                  per, heads, D)
 
 
 def pld_model_version():
@@ -685,9 +685,8 @@ def pld_cache_write(q, k, v, k_cache, v_cache, table, lens, q_out, draft_len=Non
     table[b][position / slots] of k_cache / v_cache [pages][slots][heads][D] (bfloat16, or
     float8_e4m3fn with scales fp32 [pages][heads][slots]), queries written to q_out."""
     torch = _torch or _th()
-    _on_one_device(stream, q=q, k=k, v=v, k_cache=k_cache, v_cache=v_cache, table=table, lens=lens,
-                   q_out=q_out, draft_len=draft_len, k_scale=k_scale, v_scale=v_scale,
-                   q_norm=q_norm, k_norm=k_norm, rope=rope)
+    _on_one_device(stream, q, k, v, k_cache, v_cache, table, lens, q_out, draft_len, k_scale,
+                   v_scale, q_norm, k_norm, rope)
     if q.dim() != 4:
         raise TypeError("q must be [B][n][Hq][D]")
     B, n, Hq, D = q.shape
@@ -699,7 +698,7 @@ def pld_cache_write(q, k, v, k_cache, v_cache, table, lens, q_out, draft_len=Non
     _ints(lens, "lens", B)
     _ints(draft_len, "draft_len", B)
     for t, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
-        if t is not None and (t.dtype != torch.bfloat16 or tuple(t.shape) != (D,)
+        if t is not None and (t.dtype != torch.bfloat16 or t.shape != (D,)
                               or not t.is_contiguous()):
             raise TypeError(f"{name} must be a contiguous bfloat16 tensor of {D} elements")
     rs = (0, 0) if rope is None else _need(rope, torch.float32, "rope", 2)
@@ -718,9 +717,8 @@ def pld_cache_attn(q, k_cache, v_cache, table, lens, out, workspace, draft_len=N
     """Attention of the rows q bf16 [B][n][Hq][D] (positions lens[b]-1+i, i <= draft_len[b])
     over the cache: out like q, lse fp32 [B][n][Hq]; scale defaults to 1 / sqrt(D), softcap
     and window are off at 0."""
-    _on_one_device(stream, q=q, k_cache=k_cache, v_cache=v_cache, table=table, lens=lens, out=out,
-                   workspace=workspace, draft_len=draft_len, k_scale=k_scale, v_scale=v_scale,
-                   lse=lse)
+    _on_one_device(stream, q, k_cache, v_cache, table, lens, out, workspace, draft_len, k_scale,
+                   v_scale, lse)
     if q.dim() != 4:
         raise TypeError("q must be [B][n][Hq][D]")
     B, n, Hq, D = q.shape
@@ -742,8 +740,7 @@ def pld_cache_attn_rows(q, k_cache, table, lens, row, heads, lse, attn, k_scale=
     """The attention weights of query heads `heads` (int32 [R]) at row row[b] of each sequence,
     from the q and lse of pld_cache_attn: attn fp32 [B][R][n_keys], as pld_rank_attn takes it."""
     torch = _torch or _th()
-    _on_one_device(stream, q=q, k_cache=k_cache, table=table, lens=lens, row=row, heads=heads,
-                   lse=lse, attn=attn, k_scale=k_scale)
+    _on_one_device(stream, q, k_cache, table, lens, row, heads, lse, attn, k_scale)
     if q.dim() != 4:
         raise TypeError("q must be [B][n][Hq][D]")
     B, n, Hq, D = q.shape
@@ -757,7 +754,7 @@ def pld_cache_attn_rows(q, k_cache, table, lens, row, heads, lse, attn, k_scale=
     _ints(heads, "heads", R)
     _floats(lse, "lse", B, n, Hq)
     as_ = _need(attn, torch.float32, "attn", 3)
-    if tuple(attn.shape[:2]) != (B, R):
+    if attn.shape[0] != B or attn.shape[1] != R:
         raise TypeError(f"attn must be [B = {B}][R = {R}][n_keys], got {tuple(attn.shape)}")
     return _run("pld_cache_attn_rows", (
         cache, _ptr(q), qs[0], qs[1], _ptr(lens), _ptr(row), _ptr(heads), R, _ptr(lse), B, n, Hq,
@@ -770,8 +767,8 @@ def pld_token_logprobs(logits, tokens, logprob, workspace, count=None, temperatu
     """Log probabilities of tokens [B][n] under softmax(logits / temperature), rows i < count[b],
     with the rows' entropy and their most likely tokens (top_ids, top_logprobs [B][n][top])."""
     torch = _torch or _th()
-    _on_one_device(stream, logits=logits, tokens=tokens, logprob=logprob, workspace=workspace,
-                   count=count, entropy=entropy, top_ids=top_ids, top_logprobs=top_logprobs)
+    _on_one_device(stream, logits, tokens, logprob, workspace, count, entropy, top_ids,
+                   top_logprobs)
     if logits.dtype not in (torch.float32, torch.bfloat16):
         raise TypeError("logits must be float32 or bfloat16")
     ls = _need(logits, logits.dtype, "logits", 3)
