@@ -20,7 +20,7 @@ struct AttnArgs {
     int64_t os, orow;
     float *lse;
     float *partials;
-    int4 *opened;                   // [blocks]: (entry, key head, last block) of an item that spans blocks
+    struct Opened *opened;          // [blocks]
     // the chosen heads' weights
     const int32_t *row, *heads;
     int R;
@@ -85,10 +85,11 @@ struct Item {
     int units;                    // 0: no rows
 };
 
-__device__ __forceinline__ Item item_of(const AttnArgs &a, int e, int R) {
+__device__ __forceinline__ Item make_item(const AttnArgs &a, int e, int R, int cnt, int pos0) {
     Item it;
     it.b = e / a.groups;
-    it.cnt = row_count(a.r, it.b, it.pos0);
+    it.cnt = cnt;
+    it.pos0 = pos0;
     it.r0 = (e - it.b * a.groups) * R;
     it.rows = min(it.cnt * a.G - it.r0, R);
     it.units = 0;
@@ -103,14 +104,33 @@ __device__ __forceinline__ Item item_of(const AttnArgs &a, int e, int R) {
     return it;
 }
 
+__device__ __forceinline__ Item item_of(const AttnArgs &a, int e, int R) {
+    int pos0;
+    const int cnt = row_count(a.r, e / a.groups, pos0);
+    return make_item(a, e, R, cnt, pos0);
+}
+
+// An item that begins in a block's range and ends in a later one.
+struct Opened {
+    int e, kv, last, pos0;   // entry (-1: none), key head, last block, of the sequence
+    int rows, b, r0, pad;    // as in Item
+};
+constexpr Opened kNothing = {-1, 0, 0, 0, 0, 0, 0, 0};
+
 // The part of all units that is this block's, by each block from the lengths: there are
 // as many ranges as blocks, or as units where those are fewer, so that none between
 // two others is empty.
 struct Range {
-    int64_t x0, x1;          // [x0, x1) of `total`
-    int64_t total, ranges;
+    int64_t x0, x1;          // [x0, x1) of all units
+    int64_t per;             // units of a range; the first `longer` ranges have one more
+    int longer;
     int e;                   // the entry (sequence and row group) of unit x0
+    Item it;                 // that entry's
     int64_t first;           // its first unit
+    __device__ __forceinline__ int block_of(int64_t x) const {
+        const int64_t of_longer = (per + 1) * longer;
+        return (int)(x < of_longer ? quotient(x, per + 1) : longer + quotient(x - of_longer, per));
+    }
 };
 __device__ __forceinline__ Range block_range(const AttnArgs &a, int R, int64_t *s_w, int *s_e) {
     const int lane = lane_id(), wave = uniform((int)threadIdx.x / 64);
@@ -128,26 +148,32 @@ __device__ __forceinline__ Range block_range(const AttnArgs &a, int R, int64_t *
     if (lane == 63) s_w[wave] = before;
     __syncthreads();
     Range r;
-    r.total = 0;
+    int64_t total = 0;
     before -= mine;
     for (int w = 0; w < 4; ++w) {
         if (w < wave) before += s_w[w];
-        r.total += s_w[w];
+        total += s_w[w];
     }
-    r.total = uniform(r.total);
-    r.ranges = min(r.total, (int64_t)gridDim.x);
-    const int64_t block = min((int64_t)blockIdx.x, r.ranges);
-    r.x0 = r.ranges ? r.total * block / r.ranges : 0;
-    r.x1 = block < r.ranges ? r.total * (block + 1) / r.ranges : r.x0;
+    total = uniform(total);
+    const int64_t ranges = min(total, (int64_t)gridDim.x), block = blockIdx.x;
+    r.per = ranges ? quotient(total, ranges) : 0;
+    r.longer = (int)(total - r.per * ranges);
+    r.x0 = block < ranges ? r.per * block + min(block, (int64_t)r.longer) : total;
+    r.x1 = block < ranges ? r.x0 + r.per + (block < r.longer) : total;
     if (before <= r.x0 && r.x0 < before + mine) {
         // the thread whose entries hold x0 steps to the one that does
         int e = e0;
-        for (int64_t u; r.x0 >= before + (u = (int64_t)item_of(a, e, R).units * a.c.heads); ++e) before += u;
-        *s_e = e;
+        Item it = item_of(a, e, R);
+        for (int64_t u; r.x0 >= before + (u = (int64_t)it.units * a.c.heads); it = item_of(a, ++e, R)) before += u;
+        s_e[0] = e;
+        s_e[1] = it.cnt;
+        s_e[2] = it.pos0;
         s_w[4] = before;
     }
     __syncthreads();
-    r.e = uniform(*s_e);
+    if (r.x0 >= r.x1) return r;
+    r.e = uniform(s_e[0]);
+    r.it = make_item(a, r.e, R, uniform(s_e[1]), uniform(s_e[2]));
     r.first = uniform(s_w[4]);
     return r;
 }
@@ -378,66 +404,52 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
     __shared__ float s_ml[2][4][R];
     __shared__ float s_o[4][kMT][NJ][64];
     __shared__ int64_t s_w[8];
-    __shared__ int s_e;
+    __shared__ int s_e[3];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
     const int g = lane >> 4, c = lane & 15;
 
-    const Range rg = block_range(a, R, s_w, &s_e);
+    const Range rg = block_range(a, R, s_w, s_e);
     int e = rg.e;
+    Item it = rg.it;
     int64_t x = rg.x0, first = rg.first;    // first unit of entry e
-    int4 opened = make_int4(-1, 0, 0, 0);   // the item that begins here and ends in a later block
+    Opened opened = kNothing;
     const float c1 = a.scale * kLog2E;
     while (x < rg.x1) {
-        const Item it = item_of(a, e, R);
         const int64_t span = (int64_t)it.units * a.c.heads;
         if (x >= first + span) {
             first += span;
-            ++e;
+            it = item_of(a, ++e, R);
             continue;
         }
-        const int kv = (int)((x - first) / it.units);
+        const int kv = (int)quotient(x - first, it.units);
         const int u0 = (int)((x - first) - (int64_t)kv * it.units);
         const int u1 = (int)min((int64_t)it.units, u0 + (rg.x1 - x));
         x += u1 - u0;
 
+        const int ubase = it.lo / kUnit;
+        const int kbase = (ubase + u0) * kUnit + 32 * wave, kend = (ubase + u1) * kUnit;
+        int entry = load_entry<2>(a, it, kbase);
+
         // The rows' queries, as operands in LDS (in registers they would cost a wave the
-        // room for its loads), and the keys that each lane's queries see.
-        int see_lo[kMT], see_hi[kMT];
-        __syncthreads();
+        // room for its loads): asked for here, put there once the first keys are asked for.
+        constexpr int kQ = (kMT * S + 3) / 4;   // a wave's pieces
+        u32x4_t qv[kQ];
 #pragma unroll
-        for (int t = 0; t < kMT; ++t) {
+        for (int u = 0; u < kQ; ++u) {
+            const int piece = min(4 * u + wave, kMT * S - 1), t = piece / S, s = piece % S;
             const int m = min(16 * t + c, it.rows - 1);
             const int i = (it.r0 + m) / a.G, h = kv * a.G + (it.r0 + m) % a.G;
             const uint16_t *qp =
                 a.q + (int64_t)it.b * a.qs + (int64_t)i * a.qr + (int64_t)h * D;
-#pragma unroll
-            for (int s = 0; s < S; ++s) {
-                const int d = kE4m3 ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
-                if ((t * S + s) % 4 == wave) s_q[t][s][lane] = *reinterpret_cast<const uint4 *>(qp + d);
-            }
-            const int64_t p = (int64_t)it.pos0 + i;
-            see_hi[t] = (int)min(p + 1, (int64_t)it.hi);
-            see_lo[t] = a.window && p + 1 > a.window ? (int)min(p + 1 - a.window, (int64_t)1 << 30) : 0;
+            const int d = kE4m3 ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
+            qv[u] = *reinterpret_cast<const u32x4_t *>(qp + d);
         }
-        __syncthreads();
         // keys that every row sees: [all_lo, all_hi)
         const int64_t pf = (int64_t)it.pos0 + it.r0 / a.G;
         const int64_t pl = (int64_t)it.pos0 + (it.r0 + it.rows - 1) / a.G;
         const int all_hi = (int)min(pf + 1, (int64_t)it.hi);
         const int all_lo = a.window && pl + 1 > a.window ? (int)min(pl + 1 - a.window, (int64_t)1 << 30) : 0;
 
-        f32x4_t o[kMT][NJ];
-        float m[kMT], l[kMT];   // log2 units; l: of this lane's keys
-#pragma unroll
-        for (int t = 0; t < kMT; ++t) {
-            m[t] = kNoMax;
-            l[t] = 0.f;
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) o[t][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        }
-
-        const int ubase = it.lo / kUnit;
-        const int kbase = (ubase + u0) * kUnit + 32 * wave, kend = (ubase + u1) * kUnit;
         Keys kr;
         uint32_t vr[8][NV][VW];
         f32x4_t kf[2], vf[2];
@@ -467,11 +479,34 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
             }
         };
 
-        int entry = load_entry<2>(a, it, kbase);
         Tiles tl = take_tiles<2, kE4m3>(a, it, kbase, entry, kv);
         entry = load_entry<2>(a, it, kbase + kUnit);   // ahead of the loads that go by it
         load_k(tl);
         load_v(tl);
+        int see_lo[kMT], see_hi[kMT];   // the keys that each lane's queries see
+#pragma unroll
+        for (int t = 0; t < kMT; ++t) {
+            const int64_t p = (int64_t)it.pos0 + (it.r0 + min(16 * t + c, it.rows - 1)) / a.G;
+            see_hi[t] = (int)min(p + 1, (int64_t)it.hi);
+            see_lo[t] = a.window && p + 1 > a.window ? (int)min(p + 1 - a.window, (int64_t)1 << 30) : 0;
+        }
+        f32x4_t o[kMT][NJ];
+        float m[kMT], l[kMT];   // log2 units; l: of this lane's keys
+#pragma unroll
+        for (int t = 0; t < kMT; ++t) {
+            m[t] = kNoMax;
+            l[t] = 0.f;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) o[t][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+
+        __syncthreads();   // the item before is done with LDS
+#pragma unroll
+        for (int u = 0; u < kQ; ++u) {
+            const int piece = min(4 * u + wave, kMT * S - 1);   // (a last piece twice is the same)
+            s_q[piece / S][piece % S][lane] = __builtin_bit_cast(uint4, qv[u]);
+        }
+        __syncthreads();
         for (int k0 = kbase; k0 < kend; k0 += kUnit) {
             asm volatile("" ::: "memory");   // the queries are read from LDS anew
             const bool more = k0 + kUnit < kend;
@@ -659,7 +694,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
         }
         if (u0 == 0 && !whole) {
             const int64_t end = first + (int64_t)(kv + 1) * it.units;   // of the item
-            opened = make_int4(e, kv, (int)((end * rg.ranges - 1) / rg.total), 0);   // the last unit's block
+            opened = Opened{e, kv, rg.block_of(end - 1), it.pos0, it.rows, it.b, it.r0, 0};
         }
     }
     if (threadIdx.x == 0) a.opened[blockIdx.x] = opened;
@@ -692,6 +727,8 @@ __device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds,
     const int lane = lane_id(), wave = uniform((int)threadIdx.x / 64);
     const int g = lane >> 4, c = lane & 15;
     const float c1 = a.scale * kLog2E;
+    const int kbase = (it.lo / kUnit + u0) * kUnit, kend = (it.lo / kUnit + u1) * kUnit;
+    int entry = load_entry<4>(a, it, kbase);
     constexpr int kQ = NT > 2 ? 2 : NT;   // tiles whose queries stay in registers
     bf16x8_t q[NT > 2 ? 2 : NA][S];
     int see_lo[NA], see_hi[NA];
@@ -728,7 +765,6 @@ __device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds,
         for (int j = 0; j < NJ; ++j) o[t][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
 
-    const int kbase = (it.lo / kUnit + u0) * kUnit, kend = (it.lo / kUnit + u1) * kUnit;
     const char *kh = a.c.k + (int64_t)kv * a.c.head, *vh = a.c.v + (int64_t)kv * a.c.head;
     const uint32_t slot = (uint32_t)a.c.slot;
     const uint32_t k_off = (uint32_t)c * slot + 16 * g;
@@ -737,7 +773,6 @@ __device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds,
     uint32_t vr[8][1][VW];
     float sc = 0.f;
     uint64_t bad_next = 0;
-    int entry = load_entry<4>(a, it, kbase);
     auto fetch = [&](int k0) {
         const Tiles tl = take_tiles<4, kE4m3>(a, it, k0, entry, kv);
         bad_next = tl.bad;
@@ -853,14 +888,45 @@ __device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds,
                     if constexpr (kE4m3) nan |= lds.odd[buf][hh][2];
                     nan >>= 4 * g;
                 }
+                // the tiles' scores together: one branch for all of them, and exponentials of one
+                // among sums of another
+                float sc[NT];
+                f32x4_t ks[2];
+                if constexpr (kE4m3) ks[0] = lds.scale[buf][0][8 * hh + g], ks[1] = lds.scale[buf][0][8 * hh + 4 + g];
+                bool raise = false;
+                float mx[NT];
+                const int j = j0 + 4 * g;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) sc[n] = scale_scores<kE4m3>(a, sx[n], c1, ks[0], ks[1]);
+                if (!plain) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) mask_scores(sx[n], Seen{see_lo[n] - j, see_hi[n] - j, nan});
+                }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    f32x4_t ks[2];
-                    if constexpr (kE4m3) ks[0] = lds.scale[buf][0][8 * hh + g], ks[1] = lds.scale[buf][0][8 * hh + 4 + g];
-                    const float sc = scale_scores<kE4m3>(a, sx[n], c1, ks[0], ks[1]);
-                    const int j = j0 + 4 * g;
-                    if (!plain) mask_scores(sx[n], Seen{see_lo[n] - j, see_hi[n] - j, nan});
-                    weigh<NJ>(sx[n], sc, m[n], l[n], o[n]);
+                    mx[n] = max_of(sx[n]) * sc[n];
+                    raise |= mx[n] > m[n] + kSlack;
+                }
+                if (__any(raise)) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const float mn = fmaxf(m[n], query_max(mx[n]));
+                        const float f = __builtin_amdgcn_exp2f(m[n] - mn);
+                        m[n] = mn;
+                        l[n] *= f;
+#pragma unroll
+                        for (int j = 0; j < NJ; ++j) o[n][j] *= f;
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            sx[n][t][r] = __builtin_amdgcn_exp2f(fmaf(sx[n][t][r], sc[n], -m[n]));
+                            l[n] += sx[n][t][r];
+                        }
                     if constexpr (kE4m3) {
                         sx[n][0] *= lds.scale[buf][1][8 * hh + g];
                         sx[n][1] *= lds.scale[buf][1][8 * hh + 4 + g];
@@ -929,21 +995,21 @@ template <int D, bool kE4m3, int kMT>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_wide_kernel(AttnArgs a, int R) {
     __shared__ WideLds<D> lds;
     __shared__ int64_t s_w[8];
-    __shared__ int s_e;
+    __shared__ int s_e[3];
     const int wave = uniform((int)threadIdx.x / 64);
-    const Range rg = block_range(a, R, s_w, &s_e);
+    const Range rg = block_range(a, R, s_w, s_e);
     int e = rg.e;
+    Item it = rg.it;
     int64_t x = rg.x0, first = rg.first;
-    int4 opened = make_int4(-1, 0, 0, 0);
+    Opened opened = kNothing;
     while (x < rg.x1) {
-        const Item it = item_of(a, e, R);
         const int64_t span = (int64_t)it.units * a.c.heads;
         if (x >= first + span) {
             first += span;
-            ++e;
+            it = item_of(a, ++e, R);
             continue;
         }
-        const int kv = (int)((x - first) / it.units);
+        const int kv = (int)quotient(x - first, it.units);
         const int u0 = (int)((x - first) - (int64_t)kv * it.units);
         const int u1 = (int)min((int64_t)it.units, u0 + (rg.x1 - x));
         x += u1 - u0;
@@ -959,51 +1025,71 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_wide_kernel(
             wide_segment<D, kE4m3, kMT - 1>(a, lds, it, kv, u0, u1, tile0, R);
         if (u0 == 0 && u1 < it.units) {
             const int64_t end = first + (int64_t)(kv + 1) * it.units;
-            opened = make_int4(e, kv, (int)((end * rg.ranges - 1) / rg.total), 0);
+            opened = Opened{e, kv, rg.block_of(end - 1), it.pos0, it.rows, it.b, it.r0, 0};
         }
     }
     if (threadIdx.x == 0) a.opened[blockIdx.x] = opened;
 }
 
-// One wave per row of an item that spans blocks, in the order of the blocks that open one: the parts' weights from their maxima
-// and sums, 64 parts a round, and the parts' rows added up in order.
+// D / 4 lanes per row of an item that spans blocks, which is found by the block that opens it:
+// the parts' rows, weighed by their maxima, added up in order.  Eight parts are asked for
+// together, and ahead of the eight before being used.
 template <int D>
 __global__ __launch_bounds__(256) void cache_attn_join_kernel(AttnArgs a, int R) {
-    const int lane = lane_id(), row = blockIdx.y * 4 + (int)threadIdx.x / 64;
-    const int4 item = a.opened[blockIdx.x];
-    if (item.x < 0) return;
-    const int kv = item.y, parts = item.z - (int)blockIdx.x + 1;
-    const Item it = item_of(a, item.x, R);
-    if (row >= it.rows) return;
-    auto part = [&](int i) { return partial_at<D>(a, blockIdx.x + i, i == 0, R); };
-    float mg = -INFINITY;
-    for (int i = lane; i < parts; i += 64) mg = fmaxf(mg, part(i)[R * D + 2 * row]);
-    mg = wave_max_f32(mg);
-    float lg = 0.f, y[D / 64] = {};
-    for (int i0 = 0; i0 < parts; i0 += 64) {
-        float f = 0.f, lp = 0.f;
-        if (i0 + lane < parts) {
-            const float *ml = part(i0 + lane) + R * D + 2 * row;
-            f = __builtin_amdgcn_exp2f(ml[0] - mg);
-            lp = ml[1] * f;
-        }
-        lg += wave_sum_f32(lp);
-        const int n = min(64, parts - i0);
-        for (int i = 0; i < n; ++i) {
-            const float w = __shfl(f, i);
-            const float *p = part(i0 + i) + row * D + lane * (D / 64);
+    constexpr int L = D / 4, kParts = 8;
+    const int row = blockIdx.y * (256 / L) + (int)threadIdx.x / L, lane = (int)threadIdx.x % L;
+    const Opened op = a.opened[blockIdx.x];
+    if (op.e < 0 || row >= op.rows) return;
+    const int parts = op.last - (int)blockIdx.x + 1;
+    float ml[2][kParts][2];
+    f32x4_t y[2][kParts];
+    auto load = [&](int i0, int to) {
 #pragma unroll
-            for (int k = 0; k < D / 64; ++k) y[k] = fmaf(w, p[k], y[k]);
+        for (int i = 0; i < kParts; ++i) {
+            const int n = min(i0 + i, parts - 1);   // (the last one again for those past the end)
+            const float *p = partial_at<D>(a, blockIdx.x + n, n == 0, R);
+            y[to][i] = *reinterpret_cast<const f32x4_t *>(p + row * D + 4 * lane);
+            const float2 w = *reinterpret_cast<const float2 *>(p + R * D + 2 * row);
+            ml[to][i][0] = w.x;
+            ml[to][i][1] = w.y;
+        }
+    };
+    load(0, 0);
+    float m = kNoMax, l = 0.f;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < parts; i0 += kParts) {
+        if (i0 + kParts < parts) load(i0 + kParts, 1);
+        float mx = m;
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) mx = fmaxf(mx, ml[0][i][0]);
+        const float f = __builtin_amdgcn_exp2f(m - mx);
+        m = mx;
+        l *= f;
+        o *= f;
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) {
+            if (i0 + i >= parts) continue;
+            const float w = __builtin_amdgcn_exp2f(ml[0][i][0] - m);
+            l = fmaf(w, ml[0][i][1], l);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o[k] = fmaf(w, y[0][i][k], o[k]);
+        }
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) {
+            y[0][i] = y[1][i];
+            ml[0][i][0] = ml[1][i][0];
+            ml[0][i][1] = ml[1][i][1];
         }
     }
+    Item it;
+    it.b = op.b, it.r0 = op.r0, it.pos0 = op.pos0;
     int64_t oat, lat;
     bool gone;
-    put_row<D>(a, it, kv, row, oat, lat, gone);
-    const float inv = gone ? __uint_as_float(0x7fc00000u) : 1.f / lg;
-#pragma unroll
-    for (int k = 0; k < D / 64; ++k)
-        a.out[oat + lane * (D / 64) + k] = (uint16_t)pack_bf16(y[k] * inv, 0.f);
-    if (a.lse && lane == 0) a.lse[lat] = gone ? inv : (mg + __log2f(lg)) * kLn2;
+    put_row<D>(a, it, op.kv, row, oat, lat, gone);
+    const float inv = gone ? __uint_as_float(0x7fc00000u) : 1.f / l;
+    *reinterpret_cast<uint2 *>(a.out + oat + 4 * lane) =
+        make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+    if (a.lse && lane == 0) a.lse[lat] = gone ? inv : (m + __log2f(l)) * kLn2;
 }
 
 // ------------------------------------------------ chosen heads at one row
@@ -1082,8 +1168,9 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void cache_attn_rows_kernel(
     total = uniform(total) * heads;
     before *= heads;
     mine *= heads;
-    int64_t x = total * blockIdx.x / gridDim.x;
-    const int64_t x1 = total * (blockIdx.x + 1) / gridDim.x;
+    const int64_t part = quotient(total, gridDim.x), longer = total - part * gridDim.x;
+    int64_t x = part * blockIdx.x + min((int64_t)blockIdx.x, longer);
+    const int64_t x1 = x + part + (blockIdx.x < longer);
     if (x >= x1) return;
     if (before <= x && x < before + mine) {
         int b = b0;
@@ -1104,7 +1191,7 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void cache_attn_rows_kernel(
             ++b;
             continue;
         }
-        const int ki = (int)((x - first) / units);
+        const int ki = (int)quotient(x - first, units);
         const int u0 = (int)((x - first) - ki * units), u1 = (int)min(units, u0 + (x1 - x));
         x += u1 - u0;
         const int kv = ki < used ? uniform(s_used[ki]) : -1;
@@ -1255,7 +1342,7 @@ static void launch_attn(const AttnArgs &a, const AttnShape &sh, hipStream_t s) {
         go_wide(cache_attn_wide_kernel<D, kE4m3, 2>);
     else if constexpr (D < 256)
         go_wide(cache_attn_wide_kernel<D, kE4m3, 3>);
-    hipLaunchKernelGGL(cache_attn_join_kernel<D>, dim3(grid.x, (unsigned)(R / 4)), dim3(256), 0, s, a, R);
+    hipLaunchKernelGGL(cache_attn_join_kernel<D>, dim3(grid.x, (unsigned)((R + 1024 / D - 1) / (1024 / D))), dim3(256), 0, s, a, R);
 }
 
 static int prep_attn(const pld_cache *cache, bool needs_v, const uint16_t *q, int64_t qs,
@@ -1291,7 +1378,7 @@ extern "C" size_t pld_cache_attn_workspace_bytes(int B, int n, int Hq, int heads
         (head_dim != 64 && head_dim != 128 && head_dim != 256))
         return 0;
     const AttnShape sh = attn_shape(n, Hq / heads, head_dim);
-    return partials_bytes(sh, head_dim) + kAttnBlocks * sizeof(int4);
+    return partials_bytes(sh, head_dim) + kAttnBlocks * sizeof(Opened);
 }
 
 extern "C" int pld_cache_attn(const pld_cache *cache, const uint16_t *q, int64_t q_seq_stride,
@@ -1316,7 +1403,7 @@ extern "C" int pld_cache_attn(const pld_cache *cache, const uint16_t *q, int64_t
     a.lse = lse;
     a.groups = sh.groups;
     a.partials = static_cast<float *>(workspace);
-    a.opened = reinterpret_cast<int4 *>(static_cast<char *>(workspace) + partials_bytes(sh, D));
+    a.opened = reinterpret_cast<Opened *>(static_cast<char *>(workspace) + partials_bytes(sh, D));
     const bool q8 = cache->dtype == PLD_E4M3;
     const hipStream_t s = (hipStream_t)stream;
     if (D == 64)

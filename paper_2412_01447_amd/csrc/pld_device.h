@@ -129,6 +129,11 @@ __device__ __forceinline__ uint32_t argmax_key_index(uint64_t k) {
 }
 
 // ------------------------------------------------------- wave reductions
+// a / b of numbers that are not negative: a division of 64 bits costs a wave some 0.4 us,
+// one of 32 a tenth of it, and most fit.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    return ((uint64_t)(a | b) >> 32) ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
 __device__ __forceinline__ int lane_id() { return (int)__lane_id(); }
 
 // Wave reductions use DPP lane moves -- quad permutes, the half-row and row

@@ -181,10 +181,16 @@ __global__ __launch_bounds__(kLogWaves * 64, 4) void token_logprobs_kernel(Logpr
     }
     // as many ranges as waves, or as segments where there are fewer: none between two is empty
     const int64_t total = rows * a.segs, ranges = min(total, (int64_t)gridDim.x * kLogWaves);
+    const int64_t share = ranges ? quotient(total, ranges) : 0, longer = total - share * ranges;
+    auto start = [&](int64_t id) { return share * id + min(id, longer); };
+    auto range_of = [&](int64_t x) {
+        const int64_t of_longer = (share + 1) * longer;
+        return (int)(x < of_longer ? quotient(x, share + 1) : longer + quotient(x - of_longer, share));
+    };
     for (int w = 0; w < kLogWaves; ++w) {
         const int64_t id = (int64_t)blockIdx.x * kLogWaves + w;
         if (id >= ranges) break;
-        const int64_t r0 = total * id / ranges / a.segs;   // the row of its first segment
+        const int64_t r0 = quotient(start(id), a.segs);   // the row of its first segment
         if (before <= r0 && r0 < before + mine) {
             int64_t f = before;
             int b = b0;
@@ -196,10 +202,11 @@ __global__ __launch_bounds__(kLogWaves * 64, 4) void token_logprobs_kernel(Logpr
     __syncthreads();
     const int id = (int)blockIdx.x * kLogWaves + wave;
     if (id >= ranges) return;
-    int64_t x = total * id / ranges;
-    const int64_t x1 = total * (id + 1) / ranges;
+    int64_t x = start(id);
+    const int64_t x1 = start(id + 1);
     int b = __builtin_amdgcn_readfirstlane(s_b[wave]), cnt = rows_of(a, b);
-    int i = (int)(x / a.segs - s_first[wave]), g = (int)(x % a.segs);
+    const int64_t x_row = quotient(x, a.segs);
+    int i = (int)(x_row - s_first[wave]), g = (int)(x - x_row * a.segs);
 
     while (x < x1) {
         const RowView<T, P> rv = row_view<T, P>(a.logits, a.ls, a.lr, b, i, a.V);
@@ -253,7 +260,7 @@ __global__ __launch_bounds__(kLogWaves * 64, 4) void token_logprobs_kernel(Logpr
         w.join_lanes();
         if (lane == 0) {
             a.masses[(int64_t)id * 2 + (g0 == 0)] = make_float4(w.c, w.s, w.t, 0.f);
-            if (g0 == 0) a.parts[row] = make_int2(id, (int)(((x + (a.segs - g1)) * ranges - 1) / total));
+            if (g0 == 0) a.parts[row] = make_int2(id, range_of(x + (a.segs - g1) - 1));
         }
         g = 0;
         if (x < x1 && ++i >= cnt) {
