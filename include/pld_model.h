@@ -104,7 +104,8 @@ typedef struct pld_cache {
  * Device-side rule: a row whose position is past the table of pages (or past
  * n_pos, with rope), or whose page is bad, is not stored, and its q_out is NaN.
  * Errors: PLD_ERR_INVALID (NULL, a size out of range, Hq not a multiple of the
- * cache's heads, eps not finite or negative), PLD_ERR_ALIGN, PLD_ERR_LAUNCH.
+ * cache's heads, eps not finite or negative, q_out at q with other strides),
+ * PLD_ERR_ALIGN, PLD_ERR_LAUNCH.
  */
 int pld_cache_write(const pld_cache *cache, const uint16_t *q, int64_t q_seq_stride,
                     int64_t q_row_stride, const uint16_t *k, int64_t k_seq_stride,
@@ -133,8 +134,10 @@ int pld_cache_write(const pld_cache *cache, const uint16_t *q, int64_t q_seq_str
  * Device-side rules: keys that a row does not see do not affect it, whatever
  * their slots hold; a row one of whose keys lies on a bad page or past the table
  * gets NaN in out and lse.  Where a value that a row sees is not finite, that head
- * of its out, and its lse, may be NaN as a whole.
- * Errors: PLD_ERR_INVALID, PLD_ERR_ALIGN, PLD_ERR_WORKSPACE, PLD_ERR_LAUNCH.
+ * of its out, and its lse, may be NaN as a whole.  A row has to see a score above
+ * -1e29 (no finite inputs of ordinary size come near it).
+ * Errors: PLD_ERR_INVALID (also out at q), PLD_ERR_ALIGN, PLD_ERR_WORKSPACE,
+ * PLD_ERR_LAUNCH.
  */
 size_t pld_cache_attn_workspace_bytes(int B, int n, int Hq, int heads, int head_dim);
 

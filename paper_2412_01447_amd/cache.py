@@ -16,7 +16,9 @@ class PagedCache:
     """Pages for B sequences of up to max_len positions each (committed tokens plus draft).
     dtype: torch.bfloat16, or torch.float8_e4m3fn with one fp32 scale per slot and head.
     `table` [B][pages] starts as sequence b's own run of pages; a caller that shares, moves or
-    grows sequences writes its entries (num_pages: the pages to allocate, default B's own)."""
+    grows sequences writes its entries (num_pages: the pages to allocate, default B's own).
+    There is one workspace: attend() calls on several streams at once need a PagedCache each,
+    or pld_cache_attn with workspaces of their own."""
 
     def __init__(self, B, max_len, heads, head_dim, page_size=64, dtype=torch.bfloat16,
                  device="cuda", num_pages=None):
@@ -34,13 +36,17 @@ class PagedCache:
             self.v_scale = torch.zeros((num_pages, heads, page_size), device=device)
         self.table = torch.arange(B * per, dtype=torch.int32, device=device).view(B, per)
         self.workspace = None
+        self.grown = []                  # workspaces that a larger one has replaced
 
     def reserve(self, n, Hq):
         """The attention's workspace for n rows a sequence (grown by attend() as needed: a
-        caller that captures a graph reserves before the capture)."""
+        caller that captures a graph reserves before the capture).  One that is replaced is
+        kept: captured graphs and prepared calls go on using it."""
         need = pld_cache_attn_workspace_bytes(self.B, n, Hq, self.heads, self.head_dim)
         if self.workspace is None or self.workspace.numel() < need:
-            self.workspace = torch.zeros(need, dtype=torch.uint8, device=self.k.device)
+            if self.workspace is not None:
+                self.grown.append(self.workspace)
+            self.workspace = torch.empty(need, dtype=torch.uint8, device=self.k.device)
 
     def write(self, q, k, v, lens, q_out, draft_len=None, q_norm=None, k_norm=None, eps=1e-6,
               rope=None, rope_pairs=PLD_ROPE_HALVES, stream=None, prepare=False):

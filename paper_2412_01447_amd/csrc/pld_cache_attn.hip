@@ -1398,7 +1398,7 @@ extern "C" int pld_cache_attn(const pld_cache *cache, const uint16_t *q, int64_t
         workspace_bytes < pld_cache_attn_workspace_bytes(B, n, Hq, cache->heads, D))
         return PLD_ERR_WORKSPACE;
     const AttnShape sh = attn_shape(n, a.G, D);
-    if ((int64_t)B * sh.groups > INT32_MAX / 2) return PLD_ERR_INVALID;
+    if (out == q || (int64_t)B * sh.groups > INT32_MAX / 2) return PLD_ERR_INVALID;
     a.out = out, a.os = o_seq_stride, a.orow = o_row_stride;
     a.lse = lse;
     a.groups = sh.groups;

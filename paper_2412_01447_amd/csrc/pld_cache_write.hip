@@ -165,6 +165,8 @@ extern "C" int pld_cache_write(const pld_cache *cache, const uint16_t *q, int64_
         (rc = check_rows(v, v_seq_stride, v_row_stride, B, n, kw)) != PLD_OK ||
         (rc = check_rows(q_out, o_seq_stride, o_row_stride, B, n, qw)) != PLD_OK)
         return rc;
+    if (q_out == q && ((B > 1 && o_seq_stride != q_seq_stride) || (n > 1 && o_row_stride != q_row_stride)))
+        return PLD_ERR_INVALID;
     if (!(eps >= 0.f) || !isfinite(eps)) return PLD_ERR_INVALID;
     if ((uintptr_t)q_norm % 16 || (uintptr_t)k_norm % 16) return PLD_ERR_ALIGN;
     if (rope_pairs != PLD_ROPE_HALVES && rope_pairs != PLD_ROPE_NEIGHBOURS) return PLD_ERR_INVALID;

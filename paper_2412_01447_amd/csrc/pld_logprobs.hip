@@ -421,11 +421,11 @@ __global__ __launch_bounds__(kLogWaves * 64) void token_logprobs_finish_kernel(L
     float m = 0.f;
     if (!(w.s > 0.f)) {
         m = -INFINITY;
-        for (int v = lane; v < a.V; v += kWave) m = fmaxf(m, E::get(rv.row, v));
+        for (int64_t v = lane; v < a.V; v += kWave) m = fmaxf(m, E::get(rv.row, v));
         m = wave_max_f32(m);
         none = !(m > -INFINITY);
         w = Mass{0.f, 0.f, 0.f};
-        for (int v = lane; v < a.V && !none; v += kWave) w.add(E::get(rv.row, v) - m, a.k);
+        for (int64_t v = lane; v < a.V && !none; v += kWave) w.add(E::get(rv.row, v) - m, a.k);
         w.s = wave_sum_f32(w.s);
         w.t = wave_sum_f32(w.t);
     }

@@ -94,7 +94,8 @@ class DraftStep:
         """From now on every step also gives its emitted tokens' log probabilities under
         softmax(logits / temperature): self.logprob [B][K+1], self.logprob_entropy [B][K+1]
         and, for top > 0, the rows' most likely tokens self.top_ids and self.top_logprobs
-        [B][K+1][top] (rows past out_count keep what they held).  V None: no longer."""
+        [B][K+1][top] (rows past out_count keep what they held).  V None: no longer.  The
+        buffers are new ones at each call: plans and graphs are made after it."""
         if V is None:
             self.logprob = None
             return

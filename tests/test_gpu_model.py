@@ -173,6 +173,41 @@ def test_attend_large_batch():
     c.check_attend(out, L, rows={(int(b), int(i)) for b, i in zip(rng.integers(0, 700, 90), rng.integers(0, 3, 90))})
 
 
+def test_largest_batch_of_single_tokens():
+    """65535 sequences of one token: the only key's value is the output, bit for bit, and its
+    score the log sum; then the same keys' weights, all 1."""
+    B, D = 65535, 64
+    rng = np.random.default_rng(4)
+    q, k, v = (normal(rng, B, 1, 1, D) for _ in range(3))
+    cache = PagedCache(B, 16, 1, D, page_size=16)
+    lens, q_out = torch.ones(B, dtype=torch.int32, device=dev()), torch.zeros_like(q)
+    cache.write(q, k, v, lens, q_out)
+    assert np.array_equal(bits(q_out), bits(q))
+    assert np.array_equal(bits(cache.k[:, 0]), bits(k[:, 0])) and np.array_equal(bits(cache.v[:, 0]), bits(v[:, 0]))
+    assert not cache.k[:, 1:].any() and not cache.v[:, 1:].any()
+    out, L = torch.zeros_like(q), torch.zeros((B, 1, 1), device=dev())
+    cache.attend(q, lens, out, lse=L)
+    assert np.array_equal(bits(out), bits(v))
+    x = (f64(q) * f64(k)).sum(-1) / 8
+    tol = (D + 8) * U * (np.abs(f64(q)) * np.abs(f64(k))).sum(-1) / 8
+    assert (np.abs(f64(L) - x) <= ref.lse_bound(tol, x, 1)).all()
+    attn = torch.full((B, 1, 3), 7.0, device=dev())
+    cache.weights(q, lens, torch.zeros_like(lens), d_i32([0]), L, attn)
+    a = f64(attn)
+    assert (np.abs(a[:, :, 0] - 1) <= np.expm1(2 * tol + 16 * U * (1 + np.abs(x)))[:, 0]).all() and (a[:, :, 1:] == 7).all()
+
+
+@pytest.mark.parametrize("G,D,window,dtype", [(8, 64, 0, "bf16"), (1, 128, 300, "bf16"), (12, 64, 100, "e4m3")])
+def test_prompt_chunk(G, D, window, dtype):
+    """Thousands of rows a sequence, in many groups; a sample of them is checked."""
+    n = 3000
+    c = Case([1, 500], n, G, 1, D, 64, E4M3 if dtype == "e4m3" else torch.bfloat16, [n - 1, 1700], seed=G)
+    out, L = c.attend(window=window)
+    rows = {(0, 0), (0, 1), (0, 17), (0, 1499), (0, 2998), (0, 2999), (1, 0), (1, 333), (1, 1700)}
+    c.check_attend(out, L, window=window, rows=rows)
+    assert not torch.isnan(out.float()).any()
+
+
 def test_attend_spread_scores():
     """Scores thousands apart (one key takes all), equal keys, and a head of zeros."""
     c = Case([300, 40], 2, 8, 2, 128, 16, seed=3, gain=60.0)
@@ -431,6 +466,8 @@ ROWS = [
     ([90, 257], 4, 6, 1, 256, 64, "e4m3", 0, 50, [3, 0], [5, 1, 2, 0, 4], 0),
     ([500, 100], 2, 64, 1, 128, 16, "bf16", 0, 0, [1, 1], list(range(0, 64, 2)) + [1] * 9, 300),
     ([130], 2, 4, 4, 256, 128, "bf16", 20.0, 33, [0], [2, 4, -1, 1], 1),
+    ([40, 7], 2, 6, 3, 64, 16, "bf16", 0, 0, [1, 0], [r * 5 % 8 - 1 for r in range(700)], 0),   # past the list in LDS
+    (list(range(1, 301)), 2, 4, 2, 64, 16, "bf16", 0, 0, [b % 4 - 1 for b in range(300)], [3, 0], 0),
 ]
 
 
@@ -504,6 +541,10 @@ LOGPROBS = [
     (2, 3, 12345, "bf16", 1.0, 30, "sorted"),
     (1, 2, 1000003, "bf16", 1.0, 0, "normal"),
     (1, 3, 40000, "f32", 1.0, 33, "block"),
+    (1, 2, 200003, "f32", 1.0, 64, "ties"),        # a row's maxima in several rounds
+    (2, 3, 140001, "bf16", 1.5, 64, "masked"),
+    (1, 2, 262144, "bf16", 1.0, 40, "equal"),
+    (700, 2, 129, "bf16", 1.0, 3, "normal"),       # more sequences than threads of a block
 ]
 
 
@@ -797,3 +838,63 @@ def test_two_streams_at_once():
     for x, y in got:
         assert np.array_equal(bits(x[0]), bits(wa[0])) and np.array_equal(bits(x[1]), bits(wa[1]))
         assert np.array_equal(bits(y[0]), bits(wb[0])) and np.array_equal(bits(y[1]), bits(wb[1]))
+
+
+def test_a_workspace_that_grew_stays_with_its_calls():
+    """A prepared call keeps its workspace when the cache's grows: memory that is allocated
+    afterwards is left alone, and the call's results stay the same."""
+    rng = np.random.default_rng(8)
+    cache = PagedCache(2, 2000, 2, 64, page_size=16)
+    cache.k.copy_(normal(rng, *cache.k.shape))
+    cache.v.copy_(normal(rng, *cache.v.shape))
+    q, lens = normal(rng, 2, 1, 8, 64), d_i32([1990, 700])
+    out = torch.zeros_like(q)
+    call = cache.attend(q, lens, out, prepare=True)
+    call()
+    want, size = out.clone(), cache.workspace.numel()
+    cache.attend(normal(rng, 2, 9, 8, 64), d_i32([1900, 60]), torch.zeros((2, 9, 8, 64), dtype=torch.bfloat16, device=dev()))
+    assert cache.workspace.numel() > size
+    later = [torch.full((size,), 0x55, dtype=torch.uint8, device=dev()) for _ in range(4)]
+    out.zero_()
+    call()
+    assert np.array_equal(bits(out), bits(want)) and all(bool((t == 0x55).all()) for t in later)
+
+
+def test_two_graphs_share_a_workspace():
+    """An attention and log probabilities captured twice over one workspace each, replayed in
+    turn with the program's own work between: every replay is the eager call's result."""
+    a = Case([5000, 3, 900], 5, 8, 2, 128, 16, seed=1)
+    b = Case([40, 2000], 9, 16, 2, 64, 32, seed=2)
+    ws = torch.zeros(max(pld.pld_cache_attn_workspace_bytes(len(c.lens), c.n, c.Hq, c.heads, c.D) for c in (a, b)),
+                     dtype=torch.uint8, device=dev())
+    rng = np.random.default_rng(3)
+    z = [torch.from_numpy(rng.standard_normal((2, 3, V), dtype=np.float32)).to(dev()) for V in (5000, 33000)]
+    lws = torch.zeros(pld.pld_token_logprobs_workspace_bytes(2, 3, 33000, pld.PLD_F32, 7), dtype=torch.uint8, device=dev())
+    tok = d_i32(np.full((2, 3), 4))
+    runs = []
+    for c, x in zip((a, b), z):
+        out, L = torch.zeros_like(c.q), torch.zeros((len(c.lens), c.n, c.Hq), device=dev())
+        lp, ids = torch.zeros((2, 3), device=dev()), torch.zeros((2, 3, 7), dtype=torch.int32, device=dev())
+        tl = torch.zeros((2, 3, 7), device=dev())
+
+        def run(c=c, x=x, out=out, L=L, lp=lp, ids=ids, tl=tl):
+            pld.pld_cache_attn(c.q, c.k, c.v, c.t, c.d_lens, out, ws, lse=L)
+            pld.pld_token_logprobs(x, tok, lp, lws, top_ids=ids, top_logprobs=tl)
+
+        run()
+        outs = (out, L, lp, ids, tl)
+        want = [bits(t) for t in outs]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            run()
+        runs.append((graph, outs, want))
+    noise = torch.zeros(1000, device=dev())
+    for turn in range(6):
+        for graph, outs, want in runs:
+            for t in outs:
+                t.zero_()
+            graph.replay()
+            noise += 1
+            if turn % 2:
+                torch.cuda.synchronize()
+            assert all(np.array_equal(bits(t), w) for t, w in zip(outs, want)), turn

@@ -148,6 +148,29 @@ def test_host_checks():
     refused(lp, LP, 3, wsb=pld.pld_token_logprobs_workspace_bytes(2, 2, 100, 0, 3) - 1)
 
 
+@no_gpu
+def test_limits():
+    """The largest strides and lengths that the kernels' 32-bit offsets are made for, and one
+    call whose outputs would be read while they are written."""
+    lib = pld._load()
+    calls = ((lib.pld_cache_write, WRITE), (lib.pld_cache_attn, ATTN), (lib.pld_cache_attn_rows, ROWS))
+    for kw in (dict(slot_stride=(1 << 24) + 8), dict(page_stride=(1 << 34) + 8),
+               dict(Q8, scale_page_stride=(1 << 31) + 4)):
+        for fn, args in calls:
+            assert fn(_cache(**kw), *args.values()) == 1, kw
+    # in range: the next check speaks
+    for kw in (dict(slot_stride=1 << 24, k=0x1008), dict(page_stride=1 << 34, k=0x1008),
+               dict(Q8, scale_page_stride=1 << 31, k_scale=0x4004)):
+        for fn, args in calls:
+            assert fn(_cache(**kw), *args.values()) == 2, kw
+    n_keys = 2 ** 31 - 65536
+    assert lib.pld_cache_attn_rows(_cache(), *{**ROWS, "keys": n_keys, "as_": 3 * n_keys, "ar": n_keys}.values()) == 1
+    same = P(0x8000)
+    assert lib.pld_cache_attn(_cache(), *{**ATTN, "q": same, "out": same}.values()) == 1
+    for other in (dict(os=520), dict(orow=264, os=600)):
+        assert lib.pld_cache_write(_cache(), *{**WRITE, "q": same, "out": same, **other}.values()) == 1
+
+
 def test_workspace_bytes():
     for args in ((0, 1, 8, 2, 64), (65536, 1, 8, 2, 64), (1, 0, 8, 2, 64), (1, 1, 8, 3, 64), (1, 1, 8, 2, 96), (1, 1, 0, 2, 64)):
         assert pld.pld_cache_attn_workspace_bytes(*args) == 0
