@@ -281,11 +281,34 @@ __global__ __launch_bounds__(kLogWaves * 64) void token_logprobs_finish_kernel(L
     __shared__ int s_groups[kTop ? kLogWaves : 1][kTop ? kGroups : 1];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
     const int b = blockIdx.y, i = (int)blockIdx.x * kLogWaves + wave;
-    if (i >= rows_of(a, b)) return;
+    if (i >= a.n) return;
+    // What does not go by the count is asked for together with it, whether the row exists or
+    // not: a wave has little else to do than to wait.
     const int64_t row = (int64_t)b * a.n + i;
-    const RowView<T, P> rv = row_view<T, P>(a.logits, a.ls, a.lr, b, i, a.V);
+    const int cnt = rows_of(a, b);
     const int2 part = a.parts[row];
     const int tok = a.tokens[row];
+    constexpr int kChunk = 8;   // vectors a lane: a bf16 row of up to 131072 at once
+    const uint4 *maxima = reinterpret_cast<const uint4 *>(static_cast<const T *>(a.maxima) + row * a.segs * kWave);
+    const int vecs = a.segs * (kWave / P);
+    uint4 mv[kChunk];
+    auto load = [&](int v0) {
+#pragma unroll
+        for (int q = 0; q < kChunk; ++q) mv[q] = maxima[min(v0 + q * kWave + lane, vecs - 1)];
+    };
+    // Each lane's largest of the maxima; the top-th largest of those is a floor.
+    float own = -INFINITY;
+    if constexpr (kTop) {
+        for (int v0 = 0; v0 < vecs; v0 += kChunk * kWave) {
+            load(v0);
+            // (no other lane's vector in place of an absent one: the floor counts lanes)
+#pragma unroll
+            for (int q = 0; q < kChunk; ++q)
+                if (v0 + q * kWave + lane < vecs) own = fmaxf(own, E::vmax(mv[q]));
+        }
+    }
+    if (i >= cnt) return;
+    const RowView<T, P> rv = row_view<T, P>(a.logits, a.ls, a.lr, b, i, a.V);
     const float z_tok = E::get(rv.row, tok >= 0 && tok < a.V ? tok : 0);
     Mass w;
     for (int p = part.x + lane; p <= part.y; p += kWave) {
@@ -301,23 +324,6 @@ __global__ __launch_bounds__(kLogWaves * 64) void token_logprobs_finish_kernel(L
 
     Best best{s_keys[kTop ? wave : 0], s_keys[kTop ? wave : 0] + (kTop ? kKeys : 0), a.top};
     if constexpr (kTop) {
-        // Each lane's largest of the maxima; the top-th largest of those is a floor.
-        const uint4 *maxima = reinterpret_cast<const uint4 *>(static_cast<const T *>(a.maxima) + row * a.segs * kWave);
-        constexpr int kChunk = 8;   // vectors a lane: a bf16 row of up to 131072 at once
-        const int vecs = a.segs * (kWave / P);
-        uint4 m[kChunk];
-        auto load = [&](int v0) {
-#pragma unroll
-            for (int q = 0; q < kChunk; ++q) m[q] = maxima[min(v0 + q * kWave + lane, vecs - 1)];
-        };
-        float own = -INFINITY;
-        for (int v0 = 0; v0 < vecs; v0 += kChunk * kWave) {
-            load(v0);
-            // (no other lane's vector in place of an absent one: the floor counts lanes)
-#pragma unroll
-            for (int q = 0; q < kChunk; ++q)
-                if (v0 + q * kWave + lane < vecs) own = fmaxf(own, E::vmax(m[q]));
-        }
         best.raise_floor<kBf16>(lane < vecs ? ord_f32(own) : 0);
 
         // The groups of a list of (segment, lane), L lanes each: a vector a lane.
@@ -376,7 +382,7 @@ __global__ __launch_bounds__(kLogWaves * 64) void token_logprobs_finish_kernel(L
 #pragma unroll
             for (int q = 0; q < kChunk; ++q) {
                 float y[P];
-                E::unpack(m[q], y);
+                E::unpack(mv[q], y);
 #pragma unroll
                 for (int e = 0; e < P; ++e) mask |= (uint64_t)(q * kWave + lane < vecs && y[e] >= best.at) << (q * P + e);
             }
