@@ -1038,16 +1038,20 @@ template <int D>
 __global__ __launch_bounds__(256) void cache_attn_join_kernel(AttnArgs a, int R) {
     constexpr int L = D / 4, kParts = 8;
     const int row = blockIdx.y * (256 / L) + (int)threadIdx.x / L, lane = (int)threadIdx.x % L;
-    const Opened op = a.opened[blockIdx.x];
+    // (eight neighbours change places: items of one length are opened by blocks at some even
+    // distance, which would all be joined on one XCD)
+    const uint32_t x = blockIdx.x;
+    const int block = x < (gridDim.x & ~7u) ? (x & ~7u) | ((x - x / 8 - x / 64 - blockIdx.y) & 7) : x;
+    const Opened op = a.opened[block];
     if (op.e < 0 || row >= op.rows) return;
-    const int parts = op.last - (int)blockIdx.x + 1;
+    const int parts = op.last - block + 1;
     float ml[2][kParts][2];
     f32x4_t y[2][kParts];
     auto load = [&](int i0, int to) {
 #pragma unroll
         for (int i = 0; i < kParts; ++i) {
             const int n = min(i0 + i, parts - 1);   // (the last one again for those past the end)
-            const float *p = partial_at<D>(a, blockIdx.x + n, n == 0, R);
+            const float *p = partial_at<D>(a, block + n, n == 0, R);
             y[to][i] = *reinterpret_cast<const f32x4_t *>(p + row * D + 4 * lane);
             const float2 w = *reinterpret_cast<const float2 *>(p + R * D + 2 * row);
             ml[to][i][0] = w.x;
