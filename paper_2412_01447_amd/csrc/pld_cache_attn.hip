@@ -1048,15 +1048,20 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(AttnArgs a, int R)
     float ml[2][kParts][2];
     f32x4_t y[2][kParts];
     auto load = [&](int i0, int to) {
+        auto some = [&](int first, int last) {
 #pragma unroll
-        for (int i = 0; i < kParts; ++i) {
-            const int n = min(i0 + i, parts - 1);   // (the last one again for those past the end)
-            const float *p = partial_at<D>(a, block + n, n == 0, R);
-            y[to][i] = *reinterpret_cast<const f32x4_t *>(p + row * D + 4 * lane);
-            const float2 w = *reinterpret_cast<const float2 *>(p + R * D + 2 * row);
-            ml[to][i][0] = w.x;
-            ml[to][i][1] = w.y;
-        }
+            for (int i = first; i < last; ++i) {
+                const int n = min(i0 + i, parts - 1);   // (the last one again for those past the end)
+                const float *p = partial_at<D>(a, block + n, n == 0, R);
+                y[to][i] = *reinterpret_cast<const f32x4_t *>(p + row * D + 4 * lane);
+                const float2 w = *reinterpret_cast<const float2 *>(p + R * D + 2 * row);
+                ml[to][i][0] = w.x;
+                ml[to][i][1] = w.y;
+            }
+        };
+        some(0, 2);
+        if (i0 + 2 < parts) some(2, 4);
+        if (i0 + 4 < parts) some(4, kParts);
     };
     load(0, 0);
     float m = kNoMax, l = 0.f;
@@ -1065,7 +1070,8 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(AttnArgs a, int R)
         if (i0 + kParts < parts) load(i0 + kParts, 1);
         float mx = m;
 #pragma unroll
-        for (int i = 0; i < kParts; ++i) mx = fmaxf(mx, ml[0][i][0]);
+        for (int i = 0; i < kParts; ++i)
+            if (i0 + i < parts) mx = fmaxf(mx, ml[0][i][0]);
         const float f = __builtin_amdgcn_exp2f(m - mx);
         m = mx;
         l *= f;
