@@ -77,7 +77,10 @@ __device__ __forceinline__ float query_sum(float v) {
 // blocks in equal contiguous ranges, whatever the sequences' lengths; an item that
 // spans blocks leaves one partial result per block, joined by a second launch.
 constexpr int kUnit = 128;        // keys
-constexpr int kAttnBlocks = 512;  // two per CU; nothing depends on their being resident at once
+// Two per CU; nothing depends on their being resident at once.  Twice as many cost a start
+// and a join more than evener ends gain: 39 us become 48 (8 sequences of 4096, 11 rows), and
+// 530 become 665 (4 of 131072, 33 rows).
+constexpr int kAttnBlocks = 512;
 
 struct Item {
     int b, cnt, pos0, r0, rows;   // rows: of this group
@@ -389,7 +392,11 @@ __device__ __forceinline__ bf16x8_t value_operand(const uint32_t (&vp)[8][N][W],
     return as_bf16x8(make_uint4(r[0], r[1], r[2], r[3]));
 }
 
-// Four waves a block, each with all of the item's rows and 32 of a unit's keys.
+// Four waves a block, each with all of the item's rows and 32 of a unit's keys.  Bound by
+// HBM where there is much to read: 64 sequences of 8192, a row of 32 query heads over 8 key
+// heads of 128 in bf16 (2.15 GB): 345 us, 6.2 TB/s; in e4m3 64 of 16384: 391 us.  By the way
+// of one dependent load to the next (lengths, page entries, keys, partial results) where there
+// is little: 10.4 us for one row over 1024 tokens, both launches.
 template <int D, bool kE4m3, int kMT>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnArgs a) {
     constexpr int R = 16 * kMT;
@@ -704,7 +711,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
 // wave w the tiles w, w+4, w+8.  Keys and values of 64 positions go through LDS once,
 // as operands: each wave fetches a 16-key tile of K and, of 32 keys, half the elements
 // of V, into registers while the block works on the 64 before, and turns them (e4m3 to
-// bf16, V to pairs of keys) once for all waves on the way to LDS.
+// bf16, V to pairs of keys) once for all waves on the way to LDS.  16 x 8 rows of 8 heads a key
+// head over 8192 tokens: 138 us, 3.9 TB/s, of which the slowest XCD is 20 us behind the mean.
+// With three tiles a wave it is the instructions: 64 x 17 such rows over 16384 tokens in
+// e4m3 (144 rows a key head) take 855 us, 520 TFLOP/s, the matrix units busy for 26% of the time and
+// the vector units for 44%, two waves a SIMD (512 registers hold no third) waiting for the
+// rest; 4 x 33 rows of 4 heads a key head over 131072 tokens in bf16 510 us, 555 TFLOP/s and 4.2 TB/s.
+// (A ninth tile as two waves' work, half the keys each, took 5% longer.)
 constexpr int kStep = 64;   // keys
 template <int D>
 struct WideLds {
@@ -1032,8 +1045,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_wide_kernel(
 }
 
 // D / 4 lanes per row of an item that spans blocks, which is found by the block that opens it:
-// the parts' rows, weighed by their maxima, added up in order.  Eight parts are asked for
-// together, and ahead of the eight before being used.
+// the parts' rows, weighed by their maxima, added up in order.  Up to eight parts are asked for
+// together, and ahead of the eight before being used.  5 to 14 us, by the latency of two
+// dependent loads; 25 us for 512 items of 136 rows, by the 72 MB of their parts.
 template <int D>
 __global__ __launch_bounds__(256) void cache_attn_join_kernel(AttnArgs a, int R) {
     constexpr int L = D / 4, kParts = 8;
@@ -1107,7 +1121,9 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(AttnArgs a, int R)
 // operand, against up to 16 of those as the second: with the log sums known a weight is
 // final at once, and a lane stores its four keys of a row together.  The units of all
 // (sequence, used key head) pairs are dealt to the blocks as in the attention; a block's
-// four waves have 32 of a unit's keys each.
+// four waves have 32 of a unit's keys each.  Bound by memory, keys read and weights written:
+// 40 heads of 32 sequences of up to 8192 tokens (507 MB): 110 to 117 us, 4.3 to 4.6 TB/s; 8 heads
+// of one of 1024: 6.7 us.
 constexpr int kRowsBlocks = 1024;   // four per CU
 
 template <int D, bool kE4m3>

@@ -20,22 +20,38 @@ struct WriteArgs {
 
 // Sum and maximum over a group of G consecutive lanes (8, 16 or 32), the same
 // bits in each of them.
+template <int kCtrl>
+__device__ __forceinline__ float moved(float v) {
+    return __int_as_float(dpp_move<kCtrl, 0xf>(__float_as_int(v)));
+}
 template <int G>
 __device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-    for (int o = 1; o < G; o *= 2) v += __shfl_xor(v, o);
+    v += moved<kDppQuadSwap1>(v);
+    v += moved<kDppQuadSwap2>(v);
+    v += moved<kDppHalfMirror>(v);
+    if (G > 8) v += moved<kDppMirror>(v);
+    if (G > 16) v += __shfl_xor(v, 16);
     return v;
 }
 template <int G>
 __device__ __forceinline__ float group_max(float v) {
-#pragma unroll
-    for (int o = 1; o < G; o *= 2) v = fmaxf(v, __shfl_xor(v, o));
+    v = fmaxf(v, moved<kDppQuadSwap1>(v));
+    v = fmaxf(v, moved<kDppQuadSwap2>(v));
+    v = fmaxf(v, moved<kDppHalfMirror>(v));
+    if (G > 8) v = fmaxf(v, moved<kDppMirror>(v));
+    if (G > 16) v = fmaxf(v, __shfl_xor(v, 16));
     return v;
 }
 
 // D / 8 lanes a head's row, each holding two runs of four elements, t0 and t1:
 // with pairs of halves the runs are each other's partners (t1 = t0 + rot/2), so
-// a rotation needs no other lane; elsewhere they are neighbours.
+// a rotation needs no other lane; elsewhere they are neighbours.  Bound by memory: 4 x 2048
+// rows of 32 + 2 x 8 heads of 128 (202 MB) in 41 us, 4.9 TB/s, what a large copy reaches (4.83);
+// up to 17 rows of 64 + 2 x 8 heads in each of 64 sequences, into e4m3 (36 MB), in 10.4 us, the vector
+// instructions of norms and quotients included.  One head a lane group: with four, and their
+// loads together, the waves are too few (41 and 13.5 us, and 3.9 instead of 2.6 us for a
+// single row).  Blocks of one kind of head each would have less to select, but are a third
+// more, and the launch of blocks takes as long as the memory (52 us instead of 41).
 template <int D, bool kHalves, bool kE4m3>
 __global__ __launch_bounds__(256) void cache_write_kernel(WriteArgs a) {
     constexpr int G = D / 8;
@@ -118,8 +134,14 @@ __global__ __launch_bounds__(256) void cache_write_kernel(WriteArgs a) {
         for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(x[e]));
         // a scale of at least the smallest normal number, so that the division stays finite
         const float scale = fmaxf(group_max<G>(m) / kE4m3Max, 1.17549435e-38f);
+        // a quotient from the reciprocal, with what it leaves over put right: one that is rounded
+        // otherwise than x / scale differs from it by 2^-24, before the rounding to 2^-4
+        const float inv = 1.f / scale;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = x[e] / scale;
+        for (int e = 0; e < 8; ++e) {
+            const float y = x[e] * inv;
+            x[e] = fmaf(fmaf(-y, scale, x[e]), inv, y);
+        }
         *reinterpret_cast<uint32_t *>(dst + t0) = pack_e4m3(x[0], x[1], x[2], x[3]);
         *reinterpret_cast<uint32_t *>(dst + t1) = pack_e4m3(x[4], x[5], x[6], x[7]);
         if (c == 0) (kind == 1 ? a.c.ks : a.c.vs)[scale_at(a.c, page, pos, head)] = scale;
