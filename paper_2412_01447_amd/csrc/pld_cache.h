@@ -117,7 +117,6 @@ __device__ __forceinline__ int64_t scale_at(const CacheView &c, int page, int64_
 }
 
 // Two fp32 values rounded to nearest (ties to even) as bf16, and four as e4m3.
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     const bf16x2_t v = {(__bf16)a, (__bf16)b};
     return __builtin_bit_cast(uint32_t, v);
@@ -125,11 +124,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
     int v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true);
-}
-__device__ __forceinline__ void unpack_e4m3(uint32_t v, float (&o)[4]) {
-    const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8((int)v, false);
-    const f32x2_t b = __builtin_amdgcn_cvt_pk_f32_fp8((int)v, true);
-    o[0] = a.x, o[1] = a.y, o[2] = b.x, o[3] = b.y;
 }
 
 // cap * tanh(x / cap) as 1 - 2 / (1 + e^(2|y|)), y = x / cap: its absolute error

@@ -1036,7 +1036,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_wide_kernel(
             wide_segment<D, kE4m3, 0>(a, lds, it, kv, u0, u1, tile0, R);
         else   // (or fewer, in an item of few rows)
             wide_segment<D, kE4m3, kMT - 1>(a, lds, it, kv, u0, u1, tile0, R);
-        if (u0 == 0 && u1 < it.units) {
+        if (u0 == 0 && u1 < it.units) {   // it ends in a later block
             const int64_t end = first + (int64_t)(kv + 1) * it.units;
             opened = Opened{e, kv, rg.block_of(end - 1), it.pos0, it.rows, it.b, it.r0, 0};
         }
@@ -1046,8 +1046,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_wide_kernel(
 
 // D / 4 lanes per row of an item that spans blocks, which is found by the block that opens it:
 // the parts' rows, weighed by their maxima, added up in order.  Up to eight parts are asked for
-// together, and ahead of the eight before being used.  5 to 14 us, by the latency of two
-// dependent loads; 25 us for 512 items of 136 rows, by the 72 MB of their parts.
+// together, and ahead of the eight before being used.  4 to 12 us, by the latency of two
+// dependent loads; 18 us for 512 items of 136 rows, by the 72 MB of their parts.
 template <int D>
 __global__ __launch_bounds__(256) void cache_attn_join_kernel(AttnArgs a, int R) {
     constexpr int L = D / 4, kParts = 8;
@@ -1387,6 +1387,7 @@ static int prep_attn(const pld_cache *cache, bool needs_v, const uint16_t *q, in
     a.scale = scale, a.cap = softcap;
     a.cap2 = softcap * kLog2E;
     a.inv2_log2e = softcap > 0.f ? 2.f / softcap : 0.f;   // 2 log2(e) / (cap log2(e))
+    if (!isfinite(scale * kLog2E) || !isfinite(a.cap2) || !isfinite(a.inv2_log2e)) return PLD_ERR_INVALID;
     a.G = Hq / cache->heads;
     a.page16 = (uint32_t)(a.c.page / 16), a.slot16 = (uint32_t)(a.c.slot / 16);
     a.spage32 = (uint32_t)a.c.spage;

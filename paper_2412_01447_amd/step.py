@@ -358,7 +358,8 @@ class DraftStep:
         except where "find" (past 16384 tokens), the one-call "draft" past its team and
         prompt lookup's "draft" past one launch take several: the same work as run(),
         with every argument marshalled once so that issuing a step costs only the
-        launches.  After set_logprobs the last entry is the emitted tokens' log probabilities.
+        launches.  After set_logprobs the last entry, of two kernels, is the emitted tokens' log
+        probabilities.
         commit=(limit, stats) adds the commit of the generation loop (with greedy
         verification, fused into the acceptance's launch: pld_accept_commit)."""
         P = dict(stream=stream, prepare=True)

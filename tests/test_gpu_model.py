@@ -208,6 +208,63 @@ def test_prompt_chunk(G, D, window, dtype):
     assert not torch.isnan(out.float()).any()
 
 
+@pytest.mark.parametrize("Hq,heads", [(4096, 1), (1024, 1024), (4096, 512)])
+def test_most_heads(Hq, heads):
+    """The most query heads a key head, and the most key heads, through all of the cache's calls."""
+    lens, n, D = [19, 40], 2, 64
+    c = Case(lens, n, Hq, heads, D, 16, draft_len=[1, 0], seed=Hq + heads)
+    k, v = normal(c.rng, 2, n, heads, D), normal(c.rng, 2, n, heads, D)
+    q = torch.zeros_like(c.q)
+    pld.pld_cache_write(c.q, k, v, c.k, c.v, c.t, c.d_lens, q, draft_len=c.d_dl)
+    for b, cnt in ((0, 2), (1, 1)):
+        assert np.array_equal(bits(q[b, :cnt]), bits(c.q[b, :cnt])) and not q[b, cnt:].any()
+        for i in range(cnt):
+            p = lens[b] - 1 + i
+            at = int(c.table[b, p // 16]), p % 16
+            assert np.array_equal(bits(c.k[at]), bits(k[b, i])) and np.array_equal(bits(c.v[at]), bits(v[b, i]))
+    out, L = c.attend()
+    c.check_attend(out, L, rows={(0, 1), (1, 0)})
+    chosen = [Hq - 1, 0, Hq // 2, Hq - 1, Hq // 3]
+    attn = torch.full((2, 5, 41), 7.0, device=dev())
+    pld.pld_cache_attn_rows(c.q, c.k, c.t, c.d_lens, d_i32([1, 0]), d_i32(chosen), L, attn)
+    a, lse = f64(attn), f64(L)
+    for b, i in ((0, 1), (1, 0)):
+        p = lens[b] - 1 + i
+        assert (a[b, :, p + 1:] == 7).all()
+        for r, h in enumerate(chosen):
+            kk = ref.cache_rows(c.k, None, c.table, b, h // (Hq // heads), p + 1)
+            x = kk @ f64(c.q[b, i, h]) / 8
+            tol = (D + 8) * U * (np.abs(kk) @ np.abs(f64(c.q[b, i, h]))).max() / 8
+            w = np.exp(x - lse[b, i, h])
+            bound = np.expm1(2 * tol + 16 * U * (1 + abs(lse[b, i, h]) + np.abs(x - lse[b, i, h]))) * w + 2.0 ** -126
+            assert (np.abs(a[b, r, :p + 1] - w) <= bound).all(), (b, r)
+
+
+def test_shared_pages():
+    """Sequences that share their first pages, one of them with a page twice, read the same rows."""
+    c = Case([64, 64, 50], 1, 8, 2, 64, 16, seed=9)
+    c.table[1, :3] = c.table[0, :3]
+    c.table[2, :3] = c.table[0, 0]
+    c.t = d_i32(c.table)
+    out, L = c.attend()
+    c.check_attend(out, L)
+
+
+def test_nothing_to_do():
+    """No sequence has a row: nothing is written, and the workspace serves the next call."""
+    c = Case([5, 0, 9], 2, 8, 2, 64, 16, draft_len=[-1, 1, 2], seed=9)
+    out, L = c.attend()
+    assert (out == 7).all() and (L == 7).all()
+    attn = torch.full((3, 1, 12), 7.0, device=dev())
+    pld.pld_cache_attn_rows(c.q, c.k, c.t, c.d_lens, d_i32([-1, 0, 2]), d_i32([0]), L, attn)
+    assert (attn == 7).all()
+    z, lp = torch.zeros(3, 2, 100, device=dev()), torch.full((3, 2), 7.0, device=dev())
+    ids, tl = torch.full((3, 2, 4), -7, dtype=torch.int32, device=dev()), torch.full((3, 2, 4), 7.0, device=dev())
+    ws = torch.zeros(pld.pld_token_logprobs_workspace_bytes(3, 2, 100, pld.PLD_F32, 4), dtype=torch.uint8, device=dev())
+    pld.pld_token_logprobs(z, d_i32(np.zeros((3, 2))), lp, ws, count=d_i32([0, -1, 3]), top_ids=ids, top_logprobs=tl)
+    assert (lp == 7).all() and (ids == -7).all() and (tl == 7).all()
+
+
 def test_attend_spread_scores():
     """Scores thousands apart (one key takes all), equal keys, and a head of zeros."""
     c = Case([300, 40], 2, 8, 2, 128, 16, seed=3, gain=60.0)
@@ -898,3 +955,42 @@ def test_two_graphs_share_a_workspace():
             if turn % 2:
                 torch.cuda.synchronize()
             assert all(np.array_equal(bits(t), w) for t, w in zip(outs, want)), turn
+
+
+@pytest.mark.parametrize("sample", [False, True])
+def test_plans_and_verification_give_log_probabilities(sample):
+    """After set_logprobs, verify() and a prepared plan both leave the emitted tokens' log
+    probabilities, those of pld_token_logprobs alone; without it they leave none."""
+    B, K, V, T = 3, 4, 1000, 200
+    rng = np.random.default_rng(2)
+    tokens, lens = d_i32(rng.integers(0, 30, (B, T + K + 1))), d_i32([T, 150, 90])
+    attn = torch.from_numpy(rng.random((B, 2, T + K + 1), dtype=np.float32)).to(dev())
+    z = torch.from_numpy(rng.standard_normal((B, K + 1, V), dtype=np.float32) * 3).to(dev())
+    step = DraftStep(B, T + K + 1, K, mode="fused")
+    if sample:
+        step.set_sampling(0.7, V, False, torch.from_numpy(rng.random((B, K + 1), dtype=np.float32)).to(dev()))
+    step.set_logprobs(V, bf16=False, top=5, temperature=0.7)
+    step.logprob.fill_(7.0)
+    step.make_draft(tokens, lens, attn=attn)
+    step.verify(z)
+    want = torch.full_like(step.logprob, 7.0)
+    ent, ids = torch.zeros_like(want), torch.zeros_like(step.top_ids)
+    tl = torch.zeros_like(step.top_logprobs)
+    pld.pld_token_logprobs(z, step.out_tokens, want, step.logprob_ws, count=step.out_count, temperature=0.7, entropy=ent,
+                           top_ids=ids, top_logprobs=tl)
+    assert np.array_equal(bits(step.logprob), bits(want))
+    for b in range(B):
+        m = int(step.out_count[b])
+        assert m >= 1 and not (step.logprob[b, :m] == 7).any() and (step.logprob[b, m:] == 7).all()
+        assert np.array_equal(bits(step.top_ids[b, :m]), bits(ids[b, :m]))
+        assert np.array_equal(bits(step.logprob_entropy[b, :m]), bits(ent[b, :m]))
+        assert np.array_equal(bits(step.top_logprobs[b, :m]), bits(tl[b, :m]))
+    ops = step.plan(tokens, lens, z, attn=attn)
+    assert [name for name, _ in ops][-1] == "token_logprobs"
+    step.logprob.fill_(7.0)
+    for _, op in ops:
+        op()
+    assert np.array_equal(bits(step.logprob), bits(want))
+    step.set_logprobs(None, False)
+    assert "token_logprobs" not in [name for name, _ in step.plan(tokens, lens, z, attn=attn)]
+    step.verify(z)

@@ -165,6 +165,9 @@ def test_limits():
             assert fn(_cache(**kw), *args.values()) == 2, kw
     n_keys = 2 ** 31 - 65536
     assert lib.pld_cache_attn_rows(_cache(), *{**ROWS, "keys": n_keys, "as_": 3 * n_keys, "ar": n_keys}.values()) == 1
+    for bad in (dict(scale=3e38), dict(cap=3e38), dict(cap=1e-44)):
+        for fn, args in calls[1:]:
+            assert fn(_cache(), *{**args, **bad}.values()) == 1, bad
     same = P(0x8000)
     assert lib.pld_cache_attn(_cache(), *{**ATTN, "q": same, "out": same}.values()) == 1
     for other in (dict(os=520), dict(orow=264, os=600)):
