@@ -90,7 +90,7 @@ struct Item {
 
 __device__ __forceinline__ Item make_item(const AttnArgs &a, int e, int R, int cnt, int pos0) {
     Item it;
-    it.b = e / a.groups;
+    it.b = a.groups == 1 ? e : e / a.groups;
     it.cnt = cnt;
     it.pos0 = pos0;
     it.r0 = (e - it.b * a.groups) * R;
@@ -109,7 +109,7 @@ __device__ __forceinline__ Item make_item(const AttnArgs &a, int e, int R, int c
 
 __device__ __forceinline__ Item item_of(const AttnArgs &a, int e, int R) {
     int pos0;
-    const int cnt = row_count(a.r, e / a.groups, pos0);
+    const int cnt = row_count(a.r, a.groups == 1 ? e : e / a.groups, pos0);
     return make_item(a, e, R, cnt, pos0);
 }
 
@@ -140,14 +140,13 @@ __device__ __forceinline__ Range block_range(const AttnArgs &a, int R, int64_t *
     const int entries = a.r.B * a.groups, per = (entries + 255) / 256;
     const int e0 = min((int)threadIdx.x * per, entries), e1 = min(e0 + per, entries);
     int64_t mine = 0;
-    for (int e = e0; e < e1; ++e) mine += item_of(a, e, R).units;
-    mine *= a.c.heads;
-    int64_t before = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        const int64_t x = __shfl_up(before, o);
-        if (lane >= o) before += x;
+    Item it;   // of the thread's last entry
+    for (int e = e0; e < e1; ++e) {
+        it = item_of(a, e, R);
+        mine += it.units;
     }
+    mine *= a.c.heads;
+    int64_t before = wave_incl_scan(mine);
     if (lane == 63) s_w[wave] = before;
     __syncthreads();
     Range r;
@@ -166,7 +165,7 @@ __device__ __forceinline__ Range block_range(const AttnArgs &a, int R, int64_t *
     if (before <= r.x0 && r.x0 < before + mine) {
         // the thread whose entries hold x0 steps to the one that does
         int e = e0;
-        Item it = item_of(a, e, R);
+        if (per > 1) it = item_of(a, e, R);
         for (int64_t u; r.x0 >= before + (u = (int64_t)it.units * a.c.heads); it = item_of(a, ++e, R)) before += u;
         s_e[0] = e;
         s_e[1] = it.cnt;
@@ -396,7 +395,7 @@ __device__ __forceinline__ bf16x8_t value_operand(const uint32_t (&vp)[8][N][W],
 // HBM where there is much to read: 64 sequences of 8192, a row of 32 query heads over 8 key
 // heads of 128 in bf16 (2.15 GB): 345 us, 6.2 TB/s; in e4m3 64 of 16384: 391 us.  By the way
 // of one dependent load to the next (lengths, page entries, keys, partial results) where there
-// is little: 10.4 us for one row over 1024 tokens, both launches.
+// is little: 9.9 us for one row over 1024 tokens, both launches.
 template <int D, bool kE4m3, int kMT>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnArgs a) {
     constexpr int R = 16 * kMT;
@@ -1123,7 +1122,7 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(AttnArgs a, int R)
 // (sequence, used key head) pairs are dealt to the blocks as in the attention; a block's
 // four waves have 32 of a unit's keys each.  Bound by memory, keys read and weights written:
 // 40 heads of 32 sequences of up to 8192 tokens (507 MB): 110 to 117 us, 4.3 to 4.6 TB/s; 8 heads
-// of one of 1024: 6.7 us.
+// of one of 1024: 6.5 us.
 constexpr int kRowsBlocks = 1024;   // four per CU
 
 template <int D, bool kE4m3>
@@ -1175,12 +1174,7 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void cache_attn_rows_kernel(
         if (lane == 0) s_cnt[0] = n;
     }
     // the waves' sums go through LDS at the same barrier
-    int64_t before = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        const int64_t x = __shfl_up(before, o);
-        if (lane >= o) before += x;
-    }
+    int64_t before = wave_incl_scan(mine);
     if (lane == 63) s_w[wave] = before;
     __syncthreads();
     const int used = uniform(s_cnt[0]), heads = used + unknown;

@@ -248,6 +248,21 @@ __device__ __forceinline__ int wave_excl_scan(int v, int &total) {
     return x - v;
 }
 
+// Inclusive prefix sum of counts (not negative) over the lanes, where they are small with the
+// lane moves above, some 0.5 us faster than 64-bit shuffles.
+__device__ __forceinline__ int64_t wave_incl_scan(int64_t v) {
+    if (__ballot((v >> 24) != 0) == 0) {
+        int total;
+        return wave_excl_scan((int)v, total) + v;
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const int64_t x = __shfl_up(v, o);
+        if (lane_id() >= o) v += x;
+    }
+    return v;
+}
+
 __device__ __forceinline__ uint64_t lanemask_lt() {
     int l = lane_id();
     return l == 0 ? 0ull : (~0ull >> (64 - l));

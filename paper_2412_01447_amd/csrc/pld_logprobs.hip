@@ -168,12 +168,7 @@ __global__ __launch_bounds__(kLogWaves * 64, 4) void token_logprobs_kernel(Logpr
     const int per = (a.B + 255) / 256, b0 = min((int)threadIdx.x * per, a.B), b1 = min(b0 + per, a.B);
     int64_t mine = 0;
     for (int b = b0; b < b1; ++b) mine += rows_of(a, b);
-    int64_t before = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        const int64_t x = __shfl_up(before, o);
-        if (lane >= o) before += x;
-    }
+    int64_t before = wave_incl_scan(mine);
     if (lane == 63) s_w[wave] = before;
     __syncthreads();
     int64_t rows = 0;
