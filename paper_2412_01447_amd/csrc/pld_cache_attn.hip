@@ -261,13 +261,13 @@ struct KeyRows {
     __device__ __forceinline__ static int row() { return lane_id() / kLanes; }
     __device__ __forceinline__ static int piece() { return lane_id() % kLanes; }
     // off: row() slot + 16 piece(); at(t): tile t's address
-    template <class At>
+    template <int kAux, class At>
     __device__ __forceinline__ void load(uint32_t off, uint32_t slot, At at) {
         __amdgpu_buffer_rsrc_t buf;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             if (i * kRows % 16 == 0) buf = buffer_at(at(i * kRows / 16));
-            r[i] = buffer_load16<kOnce<D, kE4m3>>(buf, off, i * kRows % 16 * slot);
+            r[i] = buffer_load16<kAux>(buf, off, i * kRows % 16 * slot);
         }
     }
     __device__ __forceinline__ static int unit(int key, int piece) { return 16 * piece + ((key ^ piece) & 15); }
@@ -465,7 +465,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
         const uint32_t slot = (uint32_t)a.c.slot;
         const uint32_t k_off = (uint32_t)Keys::row() * slot + 16 * Keys::piece(), v_off = 4 * (uint32_t)g * slot + c * (4 * VW);
         auto load_k = [&](const Tiles &tl) {
-            kr.load(k_off, slot, [&](int t) { return kh + tl.row(t); });
+            kr.template load<kOnce<D, kE4m3>>(k_off, slot, [&](int t) { return kh + tl.row(t); });
             if constexpr (kE4m3)
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
@@ -1125,7 +1125,10 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(AttnArgs a, int R)
 // of one of 1024: 6.5 us.
 constexpr int kRowsBlocks = 1024;   // four per CU
 
-template <int D, bool kE4m3>
+// kAux as above where a key head has at most 16 rows; where it has more, its keys are read
+// again for each 16 (128 rows a key head, 32 sequences of 8192: 166 us past the caches, 112
+// through them; 24 rows of 8 key heads, 16 sequences: 61 and 68).
+template <int D, bool kE4m3, int kAux>
 __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void cache_attn_rows_kernel(AttnArgs a) {
     constexpr int S = D / 32;
     using Keys = KeyRows<D, kE4m3, 2>;
@@ -1261,7 +1264,7 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void cache_attn_rows_kernel(
                 Keys kr;
                 f32x4_t kf[2];
                 auto load_k = [&](const Tiles &tl) {
-                    kr.load(k_off, slot, [&](int t) { return kh + tl.row(t); });
+                    kr.template load<kAux>(k_off, slot, [&](int t) { return kh + tl.row(t); });
                     if constexpr (kE4m3)
 #pragma unroll
                         for (int t = 0; t < 2; ++t)
@@ -1460,12 +1463,21 @@ extern "C" int pld_cache_attn_rows(const pld_cache *cache, const uint16_t *q,
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, a);
     };
-    const bool q8 = cache->dtype == PLD_E4M3;
+    const bool q8 = cache->dtype == PLD_E4M3, once = a.G <= 16 || R <= 16;
+    auto pick = [&](auto d) {
+        constexpr int D = decltype(d)::value;
+        if (q8)
+            kOnce<D, true> && once ? go(cache_attn_rows_kernel<D, true, kOnce<D, true>>)
+                                   : go(cache_attn_rows_kernel<D, true, 0>);
+        else
+            once ? go(cache_attn_rows_kernel<D, false, kOnce<D, false>>)
+                 : go(cache_attn_rows_kernel<D, false, 0>);
+    };
     if (cache->head_dim == 64)
-        q8 ? go(cache_attn_rows_kernel<64, true>) : go(cache_attn_rows_kernel<64, false>);
+        pick(std::integral_constant<int, 64>{});
     else if (cache->head_dim == 128)
-        q8 ? go(cache_attn_rows_kernel<128, true>) : go(cache_attn_rows_kernel<128, false>);
+        pick(std::integral_constant<int, 128>{});
     else
-        q8 ? go(cache_attn_rows_kernel<256, true>) : go(cache_attn_rows_kernel<256, false>);
+        pick(std::integral_constant<int, 256>{});
     return hipGetLastError() == hipSuccess ? PLD_OK : PLD_ERR_LAUNCH;
 }

@@ -523,6 +523,9 @@ ROWS = [
     ([90, 257], 4, 6, 1, 256, 64, "e4m3", 0, 50, [3, 0], [5, 1, 2, 0, 4], 0),
     ([500, 100], 2, 64, 1, 128, 16, "bf16", 0, 0, [1, 1], list(range(0, 64, 2)) + [1] * 9, 300),
     ([130], 2, 4, 4, 256, 128, "bf16", 20.0, 33, [0], [2, 4, -1, 1], 1),
+    ([70, 300], 2, 40, 2, 128, 16, "e4m3", 0, 0, [1, 0], list(range(40)), 0),      # 20 rows a key head
+    ([70], 3, 24, 1, 256, 32, "bf16", 0, 0, [2], list(range(24))[::-1], 0),
+    ([130], 1, 17, 1, 64, 16, "e4m3", 0, 60, [0], list(range(17)), 0),
     ([40, 7], 2, 6, 3, 64, 16, "bf16", 0, 0, [1, 0], [r * 5 % 8 - 1 for r in range(700)], 0),   # past the list in LDS
     (list(range(1, 301)), 2, 4, 2, 64, 16, "bf16", 0, 0, [b % 4 - 1 for b in range(300)], [3, 0], 0),
 ]
