@@ -40,7 +40,7 @@ template <int P>
 constexpr int kLogLoads = kLogElems / P;
 constexpr int kLogBlocks = 1024, kLogWaves = 4;   // 16 waves a CU
 constexpr int kKeys = 256;                        // keys a wave keeps at most before it sorts them out
-constexpr int kGroups = 128;                      // (segment, lane) groups of elements to look at
+constexpr int kGroups = 256;                      // (segment, lane) groups of elements to look at
 
 // A mass is 2^x with x = z k - c for a c near the largest z k: one fused multiply-add whose
 // only error is x's own rounding, whatever c is.  s sums 2^x, t sums 2^x x (the entropy is
@@ -134,14 +134,18 @@ struct Best {
             for (int e = 0; e < kEach; ++e) append(key(e), (mask >> e) & 1);
         }
     }
-    // The N-th best of the lanes' own best values (`own`, as ord_f32 has them; 0: none) is a
-    // floor of the values.  Of a bf16 value the upper half of ord_f32 says all.
-    template <bool kBf16>
-    __device__ __forceinline__ void raise_floor(uint32_t own) {
+    // The N-th best of the lanes' own best values (`own`, kOwn a lane, as ord_f32 has them; 0:
+    // none) is a floor of the values.  Of a bf16 value the upper half of ord_f32 says all.
+    template <bool kBf16, int kOwn>
+    __device__ __forceinline__ void raise_floor(const uint32_t (&own)[kOwn]) {
         uint32_t v = 0;
-        for (uint32_t bit = 1u << 31; bit > (kBf16 ? 0x8000u : 0u); bit >>= 1)
-            if (__popcll(__ballot(own >= (v | bit))) >= N) v |= bit;
-        if (v == 0) return;   // fewer than N lanes have one
+        for (uint32_t bit = 1u << 31; bit > (kBf16 ? 0x8000u : 0u); bit >>= 1) {
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) n += __popcll(__ballot(own[i] >= (v | bit)));
+            if (n >= N) v |= bit;
+        }
+        if (v == 0) return;   // there are fewer than N
         if (kBf16 && !(v >> 31)) v |= 0xffffu;
         floor = max(floor, (uint64_t)v << 32);
         at = fmaxf(at, unord_f32(v));
@@ -294,15 +298,21 @@ __global__ __launch_bounds__(kLogWaves * 64) void token_logprobs_finish_kernel(L
 #pragma unroll
         for (int q = 0; q < kChunk; ++q) mv[q] = maxima[min(v0 + q * kWave + lane, vecs - 1)];
     };
-    // Each lane's largest of the maxima; the top-th largest of those is a floor.
-    float own = -INFINITY;
+    // Each lane's largest of the maxima, of each fourth element; the top-th largest of the lanes',
+    // or for many alternatives of all 256, is a floor.
+    float own[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
     if constexpr (kTop) {
         for (int v0 = 0; v0 < vecs; v0 += kChunk * kWave) {
             load(v0);
             // (no other lane's vector in place of an absent one: the floor counts lanes)
 #pragma unroll
-            for (int q = 0; q < kChunk; ++q)
-                if (v0 + q * kWave + lane < vecs) own = fmaxf(own, E::vmax(mv[q]));
+            for (int q = 0; q < kChunk; ++q) {
+                float y[P];
+                E::unpack(mv[q], y);
+                if (v0 + q * kWave + lane < vecs)
+#pragma unroll
+                    for (int e = 0; e < P; ++e) own[e % 4] = fmaxf(own[e % 4], y[e]);
+            }
         }
     }
     if (i >= cnt) return;
@@ -322,7 +332,18 @@ __global__ __launch_bounds__(kLogWaves * 64) void token_logprobs_finish_kernel(L
 
     Best best{s_keys[kTop ? wave : 0], s_keys[kTop ? wave : 0] + (kTop ? kKeys : 0), a.top};
     if constexpr (kTop) {
-        best.raise_floor<kBf16>(lane < vecs ? ord_f32(own) : 0);
+        // (of 64 values the 64th best is so low that some 260 groups of a row reach it, of 256 some 80:
+        // one row of 160000 in fp32 with 64 alternatives takes 22 us by them and took 65)
+        if (a.top > 32) {
+            uint32_t four[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) four[i] = lane < vecs ? ord_f32(own[i]) : 0;
+            best.raise_floor<kBf16>(four);
+        } else {
+            const float most = fmaxf(fmaxf(own[0], own[1]), fmaxf(own[2], own[3]));
+            const uint32_t one[1] = {lane < vecs ? ord_f32(most) : 0};
+            best.raise_floor<kBf16>(one);
+        }
 
         // The groups of a list of (segment, lane), L lanes each: a vector a lane.
         int *groups = s_groups[wave];
@@ -374,25 +395,26 @@ __global__ __launch_bounds__(kLogWaves * 64) void token_logprobs_finish_kernel(L
             asm volatile("" ::: "memory");
         };
         // All of the row's groups from the floor on at once, where they are few.
-        bool done = false;
-        if (vecs <= kChunk * kWave) {
+        bool done = true;
+        for (int v0 = 0; v0 < vecs && done; v0 += kChunk * kWave) {
+            if (vecs > kChunk * kWave) load(v0);   // (else they are still there)
             uint64_t mask = 0;
 #pragma unroll
             for (int q = 0; q < kChunk; ++q) {
                 float y[P];
                 E::unpack(mv[q], y);
 #pragma unroll
-                for (int e = 0; e < P; ++e) mask |= (uint64_t)(q * kWave + lane < vecs && y[e] >= best.at) << (q * P + e);
+                for (int e = 0; e < P; ++e)
+                    mask |= (uint64_t)(v0 + q * kWave + lane < vecs && y[e] >= best.at) << (q * P + e);
             }
-            int to = wave_excl_scan(__popcll(mask), listed);
-            done = listed <= kGroups;
+            int more, to = listed + wave_excl_scan(__popcll(mask), more);
+            done = listed + more <= kGroups;
+            listed = done ? listed + more : 0;
             if (done)
                 for (; mask; mask &= mask - 1) {
                     const int bit = __ffsll((unsigned long long)mask) - 1;
-                    groups[to++] = (bit / P * kWave + lane) * P + bit % P;
+                    groups[to++] = (v0 + bit / P * kWave + lane) * P + bit % P;
                 }
-            else
-                listed = 0;
         }
         // Else in order of the vectors, that is of the segments: once there are `top` keys, an
         // equal value of a later segment loses to them, and only larger ones are of interest.

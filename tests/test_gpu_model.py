@@ -604,6 +604,10 @@ LOGPROBS = [
     (1, 2, 200003, "f32", 1.0, 64, "ties"),        # a row's maxima in several rounds
     (2, 3, 140001, "bf16", 1.5, 64, "masked"),
     (1, 2, 262144, "bf16", 1.0, 40, "equal"),
+    (1, 2, 160001, "f32", 1.0, 64, "normal"),
+    (2, 2, 128256, "bf16", 1.0, 64, "normal"),
+    (1, 2, 100000, "f32", 1.0, 33, "block"),       # most of the best side by side
+    (1, 2, 100000, "f32", 1.0, 64, "sorted1"),
     (700, 2, 129, "bf16", 1.0, 3, "normal"),       # more sequences than threads of a block
 ]
 
@@ -630,6 +634,8 @@ def test_token_logprobs(B, n, V, dtype, tau, top, kind):
     elif kind == "sorted":
         z[0] = np.sort(z[0], -1)                   # the largest last
         z[1] = np.sort(z[1], -1)[:, ::-1]
+    elif kind == "sorted1":
+        z[0, 0], z[0, 1] = np.sort(z[0, 0]), np.sort(z[0, 1])[::-1]
     elif kind == "block":
         z[:, :, 1000:1600] += 20                   # all the large ones side by side
     Z = torch.from_numpy(z).to(torch.float32 if dtype == "f32" else torch.bfloat16).to(dev())
