@@ -19,22 +19,24 @@ struct LogprobArgs {
     int32_t *top_ids;
     float *top_lp;
     int segs;           // segments per row
-    int2 *parts;        // [B][n]: first and last wave of a row
+    int2 *parts;        // [B][n]: first and last wave of a row; (0, -1): one wave has it whole
     float4 *masses;     // [waves][2]: reference, mass, mass times exponent of a wave's part of a row
+    float4 *whole;      // [B][n]: the same of a row that one wave has whole
     void *maxima;       // [B][n][segs][64], the logits' type: each lane's largest value of a segment
 };
 
-// A segment of a row is 32 elements a lane, one wave's work at a time, in 16-byte vectors:
-// lane l has the vectors l, l + 64, ...  The segments of all rows that exist, in order, are
-// dealt to the waves in equal contiguous ranges.  A wave sums up the masses of its part of a
-// row (slot 0: a row that began before it, slot 1: one that begins in it) and, where
-// alternatives are asked for, keeps each lane's largest value of a segment: 1/32 of the
-// logits, which tell a second launch, a wave per row, where the row's best elements are.
-// (Kept by the first pass itself, the best twenty cost as much as the pass: 95 us, and 46
-// without them, for 64 x 17 rows of 128256 in bf16.)  Where 920 of these rows exist
-// (236 MB) the pass takes 47 us, 5.0 TB/s: the card's reads would take 33 us, and so would an
-// element's exponential and the six or seven other vector instructions.  The second launch
-// takes 11 us with 20 alternatives.
+// A segment of a row is 32 elements a lane, one wave's work at a time, in 16-byte vectors: lane
+// l has the vectors l, l + 64, ...  The segments of all rows that exist, in order, are dealt to
+// the waves in equal contiguous ranges.  A wave sums up the masses of its part of a row (slot
+// 0: a row that began before it, slot 1: one that begins in it and ends after it, at most one
+// each; rows that do both in it have a place of their own, since of those there are several to
+// a wave where there are more rows than waves) and, where alternatives are asked for, keeps
+// each lane's largest value of a segment: 1/32 of the logits, which tell a second launch, a
+// wave per row, where the row's best elements are. (Kept by the first pass itself, the best
+// twenty cost as much as the pass: 95 us, and 46 without them, for 64 x 17 rows of 128256 in
+// bf16.)  Where 920 of these rows exist (236 MB) the pass takes 47 us, 5.0 TB/s: the card's
+// reads would take 33 us, and so would an element's exponential and the six or seven other
+// vector instructions.  The second launch takes 11 us with 20 alternatives.
 constexpr int kLogElems = 32;
 template <int P>
 constexpr int kLogLoads = kLogElems / P;
@@ -261,8 +263,9 @@ __global__ __launch_bounds__(kLogWaves * 64, 4) void token_logprobs_kernel(Logpr
         x += g1 - g0;
         w.join_lanes();
         if (lane == 0) {
-            a.masses[(int64_t)id * 2 + (g0 == 0)] = make_float4(w.c, w.s, w.t, 0.f);
-            if (g0 == 0) a.parts[row] = make_int2(id, range_of(x + (a.segs - g1) - 1));
+            const bool begins = g0 == 0, whole = begins && g1 == a.segs;
+            (whole ? a.whole[row] : a.masses[(int64_t)id * 2 + begins]) = make_float4(w.c, w.s, w.t, 0.f);
+            if (begins) a.parts[row] = whole ? make_int2(0, -1) : make_int2(id, range_of(x + (a.segs - g1) - 1));
         }
         g = 0;
         if (x < x1 && ++i >= cnt) {
@@ -289,6 +292,7 @@ __global__ __launch_bounds__(kLogWaves * 64) void token_logprobs_finish_kernel(L
     const int64_t row = (int64_t)b * a.n + i;
     const int cnt = rows_of(a, b);
     const int2 part = a.parts[row];
+    const float4 whole = a.whole[row];
     const int tok = a.tokens[row];
     constexpr int kChunk = 8;   // vectors a lane: a bf16 row of up to 131072 at once
     const uint4 *maxima = reinterpret_cast<const uint4 *>(static_cast<const T *>(a.maxima) + row * a.segs * kWave);
@@ -319,6 +323,7 @@ __global__ __launch_bounds__(kLogWaves * 64) void token_logprobs_finish_kernel(L
     const RowView<T, P> rv = row_view<T, P>(a.logits, a.ls, a.lr, b, i, a.V);
     const float z_tok = E::get(rv.row, tok >= 0 && tok < a.V ? tok : 0);
     Mass w;
+    if (part.y < 0 && lane == 0) w.c = whole.x, w.s = whole.y, w.t = whole.z;
     for (int p = part.x + lane; p <= part.y; p += kWave) {
         const float4 v = a.masses[(int64_t)p * 2 + (p == part.x)];
         Mass o;
@@ -477,6 +482,7 @@ static int log_blocks(int B, int n, int segs) {
 static size_t log_masses_bytes(int B, int n, int segs) {
     return (size_t)log_blocks(B, n, segs) * kLogWaves * 2 * sizeof(float4);
 }
+static size_t log_whole_bytes(int B, int n) { return (size_t)B * n * sizeof(float4); }
 static size_t log_parts_bytes(int B, int n) { return align_up((size_t)B * n * sizeof(int2), 256); }
 
 }  // namespace pld
@@ -489,7 +495,7 @@ extern "C" size_t pld_token_logprobs_workspace_bytes(int B, int n, int V, int dt
         return 0;
     const int segs = log_segs(V);
     const size_t maxima = top ? (size_t)B * n * segs * kWave * (dtype == PLD_F32 ? 4 : 2) : 0;
-    return log_masses_bytes(B, n, segs) + log_parts_bytes(B, n) + maxima;
+    return log_masses_bytes(B, n, segs) + log_whole_bytes(B, n) + log_parts_bytes(B, n) + maxima;
 }
 
 extern "C" int pld_token_logprobs(const void *logits, int dtype, int64_t l_seq_stride,
@@ -517,6 +523,8 @@ extern "C" int pld_token_logprobs(const void *logits, int dtype, int64_t l_seq_s
     char *ws = static_cast<char *>(workspace);
     a.masses = reinterpret_cast<float4 *>(ws);
     ws += log_masses_bytes(B, n, a.segs);
+    a.whole = reinterpret_cast<float4 *>(ws);
+    ws += log_whole_bytes(B, n);
     a.parts = reinterpret_cast<int2 *>(ws);
     a.maxima = ws + log_parts_bytes(B, n);
     const dim3 block(kLogWaves * 64), grid((unsigned)log_blocks(B, n, a.segs));
