@@ -190,7 +190,8 @@ int pld_cache_attn_rows(const pld_cache *cache, const uint16_t *q, int64_t q_seq
  *   logits, dtype, l_seq_stride, l_row_stride, V   as pld_verify_greedy, with n rows
  *   tokens      int32 [B][n];  count int32 [B] or NULL (n rows each); a count
  *               outside [0, n] counts as 0
- *   temperature finite, > 0
+ *   temperature finite, > 0 (from 2^-127 on: log2(e) / temperature is taken in fp32).  Rows
+ *               whose largest |z / temperature| is past 2^23 take longer: they are read again
  *   logprob     fp32 [B][n];  entropy fp32 [B][n] or NULL
  *   top         0 .. PLD_MAX_TOP;  top_ids int32 [B][n][top], top_logprobs fp32
  *               [B][n][top], both required when top > 0

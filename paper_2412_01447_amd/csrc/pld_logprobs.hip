@@ -44,11 +44,13 @@ constexpr int kLogBlocks = 1024, kLogWaves = 4;   // 16 waves a CU
 constexpr int kKeys = 256;                        // keys a wave keeps at most before it sorts them out
 constexpr int kGroups = 256;                      // (segment, lane) groups of elements to look at
 
-// A mass is 2^x with x = z k - c for a c near the largest z k: one fused multiply-add whose
-// only error is x's own rounding, whatever c is.  s sums 2^x, t sums 2^x x (the entropy is
+// A mass is 2^x with x = z k - c for c the largest z k, rounded: one fused multiply-add whose
+// only error is x's own rounding.  Up to |c| = 2^24 that c is rounded by at most 1/2, and all of
+// the row's x with it; past that x would leave the range of 2^x, and the row is summed up again
+// relative to its largest z, by the finishing launch.  s sums 2^x, t sums 2^x x (the entropy is
 // (log2 s - t / s) ln 2).  x is bounded so that -inf weighs nothing and 0 times x stays 0.
 // c = kNoMass: nothing but -inf so far.
-constexpr float kNoMass = -FLT_MAX;
+constexpr float kNoMass = -FLT_MAX, kMostReference = 0x1p24f;
 __device__ __forceinline__ float bounded(float x) { return fmaxf(x, -1e4f); }
 struct Mass {
     float c = kNoMass, s = 0.f, t = 0.f;
@@ -446,22 +448,35 @@ __global__ __launch_bounds__(kLogWaves * 64) void token_logprobs_finish_kernel(L
     }
 
     w.join_lanes();
-    // No mass: only -inf, or logits so low (a mask of the type's lowest value) that times k
-    // they overflow: then relative to their own maximum m.
+    // A reference past kMostReference: a small temperature, a row of -inf only, or of logits so
+    // low (a mask of the type's lowest value) that times k they overflow.  Then relative to the
+    // largest logit m, by this wave alone.
     bool none = false;
     float m = 0.f;
-    if (!(w.s > 0.f)) {
+    if (!(fabsf(w.c) <= kMostReference)) {
+        auto each = [&](auto f) {
+#pragma unroll 4
+            for (int v = lane; v < rv.nvec; v += kWave) {
+                float z[P];
+                E::unpack(rv.vec[v], z);
+#pragma unroll
+                for (int e = 0; e < P; ++e) f(z[e]);
+            }
+            if (lane < rv.head) f(E::get(rv.row, lane));
+            if (rv.body_end + lane < a.V) f(E::get(rv.row, rv.body_end + lane));
+        };
         m = -INFINITY;
-        for (int64_t v = lane; v < a.V; v += kWave) m = fmaxf(m, E::get(rv.row, v));
+        each([&](float z) { m = fmaxf(m, z); });
         m = wave_max_f32(m);
         none = !(m > -INFINITY);
         w = Mass{0.f, 0.f, 0.f};
-        for (int64_t v = lane; v < a.V && !none; v += kWave) w.add(E::get(rv.row, v) - m, a.k);
+        if (!none) each([&](float z) { w.add(z - m, a.k); });
         w.s = wave_sum_f32(w.s);
         w.t = wave_sum_f32(w.t);
     }
     const float log2_s = __builtin_amdgcn_logf(w.s);
-    auto logprob = [&](float x) { return none ? -INFINITY : (fmaf(x - m, a.k, -w.c) - log2_s) * 0.6931471805599453f; };
+    // (-inf times a k that is 0 in fp32, of a temperature past 2^149, would be NaN)
+    auto logprob = [&](float x) { return none || x == -INFINITY ? -INFINITY : (fmaf(x - m, a.k, -w.c) - log2_s) * 0.6931471805599453f; };
     if (lane == 0) {
         a.logprob[row] = tok >= 0 && tok < a.V ? logprob(z_tok) : __uint_as_float(0x7fc00000u);
         if (a.entropy) a.entropy[row] = none ? 0.f : fmaxf((log2_s - w.t / w.s) * 0.6931471805599453f, 0.f);

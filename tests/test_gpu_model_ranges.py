@@ -1,12 +1,14 @@
 """The model-side calls at the ends of the ranges that their arguments are documented for.
 References are plain, in 64 bits; bounds come from the arithmetic (see model_ref.py).
 """
+import numpy as np
 import pytest
 import torch
 
+import model_ref as ref
 import paper_2412_01447_amd as pld
-from gpu_helpers import dev, say
-from model_ref import U
+from gpu_helpers import d_i32, dev, say
+from model_ref import U, f64
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +58,33 @@ def test_more_rows_than_waves(B, n, V, dtype):
                 assert bool(((ent[b, i0:i1].double() - H).abs() <= (2 * add + 16 * U) * (1 + H)).all()), (b, i0)
                 assert torch.equal(ids[b, i0:i1].long(), order), (b, i0)
                 assert bool(close(tl[b, i0:i1].double(), want.gather(-1, order), V).all()), (b, i0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tau", [1e-5, 3e-7, 1e-7, 1e-8, 1e-9, 1e-20, 1e-30, 1e-38, 1e20, 1e40, 1e60, 1e300])
+def test_temperatures(tau, dtype):
+    """Logits that the temperature takes past what fp32 tells apart, or past its range, or to
+    nothing: one token takes all, or the equal ones do, or all that are not masked."""
+    rng = np.random.default_rng(3)
+    V, top = 5000, 8
+    z = rng.standard_normal((1, 8, V), dtype=np.float32) * 8
+    z[0, 1] -= 100                                    # a negative maximum
+    z[0, 2, [7, 2500, 4999]] = 50.0                   # a shared one
+    z[0, 3, rng.random(V) < 0.5] = -np.inf
+    z[0, 4] *= 1e30
+    z[0, 5] = -np.inf
+    z[0, 6] = np.where(rng.random(V) < 0.5, torch.finfo(torch.bfloat16).min, -1e4 + z[0, 6])
+    z[0, 7] = torch.finfo(torch.bfloat16).min
+    Z = torch.from_numpy(z).to(torch.float32 if dtype == "f32" else torch.bfloat16).to(dev())
+    zz = f64(Z)
+    tokens = np.array([[int(np.argmax(zz[0, 0])), 11, 2500, 1, int(np.argmax(zz[0, 4])), 3, 4, 4999]], np.int32)
+    tokens[0, 3] = int(np.nonzero(np.isinf(zz[0, 3]))[0][0])
+    lp, ent, ids, tl = (t.cpu().numpy() for t in logprobs(Z, d_i32(tokens), tau=tau, top=top))
+    add = (V / 64 + 96) * U
+    near = lambda x, y: x == y or abs(x - y) <= add + 8 * U * (abs(y) + 1) or (y < -1e37 and x < -1e37)
+    for i in range(8):
+        want, H, order = ref.logprob_row(zz[0, i], tau)
+        assert near(lp[0, i], want[tokens[0, i]]), (i, lp[0, i], want[tokens[0, i]])
+        assert abs(ent[0, i] - H) <= (2 * add + 16 * U) * (1 + H), (i, ent[0, i], H)
+        assert np.array_equal(ids[0, i], order[:top]), i
+        assert all(near(x, want[o]) for x, o in zip(tl[0, i], order)), (i, tl[0, i], want[order[:top]])
