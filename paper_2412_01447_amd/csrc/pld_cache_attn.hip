@@ -341,10 +341,27 @@ __device__ __forceinline__ float scale_scores(const AttnArgs &a, f32x4_t (&x)[2]
         c1 = 1.f;
     }
     if (a.cap > 0.f) {
+        float w = 0.f;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t) {
+            x[t] *= c1;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[t][r] = soft_cap(x[t][r] * c1, a.cap2, a.inv2_log2e);
+            for (int r = 0; r < 4; ++r) w = fmaxf(w, fabsf(x[t][r]));
+        }
+        // One branch for the wave: few scores come to a third of the cap as a rule (64 x 17 rows
+        // over 16384 tokens in e4m3, cap 50: 1051 us, 1300 with both forms for every score; where
+        // every wave has such a score, cap 8, 1450).
+        if (__any(w * a.inv2_log2e >= kCapNear)) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[t][r] = soft_cap(x[t][r], a.cap2, a.inv2_log2e);
+        } else {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[t][r] = soft_cap_near(x[t][r], a.inv2_log2e);
+        }
         c1 = 1.f;
     }
     return c1;

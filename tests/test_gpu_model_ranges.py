@@ -9,6 +9,7 @@ import model_ref as ref
 import paper_2412_01447_amd as pld
 from gpu_helpers import d_i32, dev, say
 from model_ref import U, f64
+from test_gpu_model import E4M3, Case
 
 pytestmark = pytest.mark.gpu
 
@@ -88,3 +89,42 @@ def test_temperatures(tau, dtype):
         assert abs(ent[0, i] - H) <= (2 * add + 16 * U) * (1 + H), (i, ent[0, i], H)
         assert np.array_equal(ids[0, i], order[:top]), i
         assert all(near(x, want[o]) for x, o in zip(tl[0, i], order)), (i, tl[0, i], want[order[:top]])
+
+
+# ------------------------------------------------------------------ capped scores
+def capped_row(q, k, v, pos, scale, cap):
+    """ref.attn_row without a window, its bound of a score's error for a cap that is taken with
+    a relative error: 20 u (the fp32 factor of the cap 2 u; from 0.26 of the cap on the
+    quotient's 16 u, below it the polynomial's few)."""
+    w, o, lse, _, spread = ref.attn_row(q, k, v, pos, scale, cap, 0)
+    x = k[:pos + 1] @ q * scale
+    size = np.abs(k[:pos + 1]) @ np.abs(q) * scale
+    return w, o, lse, (len(q) + 8) * U * size.max() + 20 * U * np.abs(cap * np.tanh(x / cap)).max(), spread
+
+
+@pytest.mark.parametrize("G,D,dtype", [(4, 128, "bf16"), (12, 64, "e4m3"), (4, 64, "e4m3"), (12, 128, "bf16"), (3, 256, "bf16")])
+@pytest.mark.parametrize("cap", [2.0 ** -20, 0.5, 8.0, 30.0, 1e4, 1e6, 1e8, 1e20, 2.0 ** 120, 2.0 ** 126])
+def test_caps(cap, G, D, dtype):
+    """Scores far below, around and far above the cap keep their digits, in the attention of few
+    and of many rows and in the chosen heads' weights."""
+    lens, n, heads = [150, 20], 5, 2
+    c = Case(lens, n, heads * G, heads, D, 16, E4M3 if dtype == "e4m3" else torch.bfloat16, seed=G + D)
+    out, L = c.attend(softcap=cap)
+    row, chosen = [4, 0], list(range(heads * G))
+    attn = torch.full((2, len(chosen), 160), 7.0, device=dev())
+    pld.pld_cache_attn_rows(c.q, c.k, c.t, c.d_lens, d_i32(row), d_i32(chosen), L, attn, k_scale=c.ks, softcap=cap)
+    out, lse, a = f64(out), f64(L), f64(attn)
+    for b in range(2):
+        for h in range(heads * G):
+            k = ref.cache_rows(c.k, c.ks, c.table, b, h // G, lens[b] - 1 + n)
+            v = ref.cache_rows(c.v, c.vs, c.table, b, h // G, lens[b] - 1 + n)
+            for i in range(n):
+                pos = lens[b] - 1 + i
+                w, o, s, tol, spread = capped_row(f64(c.q[b, i, h]), k[:pos + 1], v[:pos + 1], pos, D ** -0.5, cap)
+                assert abs(lse[b, i, h] - s) <= ref.lse_bound(tol, s, pos + 1), (b, i, h, lse[b, i, h], s)
+                assert (np.abs(out[b, i, h] - o) <= ref.out_bound(o, spread, tol)).all(), (b, i, h)
+                if i == row[b]:
+                    w = w * np.exp(s - lse[b, i, h])
+                    rel = np.expm1(2 * tol + 16 * U * (1 + abs(s) + np.abs(np.log(np.maximum(w, 1e-38)))))
+                    assert (np.abs(a[b, h, :pos + 1] - w) <= rel * w + 2.0 ** -126).all(), (b, h)
+                    assert (a[b, h, pos + 1:] == 7).all()
