@@ -126,7 +126,7 @@ int pld_cache_write(const pld_cache *cache, const uint16_t *q, int64_t q_seq_str
  *
  *   q           bf16, as pld_cache_write's q_out
  *   scale       > 0 (1 / sqrt(head_dim) as a rule);  softcap >= 0;  window >= 0
- *               (scale and softcap: at most 2^127, softcap 0 or at least 2^-125)
+ *               (scale at most 2^127; softcap 0 or from 2^-125 to 2^126)
  *   out         bf16, laid out like q with its own strides; not q
  *   lse         fp32 [B][n][Hq] or NULL
  *   workspace   pld_cache_attn_workspace_bytes(B, n, Hq, heads, head_dim) bytes,

@@ -1401,7 +1401,7 @@ static int prep_attn(const pld_cache *cache, bool needs_v, const uint16_t *q, in
     a.scale = scale, a.cap = softcap;
     a.cap2 = softcap * kLog2E;
     a.inv2_log2e = softcap > 0.f ? 2.f / softcap : 0.f;   // 2 log2(e) / (cap log2(e))
-    if (!isfinite(scale * kLog2E) || !isfinite(a.cap2) || !isfinite(a.inv2_log2e)) return PLD_ERR_INVALID;
+    if (!isfinite(scale * kLog2E) || !isfinite(2.f * a.cap2) || !isfinite(a.inv2_log2e)) return PLD_ERR_INVALID;
     a.G = Hq / cache->heads;
     a.page16 = (uint32_t)(a.c.page / 16), a.slot16 = (uint32_t)(a.c.slot / 16);
     a.spage32 = (uint32_t)a.c.spage;
