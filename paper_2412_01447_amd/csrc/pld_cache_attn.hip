@@ -842,7 +842,8 @@ __device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds,
                     vp[i][0][w] = vr[i][0][w];
             }
         uint32_t odd_keys = 0;
-        if (!(k0 >= all_lo && k0 + kStep <= all_hi)) {
+        const bool every_row = k0 >= all_lo && k0 + kStep <= all_hi;   // sees every key
+        if (!every_row) {
             // values that not every row sees (see mask_values above)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -872,9 +873,11 @@ __device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds,
         if constexpr (kE4m3) {
             if (wave == 0) sc *= c1;
             if (wave == 1) {
-                // a scale that is not finite, as with the values
-                const uint64_t ball = __ballot(!(fabsf(sc) < INFINITY));
-                if (!(fabsf(sc) < INFINITY)) sc = 0.f;
+                // a scale that is not finite, as with the values: where every row sees its key it
+                // stays, and every row's output is not finite either
+                const bool odd = !every_row && !(fabsf(sc) < INFINITY);
+                const uint64_t ball = __ballot(odd);
+                if (odd) sc = 0.f;
                 if (lane < 2) lds.odd[buf][lane][2] = (uint32_t)(ball >> (32 * lane));
             }
             if (wave < 2) reinterpret_cast<float *>(lds.scale[buf][wave])[lane] = sc;

@@ -1,6 +1,8 @@
 """The model-side calls at the ends of the ranges that their arguments are documented for.
 References are plain, in 64 bits; bounds come from the arithmetic (see model_ref.py).
 """
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -9,7 +11,7 @@ import model_ref as ref
 import paper_2412_01447_amd as pld
 from gpu_helpers import d_i32, dev, say
 from model_ref import U, f64
-from test_gpu_model import E4M3, Case
+from test_gpu_model import E4M3, Case, bits
 
 pytestmark = pytest.mark.gpu
 
@@ -128,3 +130,21 @@ def test_caps(cap, G, D, dtype):
                     rel = np.expm1(2 * tol + 16 * U * (1 + abs(s) + np.abs(np.log(np.maximum(w, 1e-38)))))
                     assert (np.abs(a[b, h, :pos + 1] - w) <= rel * w + 2.0 ** -126).all(), (b, h)
                     assert (a[b, h, pos + 1:] == 7).all()
+
+
+# ------------------------------------------------------------------ scales
+@pytest.mark.parametrize("G", [1, 4, 12])            # 5, 20 and 60 rows a key head
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("which,poison", [("k", math.nan), ("v", math.nan), ("v", math.inf)])
+def test_seen_scales_that_are_not_finite(which, poison, D, G):
+    """A key's or value's scale that is NaN, or a value's that is infinite, at an early key that
+    every row sees, reaches the output of every row of that key head, whatever their number, and
+    no other's.  (An infinite scale of a key makes scores of either infinity, of which the
+    negative one weighs nothing by its definition.)"""
+    c = Case([400, 130], 5, 2 * G, 2, D, 16, E4M3, seed=D + G)
+    clean, L = c.attend()
+    scale = c.ks if which == "k" else c.vs
+    scale[int(c.table[0, 2]), 1, 5] = poison
+    out, _ = c.attend()
+    assert np.array_equal(bits(out[1]), bits(clean[1])) and np.array_equal(bits(out[0, :, :G]), bits(clean[0, :, :G]))
+    assert not torch.isfinite(out[0, :, G:].float()).any(-1).any()
