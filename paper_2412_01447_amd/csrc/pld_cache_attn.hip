@@ -238,7 +238,7 @@ __device__ __forceinline__ Tiles take_tiles(const AttnArgs &a, const Item &it, i
     const bool ok = (uint32_t)entry < (uint32_t)a.c.num_pages;
     const uint32_t page = ok ? entry : 0, mask = (1u << a.c.shift) - 1;
     const int j = k0 + (lane_id() & (16 * T - 1));
-    r.at = (uint64_t)page * a.page16 + ((uint32_t)j & mask & ~15u) * a.slot16;
+    r.at = (uint64_t)page * a.page16 + (uint64_t)((uint32_t)j & mask & ~15u) * a.slot16;
     if constexpr (kScales) r.scale = (int64_t)((uint64_t)page * a.spage32 + (((uint32_t)kv << a.c.shift) + ((uint32_t)j & mask)));
     r.bad = __ballot(!ok && j < it.hi);
     return r;

@@ -11,7 +11,7 @@ import model_ref as ref
 import paper_2412_01447_amd as pld
 from gpu_helpers import d_i32, dev, say
 from model_ref import U, f64
-from test_gpu_model import E4M3, Case, bits
+from test_gpu_model import E4M3, Case, bits, normal
 
 pytestmark = pytest.mark.gpu
 
@@ -148,3 +148,37 @@ def test_seen_scales_that_are_not_finite(which, poison, D, G):
     out, _ = c.attend()
     assert np.array_equal(bits(out[1]), bits(clean[1])) and np.array_equal(bits(out[0, :, :G]), bits(clean[0, :, :G]))
     assert not torch.isfinite(out[0, :, G:].float()).any(-1).any()
+
+
+# ------------------------------------------------------------------ wide strides
+@pytest.mark.parametrize("D,G", [(128, 4), (64, 12)])      # 20 and 60 rows a key head
+def test_slots_far_apart(D, G):
+    """A page whose slots are so far apart that it spans more than 2^32 times 16 bytes (a cache
+    that lies slot by slot): what the write puts there, the attention and the chosen heads'
+    weights read.  The same rows in a cache of ordinary strides give the same bits."""
+    page, heads, T, slot = 4096, 2, 4090, 9 << 20
+    size = (page - 1) * slot + 2 * heads * D
+    assert (page - 16) * (slot * 2 // 16) > 2 ** 32
+    if torch.cuda.mem_get_info()[0] < 2 * size + (4 << 30):
+        pytest.skip("too little memory is free")
+    near = Case([T], 5, heads * G, heads, D, page, seed=D)
+    flat = torch.empty(size, dtype=torch.bfloat16, device=dev())        # values beside keys
+    far = [flat.as_strided((1, page, heads, D), (page * slot, slot, D, 1), at) for at in (0, heads * D)]
+    for x, old in zip(far, (near.k, near.v)):
+        x[0].copy_(old[int(near.table[0, 0])])
+    table = torch.zeros((1, 1), dtype=torch.int32, device=dev())
+    k, v = normal(near.rng, 1, 5, heads, D), normal(near.rng, 1, 5, heads, D)
+    got = []
+    for kc, vc, t in ((near.k, near.v, near.t), (far[0], far[1], table)):
+        q, out, L = torch.empty_like(near.q), torch.zeros_like(near.q), torch.zeros((1, 5, heads * G), device=dev())
+        attn = torch.zeros((1, 3, page), device=dev())
+        ws = torch.zeros(pld.pld_cache_attn_workspace_bytes(1, 5, heads * G, heads, D), dtype=torch.uint8, device=dev())
+        pld.pld_cache_write(near.q, k, v, kc, vc, t, near.d_lens, q)
+        pld.pld_cache_attn(q, kc, vc, t, near.d_lens, out, ws, lse=L)
+        pld.pld_cache_attn_rows(q, kc, t, near.d_lens, d_i32([4]), d_i32([0, G, G + 1]), L, attn)
+        got.append([bits(x) for x in (q, out, L, attn)])
+    del flat, far, kc, vc, x
+    torch.cuda.empty_cache()
+    for a, b in zip(*got):
+        assert np.array_equal(a, b)
+    near.check_attend(out, L)
