@@ -131,7 +131,8 @@ int pld_cache_write(const pld_cache *cache, const uint16_t *q, int64_t q_seq_str
  *   lse         fp32 [B][n][Hq] or NULL
  *   workspace   pld_cache_attn_workspace_bytes(B, n, Hq, heads, head_dim) bytes,
  *               16-byte aligned, contents of no importance; calls that overlap in
- *               time must not share it
+ *               time must not share it (the size never falls as n grows: one for
+ *               the most rows serves fewer)
  * Device-side rules: keys that a row does not see do not affect it, whatever
  * their slots hold; a row one of whose keys lies on a bad page or past the table
  * gets NaN in out and lse.  Where a value that a row sees is not finite, that head

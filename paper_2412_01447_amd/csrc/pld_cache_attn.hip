@@ -1355,16 +1355,18 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void cache_attn_rows_kernel(
 struct AttnShape {
     int tiles, groups;
 };
+static int most_tiles(int D) { return D == 256 ? 8 : 11; }
+static int64_t all_tiles(int n, int G) { return ((int64_t)n * G + 15) / 16; }
 static AttnShape attn_shape(int n, int G, int D) {
-    const int most = D == 256 ? 8 : 11;
-    const int64_t tiles = ((int64_t)n * G + 15) / 16;
+    const int most = most_tiles(D);
+    const int64_t tiles = all_tiles(n, G);
     AttnShape s;
     s.groups = (int)((tiles + most - 1) / most);
     s.tiles = (int)((tiles + s.groups - 1) / s.groups);
     return s;
 }
-static size_t partials_bytes(const AttnShape &s, int D) {
-    return align_up((size_t)kAttnBlocks * 2 * 16 * s.tiles * (D + 2) * sizeof(float), 256);
+static size_t partials_bytes(int tiles, int D) {
+    return align_up((size_t)kAttnBlocks * 2 * 16 * tiles * (D + 2) * sizeof(float), 256);
 }
 
 template <int D, bool kE4m3>
@@ -1421,8 +1423,10 @@ extern "C" size_t pld_cache_attn_workspace_bytes(int B, int n, int Hq, int heads
         Hq < 1 || Hq > 4096 || Hq % heads ||
         (head_dim != 64 && head_dim != 128 && head_dim != 256))
         return 0;
-    const AttnShape sh = attn_shape(n, Hq / heads, head_dim);
-    return partials_bytes(sh, head_dim) + kAttnBlocks * sizeof(Opened);
+    // (groups are even: with more rows than one group's an item may have fewer tiles than with
+    // less, and a workspace for many rows has to serve few)
+    const int64_t tiles = all_tiles(n, Hq / heads), most = most_tiles(head_dim);
+    return partials_bytes((int)(tiles < most ? tiles : most), head_dim) + kAttnBlocks * sizeof(Opened);
 }
 
 extern "C" int pld_cache_attn(const pld_cache *cache, const uint16_t *q, int64_t q_seq_stride,
@@ -1447,7 +1451,7 @@ extern "C" int pld_cache_attn(const pld_cache *cache, const uint16_t *q, int64_t
     a.lse = lse;
     a.groups = sh.groups;
     a.partials = static_cast<float *>(workspace);
-    a.opened = reinterpret_cast<Opened *>(static_cast<char *>(workspace) + partials_bytes(sh, D));
+    a.opened = reinterpret_cast<Opened *>(static_cast<char *>(workspace) + partials_bytes(sh.tiles, D));
     const bool q8 = cache->dtype == PLD_E4M3;
     const hipStream_t s = (hipStream_t)stream;
     if (D == 64)

@@ -1,5 +1,6 @@
 """Host checks of the model-side calls at the ends of their documented ranges (CPU only)."""
 import paper_2412_01447_amd as pld
+from paper_2412_01447_amd.cache import PagedCache
 from test_model_abi import ATTN, ROWS, _cache, no_gpu
 
 
@@ -11,3 +12,18 @@ def test_largest_cap():
     for fn, args in ((lib.pld_cache_attn, ATTN), (lib.pld_cache_attn_rows, ROWS)):
         assert fn(_cache(), *{**args, "cap": 1.5e38}.values()) == 1
     assert lib.pld_cache_attn(_cache(), *{**ATTN, "cap": 2.0 ** 126, "wsb": 0}.values()) == 3
+
+
+def test_workspace_of_the_most_rows_serves_fewer():
+    """The attention's workspace never falls as the rows of a sequence grow (the rows are split
+    into even groups, so that more rows can have smaller ones)."""
+    for D in (64, 128, 256):
+        for Hq, heads in ((1, 1), (8, 8), (8, 1), (40, 8), (12, 4), (56, 8), (16, 1), (96, 2), (4096, 1)):
+            sizes = [pld.pld_cache_attn_workspace_bytes(3, n, Hq, heads, D) for n in [*range(1, 400), 1000, 5000, 65535]]
+            assert sizes[0] > 0 and sizes == sorted(sizes), (D, Hq, heads)
+    cache = PagedCache(2, 100, 1, 64, page_size=16, device="cpu")
+    cache.reserve(22, 8)
+    ws = cache.workspace
+    for n in range(1, 22):
+        cache.reserve(n, 8)
+    assert cache.workspace is ws
