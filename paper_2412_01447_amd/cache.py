@@ -46,15 +46,20 @@ class PagedCache:
         return torch.zeros((num_pages, self.page_size, self.heads, self.head_dim), dtype=dtype,
                            device=device)
 
-    def reserve(self, n, Hq):
-        """The attention's workspace for n rows a sequence (grown by attend() as needed: a
+    def reserve(self, n, Hq, stream=None):
+        """The attention's workspace for up to n rows a sequence (grown by attend() as needed: a
         caller that captures a graph reserves before the capture).  One that is replaced is
-        kept: captured graphs and prepared calls go on using it."""
+        kept: captured graphs and prepared calls go on using it.  `stream`: the one that first
+        uses it, default the current one; memory that another stream's work may still be using
+        is not taken."""
         need = pld_cache_attn_workspace_bytes(self.B, n, Hq, self.heads, self.head_dim)
         if self.workspace is None or self.workspace.numel() < need:
             if self.workspace is not None:
                 self.grown.append(self.workspace)
-            self.workspace = torch.empty(need, dtype=torch.uint8, device=self.k.device)
+            if stream is not None and not hasattr(stream, "cuda_stream"):
+                stream = torch.cuda.ExternalStream(int(stream), device=self.k.device)
+            with torch.cuda.stream(stream):      # (None: the current one)
+                self.workspace = torch.empty(need, dtype=torch.uint8, device=self.k.device)
 
     def write(self, q, k, v, lens, q_out, draft_len=None, q_norm=None, k_norm=None, eps=1e-6,
               rope=None, rope_pairs=PLD_ROPE_HALVES, stream=None, prepare=False):
@@ -67,7 +72,7 @@ class PagedCache:
     def attend(self, q, lens, out, draft_len=None, lse=None, scale=None, softcap=0.0, window=0,
                stream=None, prepare=False):
         """The rows' attention over the cache."""
-        self.reserve(q.shape[1], q.shape[2])
+        self.reserve(q.shape[1], q.shape[2], stream)
         return pld_cache_attn(q, self.k, self.v, self.table, lens, out, self.workspace,
                               draft_len=draft_len, k_scale=self.k_scale, v_scale=self.v_scale,
                               lse=lse, scale=scale, softcap=softcap, window=window, stream=stream,

@@ -11,6 +11,7 @@ import model_ref as ref
 import paper_2412_01447_amd as pld
 from gpu_helpers import d_i32, dev, say
 from model_ref import U, f64
+from paper_2412_01447_amd.cache import PagedCache
 from test_gpu_model import E4M3, Case, bits, normal
 
 pytestmark = pytest.mark.gpu
@@ -182,3 +183,27 @@ def test_slots_far_apart(D, G):
     for a, b in zip(*got):
         assert np.array_equal(a, b)
     near.check_attend(out, L)
+
+
+# ------------------------------------------------------------------ another stream
+@pytest.mark.parametrize("handle", [False, True])
+def test_a_workspace_comes_from_the_stream_that_uses_it(handle, monkeypatch):
+    """attend() on another stream than the current one allocates its workspace under that
+    stream, not from memory that the current stream's earlier work may still be using."""
+    cache = PagedCache(1, 5000, 2, 64, page_size=16)
+    rng = np.random.default_rng(4)
+    for x in (cache.k, cache.v):
+        x.copy_(normal(rng, *x.shape))
+    q, lens = normal(rng, 1, 3, 8, 64), d_i32([4900])
+    want, out = torch.zeros_like(q), torch.zeros_like(q)
+    cache.attend(q, lens, want)
+    fresh = PagedCache(1, 5000, 2, 64, page_size=16)
+    fresh.k, fresh.v, fresh.table = cache.k, cache.v, cache.table
+    side, under, empty = torch.cuda.Stream(), [], torch.empty
+    torch.cuda.synchronize()
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: (under.append(torch.cuda.current_stream().cuda_stream), empty(*a, **k))[1])
+    fresh.attend(q, lens, out, stream=side.cuda_stream if handle else side)
+    monkeypatch.undo()
+    assert under == [side.cuda_stream] and torch.cuda.current_stream() != side
+    side.synchronize()
+    assert np.array_equal(bits(out), bits(want))
