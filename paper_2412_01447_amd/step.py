@@ -71,6 +71,7 @@ class DraftStep:
         self.logprob = None
         self.logprob_entropy = self.top_ids = self.top_logprobs = self.logprob_ws = None
         self.logprob_temperature = 1.0
+        self.replaced = []               # buffers that earlier plans and graphs point to
 
     def set_sampling(self, temperature, V, bf16, uniforms=None):
         """Verify by sampling at `temperature` (None: greedy again).  `uniforms` is a
@@ -95,8 +96,12 @@ class DraftStep:
         softmax(logits / temperature): self.logprob [B][K+1], self.logprob_entropy [B][K+1]
         and, for top > 0, the rows' most likely tokens self.top_ids and self.top_logprobs
         [B][K+1][top] (rows past out_count keep what they held).  V None: no longer.  The
-        buffers are new ones at each call: plans and graphs are made after it."""
+        buffers are new ones at each call: plans and graphs made before it go on writing to
+        the old ones, which are kept in self.replaced (a caller that has no such plan left may
+        clear it)."""
         if V is None:
+            if self.logprob is not None:
+                self.replaced.append(self.logprob)
             self.logprob = None
             return
         B, n = self.B, self.K + 1
@@ -104,6 +109,8 @@ class DraftStep:
         need = pld_token_logprobs_workspace_bytes(B, n, V, PLD_BF16 if bf16 else PLD_F32, top)
         if need == 0:
             raise ValueError(f"no log probabilities for V = {V}, top = {top}")
+        self.replaced += [t for t in (self.logprob_ws, self.logprob, self.logprob_entropy,
+                                      self.top_ids, self.top_logprobs) if t is not None]
         self.logprob_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
         self.logprob = torch.zeros((B, n), **f32)
         self.logprob_entropy = torch.zeros((B, n), **f32)

@@ -1,6 +1,10 @@
 """Host checks of the model-side calls at the ends of their documented ranges (CPU only)."""
+import gc
+import weakref
+
 import paper_2412_01447_amd as pld
 from paper_2412_01447_amd.cache import PagedCache
+from paper_2412_01447_amd.step import DraftStep
 from test_model_abi import ATTN, ROWS, _cache, no_gpu
 
 
@@ -27,3 +31,18 @@ def test_workspace_of_the_most_rows_serves_fewer():
     for n in range(1, 22):
         cache.reserve(n, 8)
     assert cache.workspace is ws
+
+
+def test_buffers_that_plans_point_to_are_kept():
+    """set_logprobs() replaces buffers; those that plans and graphs made before write to stay
+    allocated as long as the step does."""
+    step = DraftStep(2, 100, 4, device="cpu")
+    old = []
+    for top in (3, 0, 5):
+        step.set_logprobs(50, bf16=True, top=top)
+        old += [weakref.ref(t) for t in (step.logprob, step.logprob_entropy, step.logprob_ws, step.top_ids, step.top_logprobs)
+                if t is not None]
+    step.set_logprobs(None, bf16=True)
+    step.set_logprobs(20, bf16=True)
+    gc.collect()
+    assert len(old) == 13 and all(ref() is not None for ref in old)
