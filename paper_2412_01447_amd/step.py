@@ -77,12 +77,15 @@ class DraftStep:
         """Verify by sampling at `temperature` (None: greedy again).  `uniforms` is a
         device fp32 [B][K+1] tensor of draws the caller refreshes before each step
         (default: a buffer of zeros, self.uniforms, to be filled in place); the
-        workspace grows to what the sampling calls need for vocabulary V."""
+        workspace grows to what the sampling calls need for vocabulary V.  Buffers that it
+        replaces are kept in self.replaced, for plans and graphs made before."""
         if temperature is None:
             self.temperature = None
             return
         need = pld_verify_sample_workspace_bytes(self.B, self.K, V, PLD_BF16 if bf16 else PLD_F32)
+        self.replaced += [t for t in (self.uniforms, self.row_sample) if t is not None]
         if self.workspace.numel() < need:
+            self.replaced.append(self.workspace)
             self.workspace = torch.zeros(need, dtype=torch.uint8, device=self.device)
         if uniforms is None:
             uniforms = torch.zeros((self.B, self.K + 1), dtype=torch.float32, device=self.device)

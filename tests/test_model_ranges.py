@@ -46,3 +46,16 @@ def test_buffers_that_plans_point_to_are_kept():
     step.set_logprobs(20, bf16=True)
     gc.collect()
     assert len(old) == 13 and all(ref() is not None for ref in old)
+
+
+def test_buffers_that_sampling_replaces_are_kept():
+    """set_sampling() too."""
+    step = DraftStep(2, 100, 4, device="cpu")
+    old = [weakref.ref(step.workspace)]
+    for V in (1000, 200000):
+        step.set_sampling(0.7, V, bf16=False)
+        old += [weakref.ref(t) for t in (step.workspace, step.uniforms, step.row_sample)]
+    step.set_sampling(None, 0, False)
+    step.set_sampling(0.7, 1000, bf16=False)
+    gc.collect()
+    assert all(ref() is not None for ref in old)
