@@ -1145,9 +1145,12 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(AttnArgs a, int R)
 // of one of 1024: 6.5 us.
 constexpr int kRowsBlocks = 1024;   // four per CU
 
-// kAux as above where a key head has at most 16 rows; where it has more, its keys are read
-// again for each 16 (128 rows a key head, 32 sequences of 8192: 166 us past the caches, 112
-// through them; 24 rows of 8 key heads, 16 sequences: 61 and 68).
+// kAux as above where no key head can have more than 16 chosen rows; where one has more, its keys
+// are read again for each 16.  16 sequences of 8192, 8 key heads of 128 in bf16, keys not in the
+// caches before, through them and past them: 16 rows a key head 81 and 76 us, 17 rows 117 and 133,
+// 32 rows 146 and 148, 64 rows 269 and 301, 128 rows 514 and 703.  Which heads are chosen is known on
+// the device alone: 24 spread over key heads of 24 query heads each, 3 a key head, take 64 us this
+// way and would take 58 past the caches, but 24 of one key head would lose more.
 template <int D, bool kE4m3, int kAux>
 __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void cache_attn_rows_kernel(AttnArgs a) {
     constexpr int S = D / 32;
