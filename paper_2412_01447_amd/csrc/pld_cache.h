@@ -137,9 +137,9 @@ __device__ __forceinline__ float soft_cap_near(float x, float inv2_log2e) {
 // Anywhere: from there on as cap times 1 - 2 / (1 + e^(2|y|)), whose error of a few 2^-24 of the
 // cap is no more than that of the result; nearer to 0 the difference would cancel.
 constexpr float kCapNear = 1.f;   // of 2 |y| log2(e): |y| = 0.347
-__device__ __forceinline__ float soft_cap(float x, float cap, float inv2_log2e) {
+__device__ __forceinline__ float soft_cap(float x, float cap, float cap_x2, float inv2_log2e) {
     const float w = fabsf(x) * inv2_log2e;
-    const float far = cap - 2.f * cap * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(w) + 1.f);
+    const float far = cap - cap_x2 * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(w) + 1.f);
     return w < kCapNear ? soft_cap_near(x, inv2_log2e) : copysignf(far, x);
 }
 

@@ -10,8 +10,10 @@ struct AttnArgs {
     const uint16_t *q;
     int64_t qs, qr;
     int Hq;
-    float scale, cap, inv2_log2e;   // inv2_log2e: of scores in the attention's units
-    float cap2;                     // cap in log2 units
+    float scale;
+    // The cap, in log2 units, twice it, the score from which on soft_cap_near will not do (all 0:
+    // no cap) and soft_cap's factor: taken here they would hold vector registers all along.
+    float cap, cap_x2, cap_near, inv2_log2e;
     int window;
     int G, groups;                  // query heads per key head; row groups per sequence
     uint32_t page16, slot16;        // strides of a page and a slot in 16 bytes
@@ -349,13 +351,13 @@ __device__ __forceinline__ float scale_scores(const AttnArgs &a, f32x4_t (&x)[2]
             for (int r = 0; r < 4; ++r) w = fmaxf(w, fabsf(x[t][r]));
         }
         // One branch for the wave: few scores come to a third of the cap as a rule (64 x 17 rows
-        // over 16384 tokens in e4m3, cap 50: 1051 us, 1300 with both forms for every score; where
-        // every wave has such a score, cap 8, 1450).
-        if (__any(w * a.inv2_log2e >= kCapNear)) {
+        // over 16384 tokens in e4m3, cap 50: 1060 us, 1300 with both forms for every score; where
+        // every wave has such a score, cap 8, 1480).
+        if (__any(w >= a.cap_near)) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) x[t][r] = soft_cap(x[t][r], a.cap2, a.inv2_log2e);
+                for (int r = 0; r < 4; ++r) x[t][r] = soft_cap(x[t][r], a.cap, a.cap_x2, a.inv2_log2e);
         } else {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -1406,10 +1408,11 @@ static int prep_attn(const pld_cache *cache, bool needs_v, const uint16_t *q, in
     a.r = Rows{lens, draft_len, B, n};
     a.q = q, a.qs = qs, a.qr = qr;
     a.Hq = Hq;
-    a.scale = scale, a.cap = softcap;
-    a.cap2 = softcap * kLog2E;
+    a.scale = scale;
+    a.cap = softcap * kLog2E, a.cap_x2 = 2.f * a.cap;
+    a.cap_near = kCapNear / 2 * softcap;
     a.inv2_log2e = softcap > 0.f ? 2.f / softcap : 0.f;   // 2 log2(e) / (cap log2(e))
-    if (!isfinite(scale * kLog2E) || !isfinite(2.f * a.cap2) || !isfinite(a.inv2_log2e)) return PLD_ERR_INVALID;
+    if (!isfinite(scale * kLog2E) || !isfinite(a.cap_x2) || !isfinite(a.inv2_log2e)) return PLD_ERR_INVALID;
     a.G = Hq / cache->heads;
     a.page16 = (uint32_t)(a.c.page / 16), a.slot16 = (uint32_t)(a.c.slot / 16);
     a.spage32 = (uint32_t)a.c.spage;
