@@ -357,7 +357,7 @@ __device__ __forceinline__ float scale_scores(const AttnArgs &a, f32x4_t (&x)[2]
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) x[t][r] = soft_cap(x[t][r], a.cap, a.cap_x2, a.inv2_log2e);
+                for (int r = 0; r < 4; ++r) x[t][r] = soft_cap(x[t][r], a.cap, a.cap_x2, a.cap_near, a.inv2_log2e);
         } else {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -1410,7 +1410,7 @@ static int prep_attn(const pld_cache *cache, bool needs_v, const uint16_t *q, in
     a.Hq = Hq;
     a.scale = scale;
     a.cap = softcap * kLog2E, a.cap_x2 = 2.f * a.cap;
-    a.cap_near = kCapNear / 2 * softcap;
+    a.cap_near = kCapNear * softcap;
     a.inv2_log2e = softcap > 0.f ? 2.f / softcap : 0.f;   // 2 log2(e) / (cap log2(e))
     if (!isfinite(scale * kLog2E) || !isfinite(a.cap_x2) || !isfinite(a.inv2_log2e)) return PLD_ERR_INVALID;
     a.G = Hq / cache->heads;

@@ -133,6 +133,30 @@ def test_caps(cap, G, D, dtype):
                     assert (a[b, h, pos + 1:] == 7).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("cap", [1.0, 10.0, 30.0])
+@pytest.mark.parametrize("G", [1, 4, 12])
+def test_capped_scores_go_by_their_own_keys(G, cap, dtype):
+    """Large and infinite scores of keys that a row does not see leave its bits as they are,
+    whichever form of the cap they take."""
+    lens, n = [37, 130], 5
+    c = Case(lens, n, 2 * G, 2, 64, 16, E4M3 if dtype == "e4m3" else torch.bfloat16, seed=G)
+    c.q *= 4
+    clean, L = c.attend(softcap=cap)
+    used = np.zeros((c.k.shape[0], 16), bool)
+    for b, T in enumerate(lens):
+        for j in range(T + n - 1):
+            used[c.table[b, j // 16], j % 16] = True
+    hole = torch.from_numpy(~used).to(dev())
+    for poison in (0.01, 30.0, 1e30, math.inf):
+        if dtype == "bf16":
+            c.k[hole] = poison
+        else:
+            c.ks.transpose(1, 2)[hole] = poison
+        out, lse = c.attend(softcap=cap)
+        assert np.array_equal(bits(out), bits(clean)) and np.array_equal(bits(lse), bits(L)), poison
+
+
 # ------------------------------------------------------------------ scales
 @pytest.mark.parametrize("G", [1, 4, 12])            # 5, 20 and 60 rows a key head
 @pytest.mark.parametrize("D", [64, 128, 256])
