@@ -737,18 +737,19 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
 // rest; 4 x 33 rows of 4 heads a key head over 131072 tokens in bf16 510 us, 555 TFLOP/s and 4.2 TB/s.
 // (A ninth tile as two waves' work, half the keys each, took 5% longer.)
 constexpr int kStep = 64;   // keys
-template <int D>
+template <int D, int kMT>
 struct WideLds {
+    static constexpr bool kThird = kMT > 2;             // some waves have a third tile
     u32x4_t k[2][4][D / 32][64], v[2][2][D / 16][64];   // operands of two steps
-    u32x4_t q[3][D / 32][64];                           // the queries of tiles 8 .. 10
+    u32x4_t q[kThird ? 3 : 1][D / 32][kThird ? 64 : 1]; // the queries of tiles 8 .. 10
     f32x4_t scale[2][2][kStep / 4];
     uint32_t odd[2][2][3];                              // [step][32 keys][half; scales]: not finite
 };
 
 // A wave's whole work on an item, with NT tiles of its own (from tile0 on, every fourth):
 // a block's waves meet at the same barriers whatever their NT.
-template <int D, bool kE4m3, int NT>
-__device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds, const Item &it, int kv,
+template <int D, bool kE4m3, int NT, int kMT>
+__device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D, kMT> &lds, const Item &it, int kv,
                                              int u0, int u1, int tile0, int R) {
     constexpr int S = D / 32, NJ = D / 16, NA = NT ? NT : 1;
     constexpr int KL = kE4m3 ? S / 2 : S;           // 16-byte loads of a key's row per lane
@@ -772,10 +773,11 @@ __device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds,
         for (int s = 0; s < S; ++s) {
             const int d = kE4m3 ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
             const u32x4_t v = *reinterpret_cast<const u32x4_t *>(qp + d);
-            if (t < kQ)
+            if (t < kQ) {
                 q[t][s] = as_bf16x8(v);
-            else if (tile0 < 3)
-                lds.q[tile0][s][lane] = v;   // read by this wave alone
+            } else if constexpr (NT > 2) {
+                if (tile0 < 3) lds.q[tile0][s][lane] = v;   // read by this wave alone
+            }
         }
         const int64_t p = (int64_t)it.pos0 + i;
         see_hi[t] = (int)min(p + 1, (int64_t)it.hi);
@@ -1027,7 +1029,7 @@ __device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D> &lds,
 
 template <int D, bool kE4m3, int kMT>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_wide_kernel(AttnArgs a, int R) {
-    __shared__ WideLds<D> lds;
+    __shared__ WideLds<D, kMT> lds;
     __shared__ int64_t s_w[8];
     __shared__ int s_e[3];
     const int wave = uniform((int)threadIdx.x / 64);
