@@ -136,8 +136,10 @@ int pld_cache_write(const pld_cache *cache, const uint16_t *q, int64_t q_seq_str
  * Device-side rules: keys that a row does not see do not affect it, whatever
  * their slots hold; a row one of whose keys lies on a bad page or past the table
  * gets NaN in out and lse.  Where a value that a row sees is not finite, that head
- * of its out, and its lse, may be NaN as a whole.  A row has to see a score above
- * -1e29 (no finite inputs of ordinary size come near it).
+ * of its out, and its lse, may be NaN as a whole.  Values past 2^89 may overflow: up
+ * to 2^30 of them are summed, with weights of up to 2^8, before the division by the
+ * weights' sum.  A row has to see a score above -1e29 (no finite inputs of ordinary
+ * size come near it).
  * Errors: PLD_ERR_INVALID (also out at q), PLD_ERR_ALIGN, PLD_ERR_WORKSPACE,
  * PLD_ERR_LAUNCH.
  */

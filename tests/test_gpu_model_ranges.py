@@ -175,6 +175,23 @@ def test_seen_scales_that_are_not_finite(which, poison, D, G):
     assert not torch.isfinite(out[0, :, G:].float()).any(-1).any()
 
 
+# ------------------------------------------------------------------ large values
+@pytest.mark.parametrize("G", [1, 4, 12])
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+def test_large_values(dtype, G):
+    """Values of up to 2^89 and keys in the thousands: products are summed before the division by
+    the weights' sum, and do not overflow."""
+    c = Case([3000, 40], 5, 2 * G, 2, 128, 64, E4M3 if dtype == "e4m3" else torch.bfloat16, seed=G)
+    if dtype == "bf16":
+        c.v = (c.v.float().sign() * 2.0 ** 89).to(torch.bfloat16)
+        c.v[:, :, 1] = 2.0 ** 89
+    else:
+        c.vs *= 2.0 ** 89 / (448 * 0.03)
+    out, L = c.attend()
+    c.check_attend(out, L, rows={(0, 0), (0, 4), (1, 0), (1, 3)})
+    assert torch.isfinite(out.float()).all()
+
+
 # ------------------------------------------------------------------ wide strides
 @pytest.mark.parametrize("D,G", [(128, 4), (64, 12)])      # 20 and 60 rows a key head
 def test_slots_far_apart(D, G):
