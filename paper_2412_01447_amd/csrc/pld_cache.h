@@ -137,7 +137,7 @@ __device__ __forceinline__ float soft_cap_near(float x, float inv2_log2e) {
 // Anywhere: from |x| = cap_near on as cap times 1 - 2 / (1 + e^(2|y|)), whose error of a few 2^-24
 // of the cap is no more than that of the result; nearer to 0 the difference would cancel.  (The
 // same comparison as before a branch on many scores: a score's bits go by it alone.)
-constexpr float kCapNear = 0.5f;   // of the cap and a score in log2 units: |y| = 0.347
+constexpr float kCapNear = 0.347f;   // cap_near, of the cap
 __device__ __forceinline__ float soft_cap(float x, float cap, float cap_x2, float cap_near, float inv2_log2e) {
     const float e = __builtin_amdgcn_exp2f(fabsf(x) * inv2_log2e);   // e^(2|y|)
     const float far = cap - cap_x2 * __builtin_amdgcn_rcpf(e + 1.f);

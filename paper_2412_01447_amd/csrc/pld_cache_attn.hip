@@ -11,9 +11,10 @@ struct AttnArgs {
     int64_t qs, qr;
     int Hq;
     float scale;
-    // The cap, in log2 units, twice it, the score from which on soft_cap_near will not do (all 0:
-    // no cap) and soft_cap's factor: taken here they would hold vector registers all along.
+    // The cap in the units of the scores, twice it, the score from which on soft_cap_near will not
+    // do (all 0: no cap) and soft_cap's factor: taken here they would hold vector registers all along.
     float cap, cap_x2, cap_near, inv2_log2e;
+    float nat;                      // from log2 units, as the scores have them, to natural ones
     int window;
     int G, groups;                  // query heads per key head; row groups per sequence
     uint32_t page16, slot16;        // strides of a page and a slot in 16 bytes
@@ -293,6 +294,11 @@ __device__ __forceinline__ bf16x8_t key_operand(u32x4_t piece, int s) {
     }
 }
 
+// The log sum from a maximum in the scores' log2 units and the weights' sum.
+__device__ __forceinline__ float log_sum(const AttnArgs &a, float m, float l) {
+    return fmaf(m, a.nat, __log2f(l) * kLn2);
+}
+
 // Where a partial result is: blocks keep one of an item that began before their
 // range (slot 0) and one of an item that ends after it (slot 1).
 template <int D>
@@ -332,8 +338,9 @@ __device__ __forceinline__ float max_of(const f32x4_t (&x)[2]) {
                  fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
 }
 
-// Products into scores; returns the factor that is left to log2 units (c1, where it is the
-// same for all keys and no cap comes between).  ks: the keys' scales times c1.
+// Products into scores; returns the factor that is left to their units (c1, where it is the
+// same for all keys and no cap comes between): log2 units in the attention, whose weights are
+// then one fused multiply-add and 2^x, natural ones for the chosen heads' weights.  ks: the keys' scales times c1.
 template <bool kE4m3>
 __device__ __forceinline__ float scale_scores(const AttnArgs &a, f32x4_t (&x)[2], float c1, f32x4_t ks0,
                                               f32x4_t ks1) {
@@ -709,7 +716,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
                 }
                 if (r == 0 && g == 0) {
                     if (whole) {
-                        if (a.lse) a.lse[lat] = gone ? nan : (mg[t] + __log2f(lg[t])) * kLn2;
+                        if (a.lse) a.lse[lat] = gone ? nan : log_sum(a, mg[t], lg[t]);
                     } else {
                         part[R * D + 2 * row] = mg[t];
                         part[R * D + 2 * row + 1] = lg[t];
@@ -1018,7 +1025,7 @@ __device__ __forceinline__ void wide_segment(const AttnArgs &a, WideLds<D, kMT> 
             }
         if (g == 0) {
             if (whole) {
-                if (a.lse) a.lse[lat] = gone ? nan : (m[n] + __log2f(lg)) * kLn2;
+                if (a.lse) a.lse[lat] = gone ? nan : log_sum(a, m[n], lg);
             } else {
                 part[R * D + 2 * row] = m[n];
                 part[R * D + 2 * row + 1] = lg;
@@ -1136,7 +1143,7 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(AttnArgs a, int R)
     const float inv = gone ? __uint_as_float(0x7fc00000u) : 1.f / l;
     *reinterpret_cast<uint2 *>(a.out + oat + 4 * lane) =
         make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
-    if (a.lse && lane == 0) a.lse[lat] = gone ? inv : (m + __log2f(l)) * kLn2;
+    if (a.lse && lane == 0) a.lse[lat] = gone ? inv : log_sum(a, m, l);
 }
 
 // ------------------------------------------------ chosen heads at one row
@@ -1232,7 +1239,7 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void cache_attn_rows_kernel(
     int b = uniform(s_b);
     int64_t first = uniform(s_w[4]);
 
-    const float c1 = a.scale * kLog2E, nan = __uint_as_float(0x7fc00000u);
+    const float c1 = a.scale, nan = __uint_as_float(0x7fc00000u);
     const int64_t cap = (int64_t)a.c.max_pages << a.c.shift;
     while (x < x1) {
         const int64_t units = uniform(units_of(b)), span = units * heads;
@@ -1282,7 +1289,7 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void cache_attn_rows_kernel(
                     const int d = kE4m3 ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
                     q[s] = as_bf16x8(*reinterpret_cast<const u32x4_t *>(qp + d));
                 }
-                const float lse2 = a.lse[((int64_t)b * a.r.n + row) * a.Hq + head] * kLog2E;
+                const float lse = a.lse[((int64_t)b * a.r.n + row) * a.Hq + head];
                 float *dst = a.attn + (int64_t)b * a.as + (int64_t)r * a.ar;
                 const bool vec = ((uintptr_t)dst & 15) == 0;
 
@@ -1325,7 +1332,7 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void cache_attn_rows_kernel(
 #pragma unroll
                     for (int t = 0; t < 2; ++t)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) w[t][e] = __builtin_amdgcn_exp2f(fmaf(w[t][e], sc, -lse2));
+                        for (int e = 0; e < 4; ++e) w[t][e] = __builtin_amdgcn_exp2f(fmaf(w[t][e], sc, -lse) * kLog2E);
                     if (bad || kv < 0 || k0 < lo || k0 + 32 > it.hi) {
 #pragma unroll
                         for (int t = 0; t < 2; ++t)
@@ -1399,7 +1406,7 @@ static void launch_attn(const AttnArgs &a, const AttnShape &sh, hipStream_t s) {
 
 static int prep_attn(const pld_cache *cache, bool needs_v, const uint16_t *q, int64_t qs,
                      int64_t qr, const int32_t *lens, const int32_t *draft_len, int B, int n,
-                     int Hq, float scale, float softcap, int window, AttnArgs &a) {
+                     int Hq, float scale, float softcap, int window, float unit, AttnArgs &a) {
     a = AttnArgs{};
     int rc = prep_cache(cache, needs_v, a.c);
     if (rc == PLD_OK) rc = check_batch(cache, lens, B, n, Hq);
@@ -1411,10 +1418,12 @@ static int prep_attn(const pld_cache *cache, bool needs_v, const uint16_t *q, in
     a.q = q, a.qs = qs, a.qr = qr;
     a.Hq = Hq;
     a.scale = scale;
-    a.cap = softcap * kLog2E, a.cap_x2 = 2.f * a.cap;
-    a.cap_near = kCapNear * softcap;
-    a.inv2_log2e = softcap > 0.f ? 2.f / softcap : 0.f;   // 2 log2(e) / (cap log2(e))
-    if (!isfinite(scale * kLog2E) || !isfinite(a.cap_x2) || !isfinite(a.inv2_log2e)) return PLD_ERR_INVALID;
+    a.cap = softcap * unit, a.cap_x2 = 2.f * a.cap, a.cap_near = kCapNear * a.cap;
+    a.inv2_log2e = softcap > 0.f ? (float)(2. * kLog2E / a.cap) : 0.f;
+    // (scale and cap times log2(e) are rounded, a relative error of every score; the way back by
+    // the rounded ones takes it from the log sum, which would be off by 10^-6 at a score of 15)
+    a.nat = softcap > 0.f ? (float)((double)softcap / a.cap) : (float)((double)scale / (scale * unit));
+    if (!isfinite(scale * kLog2E) || !isfinite(2.f * (softcap * kLog2E)) || !isfinite(a.inv2_log2e)) return PLD_ERR_INVALID;
     a.G = Hq / cache->heads;
     a.page16 = (uint32_t)(a.c.page / 16), a.slot16 = (uint32_t)(a.c.slot / 16);
     a.spage32 = (uint32_t)a.c.spage;
@@ -1444,7 +1453,7 @@ extern "C" int pld_cache_attn(const pld_cache *cache, const uint16_t *q, int64_t
                               float *lse, void *workspace, size_t workspace_bytes, void *stream) {
     AttnArgs a;
     int rc = prep_attn(cache, true, q, q_seq_stride, q_row_stride, lens, draft_len, B, n, Hq,
-                       scale, softcap, window, a);
+                       scale, softcap, window, kLog2E, a);
     if (rc != PLD_OK) return rc;
     const int D = cache->head_dim;
     rc = check_rows(out, o_seq_stride, o_row_stride, B, n, (int64_t)Hq * D);
@@ -1479,7 +1488,7 @@ extern "C" int pld_cache_attn_rows(const pld_cache *cache, const uint16_t *q,
                                    int64_t a_row_stride, int64_t n_keys, void *stream) {
     AttnArgs a;
     int rc = prep_attn(cache, false, q, q_seq_stride, q_row_stride, lens, nullptr, B, n, Hq, scale,
-                       softcap, window, a);
+                       softcap, window, 1.f, a);
     if (rc != PLD_OK) return rc;
     if (!row || !heads || !lse || !attn || R < 1 || R > 65535 || n_keys < 1 ||
         n_keys > INT32_MAX - 65536)

@@ -157,6 +157,34 @@ def test_capped_scores_go_by_their_own_keys(G, cap, dtype):
         assert np.array_equal(bits(out), bits(clean)) and np.array_equal(bits(lse), bits(L)), poison
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("cap", [0.0, 1000.0])
+def test_weights_of_exact_products(cap, D):
+    """Whole numbers, whose products are exact in fp32: what is left of a weight's error is that of
+    the score's last roundings, of its distance d from the log sum (2.3 u of it: the difference and
+    the product with log2(e), a constant off by 0.22 u) and of 2^x (2 u), and does not go with the
+    score's size.  A capped score has its own 20 u."""
+    c = Case([400, 77], 2, 8, 2, D, 16, seed=D)
+    scale = float(np.float32(D ** -0.5))
+    c.q = c.q.float().round().mul(2).to(torch.bfloat16)
+    c.k = c.k.float().round().to(torch.bfloat16)
+    row, lens = [1, 0], c.lens
+    L, want = torch.zeros(2, 2, 8, device=dev()), {}
+    for b in range(2):
+        for h in range(8):
+            x = ref.cache_rows(c.k, None, c.table, b, h // 4, lens[b] + row[b]) @ f64(c.q[b, row[b], h]) * scale
+            x = cap * np.tanh(x / cap) if cap else x
+            L[b, row[b], h] = float(np.logaddexp.reduce(x))
+            want[b, h] = x - float(L[b, row[b], h]), np.abs(x)
+    attn = torch.full((2, 8, 410), 7.0, device=dev())
+    pld.pld_cache_attn_rows(c.q, c.k, c.t, c.d_lens, d_i32(row), d_i32(list(range(8))), L, attn, scale=scale, softcap=cap)
+    a = f64(attn)
+    for (b, h), (d, x) in want.items():
+        rel = (2.5 * np.abs(d) + 4 + (21 * x if cap else 0)) * U
+        assert x.max() > 4
+        assert (np.abs(a[b, h, :len(d)] / np.exp(d) - 1) <= rel).all(), (b, h, (np.abs(a[b, h, :len(d)] / np.exp(d) - 1) / rel).max())
+
+
 # ------------------------------------------------------------------ scales
 @pytest.mark.parametrize("G", [1, 4, 12])            # 5, 20 and 60 rows a key head
 @pytest.mark.parametrize("D", [64, 128, 256])
