@@ -81,8 +81,8 @@ __device__ __forceinline__ float query_sum(float v) {
 // spans blocks leaves one partial result per block, joined by a second launch.
 constexpr int kUnit = 128;        // keys
 // Two per CU; nothing depends on their being resident at once.  Twice as many cost a start
-// and a join more than evener ends gain: 39 us become 48 (8 sequences of 4096, 11 rows), and
-// 530 become 665 (4 of 131072, 33 rows).
+// and a join more than evener ends gain: 35 us become 47 (8 sequences of 4096, 11 rows), and
+// 510 become 540 (4 of 131072, 33 rows).
 constexpr int kAttnBlocks = 512;
 
 struct Item {
@@ -193,10 +193,12 @@ __device__ __forceinline__ u32x4_t buffer_load16(__amdgpu_buffer_rsrc_t b, uint3
     return __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(b, off, soff, kAux));
 }
 // kAux of rows that one block reads once: without it the caches keep what nobody asks for
-// again (64 sequences of 8192 tokens, 8 heads of 128 in bf16: 383 us without, 347 with it).
-// Not for rows of half a 128-byte line, whose other half is the next head's and would be
-// fetched twice (32 heads of 64 in e4m3: 201 without, 225 with it), and not in the wide form,
-// whose keys other row groups read too (a 2048-token prefill: 489 without, 581 with it).
+// again (64 sequences of 8192 tokens, 8 heads of 128 in bf16: 367 us without, 331 with it).
+// Not for rows of half a 128-byte line, whose other half is the next head's, read by another
+// block (32 heads of 64 in e4m3, slot by slot: 376 without and 391 with it for 16 sequences of
+// 16384 in pages of 16, though 419 and 377 for 32 of 8192 in pages of 64; head by head 198 to
+// 204 either way), and not in the wide form, whose keys other row groups read too (4 x 2048 rows
+// over 8192 tokens: 1510 without, 1880 with it).
 template <int D, bool kE4m3>
 constexpr int kOnce = D * (kE4m3 ? 1 : 2) >= 128 ? 2 : 0;
 template <int kBytes, int kAux = 0, int W>
@@ -419,9 +421,9 @@ __device__ __forceinline__ bf16x8_t value_operand(const uint32_t (&vp)[8][N][W],
 
 // Four waves a block, each with all of the item's rows and 32 of a unit's keys.  Bound by
 // HBM where there is much to read: 64 sequences of 8192, a row of 32 query heads over 8 key
-// heads of 128 in bf16 (2.15 GB): 345 us, 6.2 TB/s; in e4m3 64 of 16384: 391 us.  By the way
+// heads of 128 in bf16 (2.15 GB): 331 us, 6.5 TB/s; in e4m3 64 of 16384: 367 us.  By the way
 // of one dependent load to the next (lengths, page entries, keys, partial results) where there
-// is little: 9.9 us for one row over 1024 tokens, both launches.
+// is little: 10.3 us for one row over 1024 tokens, both launches.
 template <int D, bool kE4m3, int kMT>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnArgs a) {
     constexpr int R = 16 * kMT;
@@ -737,11 +739,12 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attn_kernel(AttnA
 // as operands: each wave fetches a 16-key tile of K and, of 32 keys, half the elements
 // of V, into registers while the block works on the 64 before, and turns them (e4m3 to
 // bf16, V to pairs of keys) once for all waves on the way to LDS.  16 x 8 rows of 8 heads a key
-// head over 8192 tokens: 138 us, 3.9 TB/s, of which the slowest XCD is 20 us behind the mean.
+// head over 8192 tokens: 133 us, 4.1 TB/s, of which the slowest XCD is 20 us behind the mean.
 // With three tiles a wave it is the instructions: 64 x 17 such rows over 16384 tokens in
-// e4m3 (144 rows a key head) take 855 us, 520 TFLOP/s, the matrix units busy for 26% of the time and
-// the vector units for 44%, two waves a SIMD (512 registers hold no third) waiting for the
-// rest; 4 x 33 rows of 4 heads a key head over 131072 tokens in bf16 510 us, 555 TFLOP/s and 4.2 TB/s.
+// e4m3 (144 rows a key head) take 840 us, 530 TFLOP/s, the matrix units busy for 27% of the time and
+// the vector units for 46%, two waves a SIMD (512 registers hold no third) waiting for the
+// rest; 4 x 33 rows of 4 heads a key head over 131072 tokens in bf16 490 to 515 us, some 560 TFLOP/s
+// and 4.3 TB/s.
 // (A ninth tile as two waves' work, half the keys each, took 5% longer.)
 constexpr int kStep = 64;   // keys
 template <int D, int kMT>
@@ -1152,8 +1155,8 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(AttnArgs a, int R)
 // final at once, and a lane stores its four keys of a row together.  The units of all
 // (sequence, used key head) pairs are dealt to the blocks as in the attention; a block's
 // four waves have 32 of a unit's keys each.  Bound by memory, keys read and weights written:
-// 40 heads of 32 sequences of up to 8192 tokens (507 MB): 110 to 117 us, 4.3 to 4.6 TB/s; 8 heads
-// of one of 1024: 6.5 us.
+// 40 heads of 32 sequences of up to 8192 tokens (507 MB): 109 to 113 us, 4.5 to 4.6 TB/s (in e4m3,
+// 280 MB, 74 us); 8 heads of one of 1024: 7.0 us.
 constexpr int kRowsBlocks = 1024;   // four per CU
 
 // kAux as above where no key head can have more than 16 chosen rows; where one has more, its keys

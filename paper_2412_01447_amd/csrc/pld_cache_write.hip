@@ -47,7 +47,7 @@ __device__ __forceinline__ float group_max(float v) {
 // with pairs of halves the runs are each other's partners (t1 = t0 + rot/2), so
 // a rotation needs no other lane; elsewhere they are neighbours.  Bound by memory: 4 x 2048
 // rows of 32 + 2 x 8 heads of 128 (202 MB) in 41 us, 4.9 TB/s, what a large copy reaches (4.83);
-// up to 17 rows of 64 + 2 x 8 heads in each of 64 sequences, into e4m3 (36 MB), in 10.4 us, the vector
+// up to 17 rows of 64 + 2 x 8 heads in each of 64 sequences, into e4m3 (36 MB), in 11 us, the vector
 // instructions of norms and quotients included.  One head a lane group: with four, and their
 // loads together, the waves are too few (41 and 13.5 us, and 3.9 instead of 2.6 us for a
 // single row).  Blocks of one kind of head each would have less to select, but are a third

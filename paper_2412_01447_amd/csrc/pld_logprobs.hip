@@ -34,9 +34,9 @@ struct LogprobArgs {
 // each lane's largest value of a segment: 1/32 of the logits, which tell a second launch, a
 // wave per row, where the row's best elements are. (Kept by the first pass itself, the best
 // twenty cost as much as the pass: 95 us, and 46 without them, for 64 x 17 rows of 128256 in
-// bf16.)  Where 920 of these rows exist (236 MB) the pass takes 47 us, 5.0 TB/s: the card's
+// bf16.)  Where 920 of these rows exist (236 MB) the pass takes 48 us, 4.9 TB/s: the card's
 // reads would take 33 us, and so would an element's exponential and the six or seven other
-// vector instructions.  The second launch takes 11 us with 20 alternatives.
+// vector instructions.  The second launch takes 12 us with 20 alternatives.
 constexpr int kLogElems = 32;
 template <int P>
 constexpr int kLogLoads = kLogElems / P;
