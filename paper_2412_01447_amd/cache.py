@@ -57,7 +57,9 @@ class PagedCache:
             if self.workspace is not None:
                 self.grown.append(self.workspace)
             if stream is not None and not hasattr(stream, "cuda_stream"):
-                stream = torch.cuda.ExternalStream(int(stream), device=self.k.device)
+                # a handle; 0, the default stream's, makes ExternalStream a new stream
+                stream = (torch.cuda.ExternalStream(int(stream), device=self.k.device)
+                          if int(stream) else torch.cuda.default_stream(self.k.device))
             with torch.cuda.stream(stream):      # (None: the current one)
                 self.workspace = torch.empty(need, dtype=torch.uint8, device=self.k.device)
 

@@ -276,3 +276,16 @@ def test_a_workspace_comes_from_the_stream_that_uses_it(handle, monkeypatch):
     assert under == [side.cuda_stream] and torch.cuda.current_stream() != side
     side.synchronize()
     assert np.array_equal(bits(out), bits(want))
+
+
+def test_a_workspace_for_the_default_stream(monkeypatch):
+    """The default stream's handle is 0."""
+    cache, under, empty = PagedCache(1, 100, 2, 64, page_size=16), [], torch.empty
+    q, lens = torch.zeros((1, 3, 8, 64), dtype=torch.bfloat16, device=dev()), d_i32([50])
+    torch.cuda.synchronize()
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: (under.append(torch.cuda.current_stream().cuda_stream), empty(*a, **k))[1])
+    with torch.cuda.stream(torch.cuda.Stream()):
+        cache.attend(q, lens, torch.zeros_like(q), stream=0)
+    monkeypatch.undo()
+    assert under == [0]
+    torch.cuda.synchronize()
