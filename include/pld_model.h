@@ -86,6 +86,7 @@ typedef struct pld_cache {
  * slots, quantised where the cache is PLD_E4M3, and the queries written out.
  * For a head's row x (fp32 throughout, rounded once at the end):
  *   norm     x_t = x_t / sqrt(mean(x^2) + eps) * w_t   (q_norm / k_norm NULL: skipped)
+ *            (elements of up to 2^59: the squares are summed in fp32)
  *   rotate   each pair (a, c) of the first rot_dim elements becomes
  *            (a cos - c sin, c cos + a sin) with the pair's cos and sin of the
  *            row's position (rope NULL: skipped); values are neither normed

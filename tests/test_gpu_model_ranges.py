@@ -220,6 +220,24 @@ def test_large_values(dtype, G):
     assert torch.isfinite(out.float()).all()
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("size", [2.0 ** -60, 2.0 ** 59])
+def test_norms_of_large_and_small_elements(size, D):
+    """Norms of elements of one size, whose squares are near the ends of fp32: the signs times the
+    weights, each rounded once (and the weights' products four times in fp32)."""
+    c = Case([20], 3, 4, 2, D, 16, seed=D)
+    sign = lambda *shape: (normal(c.rng, *shape).float() >= 0).float() * 2 - 1
+    q, k, v = sign(1, 3, 4, D), sign(1, 3, 2, D), normal(c.rng, 1, 3, 2, D)
+    w = normal(c.rng, D)
+    out = torch.zeros_like(c.q)
+    pld.pld_cache_write((q * size).to(torch.bfloat16), (k * size).to(torch.bfloat16), v, c.k, c.v, c.t, c.d_lens, out,
+                        q_norm=w, k_norm=w, eps=0.0)
+    stored = torch.stack([c.k[int(c.table[0, p // 16]), p % 16] for p in (19, 20, 21)])[None]
+    for got, s in ((out, q), (stored, k)):
+        want = f64(s) * f64(w)
+        assert (np.abs(f64(got) - want) <= (2.0 ** -8 + 4 * U) * np.abs(want)).all()
+
+
 # ------------------------------------------------------------------ wide strides
 @pytest.mark.parametrize("D,G", [(128, 4), (64, 12)])      # 20 and 60 rows a key head
 def test_slots_far_apart(D, G):
