@@ -30,6 +30,10 @@ __all__ = [
     "pld_model_version", "pld_cache_write", "pld_cache_attn", "pld_cache_attn_workspace_bytes",
     "pld_cache_attn_rows", "pld_token_logprobs", "pld_token_logprobs_workspace_bytes", "PLD_E4M3",
     "PLD_ROPE_HALVES", "PLD_ROPE_NEIGHBOURS", "PLD_MAX_TOP",
+    "pld_prompt_version", "pld_cache_write_packed", "pld_prompt_attn", "PageLayers",
+    "pld_pages_workspace_bytes", "pld_pages_take", "pld_pages_free", "pld_pages_fork",
+    "pld_pages_compact", "pld_pages_copy", "PLD_MAX_PACKED_ROWS", "PLD_MAX_AXES", "PLD_MAX_LAYERS",
+    "PLD_MAX_PAGES", "PLD_MAX_PAGE_ENTRIES",
 ]
 
 PLD_OK, PLD_ERR_INVALID, PLD_ERR_ALIGN, PLD_ERR_WORKSPACE, PLD_ERR_LAUNCH, PLD_ERR_SCRATCH = range(6)
@@ -39,6 +43,8 @@ PLD_E4M3 = 2                    # a quantised cache's elements (include/pld_mode
 PLD_AGG_SUM, PLD_AGG_MAX = 0, 1
 PLD_ROPE_HALVES, PLD_ROPE_NEIGHBOURS = 0, 1
 PLD_MAX_TOP = 64                # alternatives per row of pld_token_logprobs
+PLD_MAX_PACKED_ROWS, PLD_MAX_AXES = 1 << 24, 4              # include/pld_prompt.h
+PLD_MAX_LAYERS, PLD_MAX_PAGES, PLD_MAX_PAGE_ENTRIES = 64, 1 << 24, 4096
 PLD_MAX_NGRAM, PLD_MAX_HIDDEN, PLD_MAX_BATCH, PLD_MAX_DRAFT_SPLIT = 8, 16384, 4096, 1024
 PLD_MAX_SAMPLE_ROWS = 16384
 PLD_MAX_MATCH = 1024
@@ -61,7 +67,13 @@ class _Cache(ctypes.Structure):
                 ("page_size", _int), ("max_pages", _int), ("heads", _int), ("head_dim", _int)]
 
 
-_cachep = ctypes.POINTER(_Cache)
+class _Pool(ctypes.Structure):
+    """struct pld_pool of include/pld_prompt.h."""
+    _fields_ = [("table", _vp), ("table_stride", _i64), ("refs", _vp), ("seqs", _int),
+                ("max_pages", _int), ("num_pages", _int), ("page_size", _int)]
+
+
+_cachep, _poolp = ctypes.POINTER(_Cache), ctypes.POINTER(_Pool)
 
 _SIGNATURES = {
     "pld_version": ([], _int),
@@ -121,6 +133,18 @@ _SIGNATURES = {
     "pld_cache_attn_rows": ([_cachep, _vp, _i64, _i64, _vp, _vp, _vp, _int, _vp, _int, _int, _int,
                              _f32, _f32, _int, _vp, _i64, _i64, _i64, _vp], _int),
     "pld_token_logprobs_workspace_bytes": ([_int, _int, _int, _int, _int], _sz),
+    "pld_prompt_version": ([], _int),
+    "pld_cache_write_packed": ([_cachep, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _f32, _vp, _i64, _int,
+                                _int, _int, _vp, _int, _i64, _vp, _vp, _vp, _int, _int, _int, _vp, _i64,
+                                _vp, _i64, _vp], _int),
+    "pld_prompt_attn": ([_vp, _i64, _vp, _i64, _vp, _i64, _vp, _int, _int, _int, _int, _int, _f32, _f32,
+                         _int, _vp, _i64, _vp, _vp], _int),
+    "pld_pages_workspace_bytes": ([_poolp, _int], _sz),
+    "pld_pages_take": ([_poolp, _vp, _vp, _int, _vp, _vp, _sz, _vp], _int),
+    "pld_pages_free": ([_poolp, _vp, _vp, _int, _vp], _int),
+    "pld_pages_fork": ([_poolp, _cachep, _int, _vp, _vp, _vp, _int, _vp, _vp, _sz, _vp], _int),
+    "pld_pages_compact": ([_poolp, _cachep, _int, _vp, _vp, _vp, _i64, _vp, _vp, _sz, _vp], _int),
+    "pld_pages_copy": ([_cachep, _cachep, _int, _vp, _vp, _vp, _int, _vp], _int),
     "pld_token_logprobs": ([_vp, _int, _i64, _i64, _int, _int, _vp, _vp, _int, ctypes.c_double, _vp,
                             _vp, _int, _vp, _vp, _vp, _sz, _vp], _int),
 }
@@ -789,3 +813,201 @@ def pld_token_logprobs(logits, tokens, logprob, workspace, count=None, temperatu
         _ptr(logprob), _ptr(entropy), top, _ptr(top_ids) if top else None,
         _ptr(top_logprobs) if top else None, _ptr(workspace), _nbytes(workspace),
         _stream(stream)), prepare)
+
+
+# ------------------------------------------------- a prompt's pass and its pages
+def pld_prompt_version():
+    return _load().pld_prompt_version()
+
+
+def _packed_rows(t, name, N, heads, D):
+    """Row stride of a bf16 [N][heads][D] tensor whose heads follow each other."""
+    torch = _torch or _th()
+    if t.dtype != torch.bfloat16 or t.shape != (N, heads, D):
+        raise TypeError(f"{name}: expected bfloat16 {(N, heads, D)}, got {t.dtype} {tuple(t.shape)}")
+    st = t.stride()
+    if st[2] != 1 or (heads > 1 and st[1] != D):
+        raise TypeError(f"{name}: a row's heads must follow each other")
+    return st[0]
+
+
+def pld_cache_write_packed(q, k, v, k_cache, v_cache, table, starts, first, q_out, k_out=None,
+                           k_scale=None, v_scale=None, q_norm=None, k_norm=None, eps=1e-6, rope=None,
+                           rope_pairs=PLD_ROPE_HALVES, positions=None, pair_axis=None, stream=None,
+                           prepare=False):
+    """pld_cache_write for packed rows q bf16 [N][Hq][D], k and v [N][heads][D]: row r of sequence b,
+    starts[b] <= r < starts[b+1] (int32 [B+1]), goes to position first[b] + r - starts[b] of its cache.
+    positions int32 [axes][N]: the rows' positions in rope on each axis, pair_axis int32 [rot_dim/2]
+    the axis of each pair (default: the cache's position on all); k_out: the finished keys."""
+    torch = _torch or _th()
+    _on_one_device(stream, q, k, v, k_cache, v_cache, table, starts, first, q_out, k_out, k_scale,
+                   v_scale, q_norm, k_norm, rope, positions, pair_axis)
+    if q.dim() != 3:
+        raise TypeError("q must be [N][Hq][D]")
+    N, Hq, D = q.shape
+    B = first.numel()
+    cache = _cache_of(k_cache, v_cache, table, k_scale, v_scale, B)
+    if cache.head_dim != D:
+        raise TypeError(f"q has heads of {D} elements, the cache of {cache.head_dim}")
+    heads = cache.heads
+    qs, ks = _packed_rows(q, "q", N, Hq, D), _packed_rows(k, "k", N, heads, D)
+    vs, os_ = _packed_rows(v, "v", N, heads, D), _packed_rows(q_out, "q_out", N, Hq, D)
+    kos = 0 if k_out is None else _packed_rows(k_out, "k_out", N, heads, D)
+    _ints(starts, "starts", B + 1)
+    _ints(first, "first", B)
+    for t, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+        if t is not None and (t.dtype != torch.bfloat16 or t.shape != (D,)
+                              or not t.is_contiguous()):
+            raise TypeError(f"{name} must be a contiguous bfloat16 tensor of {D} elements")
+    rs = (0, 0) if rope is None else _need(rope, torch.float32, "rope", 2)
+    n_pos, rot = (0, 0) if rope is None else rope.shape
+    if n_pos == 1:
+        rs = (rot, 1)
+    axes, axis_stride = 1, N
+    if positions is not None:
+        if positions.dtype != torch.int32 or positions.dim() != 2 or positions.shape[1] != N or (
+                N > 1 and positions.stride(1) != 1):
+            raise TypeError(f"positions must be an int32 [axes][{N}] tensor")
+        axes, axis_stride = positions.shape[0], positions.stride(0)
+        if axes == 1:
+            axis_stride = N
+    elif pair_axis is not None:
+        raise TypeError("pair_axis goes with positions")
+    if rope is not None:
+        _ints(pair_axis, "pair_axis", rot // 2)
+    return _run("pld_cache_write_packed", (
+        cache, _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _ptr(q_norm), _ptr(k_norm), float(eps),
+        _ptr(rope), rs[0], n_pos, rot, int(rope_pairs), _ptr(positions), axes, axis_stride,
+        _ptr(pair_axis), _ptr(starts), _ptr(first), B, N, Hq, _ptr(q_out), os_, _ptr(k_out), kos,
+        _stream(stream)), prepare)
+
+
+def pld_prompt_attn(q, k, v, starts, out, lse=None, scale=None, softcap=0.0, window=0, stream=None,
+                    prepare=False):
+    """Causal attention of the packed rows q bf16 [N][Hq][D] of the sequences starts int32 [B+1] to
+    the keys and values k, v [N][heads][D] of their own sequence: out like q, lse fp32 [N][Hq];
+    scale defaults to 1 / sqrt(D), softcap and window are off at 0."""
+    _on_one_device(stream, q, k, v, starts, out, lse)
+    if q.dim() != 3 or k.dim() != 3 or starts.dim() != 1:
+        raise TypeError("q must be [N][Hq][D], k [N][heads][D] and starts [B+1]")
+    N, Hq, D = q.shape
+    heads, B = k.shape[1], starts.shape[0] - 1
+    qs, ks = _packed_rows(q, "q", N, Hq, D), _packed_rows(k, "k", N, heads, D)
+    vs, os_ = _packed_rows(v, "v", N, heads, D), _packed_rows(out, "out", N, Hq, D)
+    _ints(starts, "starts", B + 1)
+    _floats(lse, "lse", N, Hq)
+    return _run("pld_prompt_attn", (
+        _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _ptr(starts), B, N, Hq, heads, D,
+        D ** -0.5 if scale is None else float(scale), float(softcap), int(window), _ptr(out), os_,
+        _ptr(lse), _stream(stream)), prepare)
+
+
+class PageLayers:
+    """The caches of the pld_pages_* calls, marshalled once: a list of [pages][slots][heads][D]
+    tensors each for keys and values (and of scales for float8_e4m3fn), one a layer, alike in
+    shape and strides.  The tensors are kept."""
+
+    def __init__(self, k_caches, v_caches, k_scales=None, v_scales=None):
+        torch = _torch or _th()
+        if len(k_caches) != len(v_caches) or any(
+                s is not None and len(s) != len(k_caches) for s in (k_scales, v_scales)):
+            raise TypeError("as many v_caches (and scales) as k_caches")
+        self.tensors = [tuple(k_caches), tuple(v_caches), k_scales and tuple(k_scales),
+                        v_scales and tuple(v_scales)]
+        self.count = len(k_caches)
+        none = torch.empty((1, 1), dtype=torch.int32, device=k_caches[0].device if self.count else "cpu")
+        self.caches = (_Cache * max(1, self.count))(*(
+            _cache_of(k, v, none, k_scales and k_scales[i], v_scales and v_scales[i], 1)
+            if none.is_cuda else _layer_off(k) for i, (k, v) in enumerate(zip(k_caches, v_caches))))
+        self.each = [t for ts in self.tensors if ts for t in ts]
+        if self.count and len({t.get_device() for t in self.each}) > 1:
+            raise TypeError("caches on several devices")
+        if len({(c.dtype, c.scale_page_stride, c.page_stride, c.slot_stride, c.head_stride, c.num_pages,
+                 c.page_size, c.heads, c.head_dim) for c in self.caches}) > 1:
+            raise TypeError("the layers' caches must be alike in type, shape and strides")
+
+
+def _layer_off(t):
+    raise TypeError(f"expected device tensors, got one on {t.device}")
+
+
+def _pool_of(table, refs, page_size):
+    """struct pld_pool of the table int32 [seqs][pages] and the references int32 [num_pages]."""
+    torch = _torch or _th()
+    ts = _need(table, torch.int32, "table", 2)
+    _ints(refs, "refs", refs.numel())
+    return _Pool(_ptr(table), max(ts[0], table.shape[1]) if table.shape[0] == 1 else ts[0], _ptr(refs),
+                 table.shape[0], table.shape[1], refs.numel(), page_size)
+
+
+def pld_pages_workspace_bytes(table, refs, page_size, count):
+    return int(_load().pld_pages_workspace_bytes(_pool_of(table, refs, page_size), count))
+
+
+def pld_pages_take(table, refs, page_size, seq, need, status, workspace, stream=None, prepare=False):
+    """The entries of sequences seq int32 [count] for positions below need[i] that name no page get
+    free ones of the pool (table int32 [seqs][pages], refs int32 [num_pages])."""
+    _on_one_device(stream, table, refs, seq, need, status, workspace)
+    count = seq.numel()
+    for t, name in ((seq, "seq"), (need, "need"), (status, "status")):
+        _ints(t, name, count)
+    return _run("pld_pages_take", (
+        _pool_of(table, refs, page_size), _ptr(seq), _ptr(need), count, _ptr(status),
+        _ptr(workspace), _nbytes(workspace), _stream(stream)), prepare)
+
+
+def pld_pages_free(table, refs, page_size, seq, keep=None, stream=None, prepare=False):
+    """Sequences seq int32 [count] give back the pages behind their first keep[i] positions (all)."""
+    _on_one_device(stream, table, refs, seq, keep)
+    count = seq.numel()
+    _ints(seq, "seq", count)
+    _ints(keep, "keep", count)
+    return _run("pld_pages_free", (_pool_of(table, refs, page_size), _ptr(seq), _ptr(keep), count,
+                                   _stream(stream)), prepare)
+
+
+def pld_pages_fork(table, refs, page_size, layers, src, dst, lens, status, workspace, stream=None,
+                   prepare=False):
+    """Sequences dst[i] go on from the first lens[i] tokens of src[i]: whole pages shared, the last
+    token's page copied in every one of `layers` (a PageLayers)."""
+    _on_one_device(stream, table, refs, src, dst, lens, status, workspace, *layers.each[:1])
+    count = src.numel()
+    for t, name in ((src, "src"), (dst, "dst"), (lens, "lens"), (status, "status")):
+        _ints(t, name, count)
+    return _run("pld_pages_fork", (
+        _pool_of(table, refs, page_size), layers.caches, layers.count, _ptr(src), _ptr(dst),
+        _ptr(lens), count, _ptr(status), _ptr(workspace), _nbytes(workspace), _stream(stream)), prepare)
+
+
+def pld_pages_compact(table, refs, page_size, layers, page_map, used, workspace, table_out=None,
+                      refs_out=None, stream=None, prepare=False):
+    """Pages in use move to the lowest indices, in every one of `layers`: page_map int32 [num_pages]
+    gets their new places, used int32 [1] their number, table_out and refs_out (default: the pool's
+    own) the new table and references."""
+    torch = _torch or _th()
+    table_out = table if table_out is None else table_out
+    refs_out = refs if refs_out is None else refs_out
+    _on_one_device(stream, table, refs, page_map, used, table_out, refs_out, workspace, *layers.each[:1])
+    ts = _need(table_out, torch.int32, "table_out", 2)
+    if table_out.shape != table.shape:
+        raise TypeError(f"table_out must be {tuple(table.shape)}, got {tuple(table_out.shape)}")
+    _ints(page_map, "page_map", refs.numel())
+    _ints(refs_out, "refs_out", refs.numel())
+    _ints(used, "used", 1)
+    return _run("pld_pages_compact", (
+        _pool_of(table, refs, page_size), layers.caches, layers.count, _ptr(page_map), _ptr(used),
+        _ptr(table_out), max(ts[0], table.shape[1]), _ptr(refs_out), _ptr(workspace),
+        _nbytes(workspace), _stream(stream)), prepare)
+
+
+def pld_pages_copy(layers_from, layers_to, src, dst, slots=None, stream=None, prepare=False):
+    """The first slots[i] slots (all) of page src[i] of every layer of `layers_from` to page dst[i] of
+    the same layer of `layers_to`."""
+    _on_one_device(stream, src, dst, slots, *layers_from.each[:1], *layers_to.each[:1])
+    count = src.numel()
+    for t, name in ((src, "src"), (dst, "dst"), (slots, "slots")):
+        _ints(t, name, count)
+    if layers_from.count != layers_to.count:
+        raise TypeError(f"{layers_from.count} layers and {layers_to.count}")
+    return _run("pld_pages_copy", (layers_from.caches, layers_to.caches, layers_from.count, _ptr(src),
+                                   _ptr(dst), _ptr(slots), count, _stream(stream)), prepare)

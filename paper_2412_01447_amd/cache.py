@@ -8,8 +8,18 @@ verification `weights` renews the attention rows that the next step ranks by.
 """
 import torch
 
-from . import (PLD_ROPE_HALVES, pld_cache_attn, pld_cache_attn_rows,
-               pld_cache_attn_workspace_bytes, pld_cache_write)
+from . import (PLD_ROPE_HALVES, PageLayers, pld_cache_attn, pld_cache_attn_rows,
+               pld_cache_attn_workspace_bytes, pld_cache_write, pld_cache_write_packed, pld_pages_compact,
+               pld_pages_copy, pld_pages_fork, pld_pages_free, pld_pages_take, pld_pages_workspace_bytes)
+
+
+def _under(stream, device):
+    """torch.cuda.stream of a stream, its handle, or None (the current one)."""
+    if stream is not None and not hasattr(stream, "cuda_stream"):
+        # a handle; 0, the default stream's, makes ExternalStream a new stream
+        stream = (torch.cuda.ExternalStream(int(stream), device=device)
+                  if int(stream) else torch.cuda.default_stream(device))
+    return torch.cuda.stream(stream)
 
 
 class PagedCache:
@@ -56,11 +66,7 @@ class PagedCache:
         if self.workspace is None or self.workspace.numel() < need:
             if self.workspace is not None:
                 self.grown.append(self.workspace)
-            if stream is not None and not hasattr(stream, "cuda_stream"):
-                # a handle; 0, the default stream's, makes ExternalStream a new stream
-                stream = (torch.cuda.ExternalStream(int(stream), device=self.k.device)
-                          if int(stream) else torch.cuda.default_stream(self.k.device))
-            with torch.cuda.stream(stream):      # (None: the current one)
+            with _under(stream, self.k.device):
                 self.workspace = torch.empty(need, dtype=torch.uint8, device=self.k.device)
 
     def write(self, q, k, v, lens, q_out, draft_len=None, q_norm=None, k_norm=None, eps=1e-6,
@@ -70,6 +76,17 @@ class PagedCache:
                                draft_len=draft_len, k_scale=self.k_scale, v_scale=self.v_scale,
                                q_norm=q_norm, k_norm=k_norm, eps=eps, rope=rope,
                                rope_pairs=rope_pairs, stream=stream, prepare=prepare)
+
+    def write_packed(self, q, k, v, starts, first, q_out, k_out=None, q_norm=None, k_norm=None, eps=1e-6,
+                     rope=None, rope_pairs=PLD_ROPE_HALVES, positions=None, pair_axis=None,
+                     stream=None, prepare=False):
+        """The packed rows' keys and values into their slots, the finished queries (and keys, for
+        pld_prompt_attn) into q_out and k_out."""
+        return pld_cache_write_packed(q, k, v, self.k, self.v, self.table, starts, first, q_out,
+                                      k_out=k_out, k_scale=self.k_scale, v_scale=self.v_scale,
+                                      q_norm=q_norm, k_norm=k_norm, eps=eps, rope=rope,
+                                      rope_pairs=rope_pairs, positions=positions,
+                                      pair_axis=pair_axis, stream=stream, prepare=prepare)
 
     def attend(self, q, lens, out, draft_len=None, lse=None, scale=None, softcap=0.0, window=0,
                stream=None, prepare=False):
@@ -87,3 +104,73 @@ class PagedCache:
         return pld_cache_attn_rows(q, self.k, self.table, lens, row, heads, lse, attn,
                                    k_scale=self.k_scale, scale=scale, softcap=softcap,
                                    window=window, stream=stream, prepare=prepare)
+
+
+class PagePool:
+    """The pages of several layers' caches, shared by sequences that go on from the same prompt.
+
+    Lists of [pages][slots][heads][D] tensors for keys and values, and of [pages][heads][slots]
+    scales, one a layer (of_caches: PagedCache objects, which get the pool's table); table int32
+    [seqs][pages], with -1 for entries that name no page, and refs int32 [pages], how many entries
+    name a page.  Left out, both are absent: such a pool only copies.
+    Calls on one pool follow each other (one stream, or events between): there is one workspace."""
+
+    def __init__(self, k_caches, v_caches, k_scales=None, v_scales=None, table=None, refs=None):
+        self.layers = PageLayers(k_caches, v_caches, k_scales, v_scales)
+        self.table, self.refs = table, refs
+        self.page_size = k_caches[0].shape[1]
+        self.workspace = None
+        self.grown = []                  # workspaces that a larger one has replaced
+
+    @classmethod
+    def of_caches(cls, caches, seqs=None, max_len=None):
+        """A pool over PagedCache objects of the same shape, all pages free: seqs sequences of up to
+        max_len positions (default: as the first cache has them)."""
+        c = caches[0]
+        seqs = c.table.shape[0] if seqs is None else seqs
+        per = c.table.shape[1] if max_len is None else -(-max_len // c.page_size)
+        table = torch.full((seqs, per), -1, dtype=torch.int32, device=c.k.device)
+        refs = torch.zeros(c.k.shape[0], dtype=torch.int32, device=c.k.device)
+        scales = (None, None) if c.k_scale is None else ([x.k_scale for x in caches], [x.v_scale for x in caches])
+        for x in caches:
+            x.table = table
+        return cls([x.k for x in caches], [x.v for x in caches], *scales, table=table, refs=refs)
+
+    def reserve(self, count, stream=None):
+        """The workspace for calls of up to `count` sequences or forks (grown as needed: a caller that
+        captures a graph reserves before the capture).  One that is replaced is kept."""
+        need = pld_pages_workspace_bytes(self.table, self.refs, self.page_size, count)
+        if self.workspace is None or self.workspace.numel() < need:
+            if self.workspace is not None:
+                self.grown.append(self.workspace)
+            with _under(stream, self.refs.device):
+                self.workspace = torch.empty(need, dtype=torch.uint8, device=self.refs.device)
+
+    def take(self, seq, need, status, stream=None, prepare=False):
+        """Pages for the positions below need[i] of sequences seq[i]."""
+        self.reserve(seq.numel(), stream)
+        return pld_pages_take(self.table, self.refs, self.page_size, seq, need, status,
+                              self.workspace, stream=stream, prepare=prepare)
+
+    def free(self, seq, keep=None, stream=None, prepare=False):
+        """Sequences seq[i] give back what lies behind their first keep[i] positions (all)."""
+        return pld_pages_free(self.table, self.refs, self.page_size, seq, keep, stream=stream,
+                              prepare=prepare)
+
+    def fork(self, src, dst, lens, status, stream=None, prepare=False):
+        """Sequences dst[i] go on from the first lens[i] tokens of src[i]."""
+        self.reserve(src.numel(), stream)
+        return pld_pages_fork(self.table, self.refs, self.page_size, self.layers, src, dst, lens,
+                              status, self.workspace, stream=stream, prepare=prepare)
+
+    def compact(self, page_map, used, table_out=None, refs_out=None, stream=None, prepare=False):
+        """Pages in use move to the lowest indices; page_map and used say where and how many."""
+        self.reserve(1, stream)
+        return pld_pages_compact(self.table, self.refs, self.page_size, self.layers, page_map, used,
+                                 self.workspace, table_out=table_out, refs_out=refs_out,
+                                 stream=stream, prepare=prepare)
+
+    def copy_from(self, other, src, dst, slots=None, stream=None, prepare=False):
+        """Page src[i] of another pool (its first slots[i] slots) to page dst[i] of this one."""
+        return pld_pages_copy(other.layers, self.layers, src, dst, slots, stream=stream,
+                              prepare=prepare)

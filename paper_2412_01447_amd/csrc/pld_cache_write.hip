@@ -1,6 +1,6 @@
 // pld_cache_write.hip -- a layer's new rows join its paged cache: per-head norms
 // and position rotation of queries and keys, quantisation, the page slots.
-#include "pld_cache.h"
+#include "pld_heads.h"
 
 namespace pld {
 
@@ -17,31 +17,6 @@ struct WriteArgs {
     uint16_t *out;
     int64_t os, orow;
 };
-
-// Sum and maximum over a group of G consecutive lanes (8, 16 or 32), the same
-// bits in each of them.
-template <int kCtrl>
-__device__ __forceinline__ float moved(float v) {
-    return __int_as_float(dpp_move<kCtrl, 0xf>(__float_as_int(v)));
-}
-template <int G>
-__device__ __forceinline__ float group_sum(float v) {
-    v += moved<kDppQuadSwap1>(v);
-    v += moved<kDppQuadSwap2>(v);
-    v += moved<kDppHalfMirror>(v);
-    if (G > 8) v += moved<kDppMirror>(v);
-    if (G > 16) v += __shfl_xor(v, 16);
-    return v;
-}
-template <int G>
-__device__ __forceinline__ float group_max(float v) {
-    v = fmaxf(v, moved<kDppQuadSwap1>(v));
-    v = fmaxf(v, moved<kDppQuadSwap2>(v));
-    v = fmaxf(v, moved<kDppHalfMirror>(v));
-    if (G > 8) v = fmaxf(v, moved<kDppMirror>(v));
-    if (G > 16) v = fmaxf(v, __shfl_xor(v, 16));
-    return v;
-}
 
 // D / 8 lanes a head's row, each holding two runs of four elements, t0 and t1:
 // with pairs of halves the runs are each other's partners (t1 = t0 + rot/2), so
@@ -81,74 +56,31 @@ __global__ __launch_bounds__(256) void cache_write_kernel(WriteArgs a) {
                                       : a.v + (int64_t)b * a.vs + (int64_t)i * a.vr;
     src += (int64_t)head * D;
     float x[8];
-    auto get = [](const uint16_t *p, float *o) {
-        const uint2 w = *reinterpret_cast<const uint2 *>(p);
-        o[0] = bf16_lo(w.x), o[1] = bf16_hi(w.x), o[2] = bf16_lo(w.y), o[3] = bf16_hi(w.y);
-    };
-    get(src + t0, x);
-    get(src + t1, x + 4);
+    get4(src + t0, x);
+    get4(src + t1, x + 4);
 
     const uint16_t *w = kind == 0 ? a.qw : kind == 1 ? a.kw : nullptr;
-    if (w) {
-        float s = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s = fmaf(x[e], x[e], s);
-        const float inv = 1.f / sqrtf(group_sum<G>(s) / (float)D + a.eps);
-        float g[8];
-        get(w + t0, g);
-        get(w + t1, g + 4);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * g[e];
-    }
+    if (w) norm_row<D>(x, w, t0, t1, a.eps);
     if (mine && ok) {
         const float *row = a.rope + pos * a.rope_stride + 4 * c;
         const float4 co = *reinterpret_cast<const float4 *>(row);
         const float4 si = *reinterpret_cast<const float4 *>(row + rot / 2);
         const float cs[4] = {co.x, co.y, co.z, co.w}, sn[4] = {si.x, si.y, si.z, si.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float &p = kHalves ? x[e] : x[2 * e];
-            float &r = kHalves ? x[e + 4] : x[2 * e + 1];
-            const float np = p * cs[e] - r * sn[e], nr = r * cs[e] + p * sn[e];
-            p = np;
-            r = nr;
-        }
+        turn_row<kHalves>(x, cs, sn);
     }
-    auto put = [](uint16_t *p, const float *o) {
-        *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
-    };
     if (kind == 0) {
         if (!ok)
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(0x7fc00000u);
         uint16_t *dst = a.out + (int64_t)b * a.os + (int64_t)i * a.orow + (int64_t)head * D;
-        put(dst + t0, x);
-        put(dst + t1, x + 4);
+        put4(dst + t0, x);
+        put4(dst + t1, x + 4);
         return;
     }
     if (!ok) return;
     char *dst = (kind == 1 ? a.c.k : a.c.v) + slot_at(a.c, page, pos, head);
-    if constexpr (kE4m3) {
-        float m = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(x[e]));
-        // a scale of at least the smallest normal number, so that the division stays finite
-        const float scale = fmaxf(group_max<G>(m) / kE4m3Max, 1.17549435e-38f);
-        // a quotient from the reciprocal, with what it leaves over put right: one that is rounded
-        // otherwise than x / scale differs from it by 2^-24, before the rounding to 2^-4
-        const float inv = 1.f / scale;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float y = x[e] * inv;
-            x[e] = fmaf(fmaf(-y, scale, x[e]), inv, y);
-        }
-        *reinterpret_cast<uint32_t *>(dst + t0) = pack_e4m3(x[0], x[1], x[2], x[3]);
-        *reinterpret_cast<uint32_t *>(dst + t1) = pack_e4m3(x[4], x[5], x[6], x[7]);
-        if (c == 0) (kind == 1 ? a.c.ks : a.c.vs)[scale_at(a.c, page, pos, head)] = scale;
-    } else {
-        put(reinterpret_cast<uint16_t *>(dst) + t0, x);
-        put(reinterpret_cast<uint16_t *>(dst) + t1, x + 4);
-    }
+    float *scale_to = kE4m3 ? (kind == 1 ? a.c.ks : a.c.vs) + scale_at(a.c, page, pos, head) : nullptr;
+    store_row<D, kE4m3>(x, dst, t0, t1, scale_to, c == 0);
 }
 
 template <int D>
