@@ -24,10 +24,15 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Werro
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", INCLUDE, "-I", CSRC]
 
+# Results of matrix instructions in the registers that vector instructions can use: with up to 512
+# registers a lane the compiler would move them to and fro at every step of a loop (prompts of heads of
+# 256: 76 registers spilled otherwise, and 1.8 times the time).
+SOURCE_FLAGS = {"pld_prompt_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+
 
 def _compile(src, verbose, build_dir, extra):
     obj = os.path.join(build_dir, os.path.basename(src) + ".o")
-    cmd = [HIPCC] + FLAGS + list(extra) + ["-c", src, "-o", obj]
+    cmd = [HIPCC] + FLAGS + SOURCE_FLAGS.get(os.path.basename(src), []) + list(extra) + ["-c", src, "-o", obj]
     if verbose:
         print(" ".join(cmd), flush=True)
     r = subprocess.run(cmd, capture_output=True, text=True)

@@ -4,6 +4,8 @@
 
 namespace pld {
 
+#define PLD_INLINE __attribute__((always_inline))   // of a lambda: its arrays are registers
+
 struct PromptArgs {
     const uint16_t *q, *k, *v;
     int64_t qr, kr, vr;
@@ -42,6 +44,12 @@ __device__ __forceinline__ float pair_sum(float v) {
     const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
+// A pointer that is the same in every lane, as a scalar.
+__device__ __forceinline__ const char *uniform(const char *p) {
+    const uint64_t v = (uint64_t)p;
+    return (const char *)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 |
+                          (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
+}
 __device__ __forceinline__ int wave_min(int v) {
 #pragma unroll
     for (int o = 32; o; o >>= 1) v = min(v, __shfl_xor(v, o));
@@ -56,10 +64,18 @@ __device__ __forceinline__ int wave_max(int v) {
 // 16 bytes a lane from base + off to LDS, lane after lane from `to` on, without a register between
 // (a lane's place in LDS is fixed, so the swizzle is in the addresses it reads).  The caller waits
 // (vmcnt): the compiler does not know of these loads.
+template <int kAhead>   // a distance of both addresses
 __device__ __forceinline__ void load_to_lds(uint32_t to, const void *base, uint32_t off) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3" ::"s"(to), "v"(off), "s"(base), "n"(kAhead) : "memory");
 }
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void load_far_to_lds(uint32_t to, const void *from) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+}
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0), in a form that the compiler counts by too
+    asm volatile("" ::: "memory");
+}
 __device__ __forceinline__ void block_barrier() {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -71,26 +87,26 @@ constexpr float kNoMax = -1e30f;   // of a query that has seen no key
 
 // kWaves waves of 32 kQT rows each: a tile of the rows of one key head, row m of all being query head
 // m % G of row m / G, over the keys that they see, kKeys at a time.
-template <int D, int kQT, int kWaves, int kKeys, bool kCap>
+constexpr int kKeys = 64;
+template <int D, int kQT, int kWaves>
 struct PromptTile {
     static constexpr int kRows = kWaves * 32 * kQT;
-    static constexpr int kPieces = D / 8;                    // 16-byte pieces of a key's row
+    // Keys and values in LDS: units of 16 rows by four pieces of 16 bytes, what one load instruction of a
+    // wave brings, piece by piece with row j of a unit's piece q at place j ^ 4 q.  Sixteen lanes that read
+    // a piece of as many rows, or two pieces of four, meet no bank twice, nor do 32, and where a
+    // lane reads changes from unit to unit by constants alone.
+    static constexpr int kUnits = D / 32;                    // of 16 rows
+    static constexpr int kGroup = kUnits * 1024;             // bytes of 16 rows
     static constexpr int kTileBytes = kKeys * D * 2;
-    static constexpr int kLoads = kKeys * kPieces / 64 / kWaves;   // instructions a wave for a tile's keys
-    static constexpr int kKT = kKeys / 32, kDT = D / 32;
-    static_assert(kLoads >= 1);
-
-    // Piece p of key j's row is at place p ^ key_swizzle(j) of it.
-    // keys: lanes read one piece of consecutive keys, 8 in 128 bytes of banks and 16 in 256;
-    // values: 16 lanes read two pieces of each of four keys, 32 four.
-    __device__ __forceinline__ static int key_swizzle(int j) { return D == 64 ? (j & 7) ^ (j >> 3 & 1) : j & 15; }
-    __device__ __forceinline__ static int value_swizzle(int j) { return D == 64 ? (j & 3) << 1 : (j & 1) * 10 ^ (j & 2) << 1; }
+    static constexpr int kLoads = kKeys / 16 * kUnits / kWaves;   // a wave's units of a tile, of the same rows
+    static constexpr int kDT = D / 32;
+    static_assert((kLoads == 1 || kLoads == 2 || kLoads == 4 || kLoads == 8) && kUnits % kLoads == 0);
 };
 
-template <int D, int kQT, int kWaves, int kKeys, bool kCap>
-__global__ __launch_bounds__(kWaves * 64) void prompt_attn_kernel(PromptArgs a) {
-    using T = PromptTile<D, kQT, kWaves, kKeys, kCap>;
-    constexpr int kKT = T::kKT, kDT = T::kDT, kLoads = T::kLoads;
+template <int D, int kQT, int kWaves, bool kCap>
+__global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_kernel(PromptArgs a) {
+    using T = PromptTile<D, kQT, kWaves>;
+    constexpr int kDT = T::kDT, kLoads = T::kLoads;
     __shared__ __attribute__((aligned(256))) char s_k[2][T::kTileBytes], s_v[2][T::kTileBytes];
     __shared__ int s_range[kWaves][2];
     __shared__ uint32_t s_bad[2];
@@ -146,186 +162,134 @@ __global__ __launch_bounds__(kWaves * 64) void prompt_attn_kernel(PromptArgs a) 
     block_lo = __builtin_amdgcn_readfirstlane(block_lo);
     block_hi = __builtin_amdgcn_readfirstlane(block_hi);
     if (block_lo >= block_hi) return;
-    const int n = (block_hi - block_lo + kKeys - 1) / kKeys;   // tiles of keys
 
-    // ---- loads: instruction i of a wave brings pieces (wave kLoads + i) 64 .. + 63 of a tile
-    const uint16_t *kbase = a.k + (int64_t)kv * D, *vbase = a.v + (int64_t)kv * D;
-    auto place = [&](int i, int &j, int &p) {
-        const int at = (wave * kLoads + i) * 64 + lane;
-        j = at / T::kPieces, p = at % T::kPieces;
+    // ---- loads: a wave brings kLoads units of the same 16 rows, a lane 16 bytes of one row of each
+    const int unit0 = wave * kLoads;
+    const int j0 = unit0 / T::kUnits * 16 + ((lane & 15) ^ (lane >> 4) * 4);
+    const int64_t byte0 = unit0 % T::kUnits * 64;
+    const char *kbase = (const char *)(a.k + (int64_t)kv * D) + byte0, *vbase = (const char *)(a.v + (int64_t)kv * D) + byte0;
+    const uint32_t kstride = (uint32_t)(a.kr * 2), vstride = (uint32_t)(a.vr * 2), piece = (lane >> 4) * 16;
+    const uint32_t koff = (uint32_t)j0 * kstride + piece, voff = (uint32_t)j0 * vstride + piece;
+    const uint32_t k_lds = (uint32_t)(uintptr_t)(lds_ptr)&s_k[0][0] + unit0 * 1024;
+    const uint32_t v_lds = (uint32_t)(uintptr_t)(lds_ptr)&s_v[0][0] + unit0 * 1024;
+    // keys or values of 64 rows from `from` on to a buffer
+    auto fetch_at = [&](const char *from, int buf, bool values) PLD_INLINE {
+        const uint32_t to = (values ? v_lds : k_lds) + buf * T::kTileBytes, off = values ? voff : koff;
+        load_to_lds<0>(to, from, off);
+        if constexpr (kLoads > 1) load_to_lds<64>(to + 960, from, off);
+        if constexpr (kLoads > 2) load_to_lds<128>(to + 1920, from, off), load_to_lds<192>(to + 2880, from, off);
+        if constexpr (kLoads > 4) {
+            load_to_lds<256>(to + 3840, from, off), load_to_lds<320>(to + 4800, from, off);
+            load_to_lds<384>(to + 5760, from, off), load_to_lds<448>(to + 6720, from, off);
+        }
     };
-    uint32_t koff[kLoads], voff[kLoads];
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-        int j, p;
-        place(i, j, p);
-        koff[i] = (uint32_t)j * (uint32_t)(a.kr * 2) + (p ^ T::key_swizzle(j)) * 16;
-        voff[i] = (uint32_t)j * (uint32_t)(a.vr * 2) + (p ^ T::value_swizzle(j)) * 16;
-    }
-    const uint32_t k_lds = (uint32_t)(uintptr_t)(lds_ptr)&s_k[0][0], v_lds = (uint32_t)(uintptr_t)(lds_ptr)&s_v[0][0];
-    // tile i of keys or values to its buffer; the last key stands in for those past the block's
-    auto fetch = [&](int i, bool values) {
-        const int k0 = block_lo + i * kKeys;
-        const uint16_t *base = values ? vbase + k0 * a.vr : kbase + k0 * a.kr;
-        const uint32_t to = (values ? v_lds : k_lds) + (i & 1) * T::kTileBytes + wave * kLoads * 1024;
+    // the same from row k0 on; for rows outside the block's the nearest one stands in
+    auto fetch = [&](int k0, int buf, bool values) PLD_INLINE {
+        const uint32_t stride = values ? vstride : kstride;
+        const char *base = values ? vbase : kbase;
         if (k0 + kKeys <= block_hi) {
-#pragma unroll
-            for (int x = 0; x < kLoads; ++x) load_to_lds(to + x * 1024, base, values ? voff[x] : koff[x]);
+            fetch_at(uniform(base + (int64_t)k0 * stride), buf, values);
         } else {
-            const uint32_t stride = (uint32_t)((values ? a.vr : a.kr) * 2);
+            const uint32_t to = (values ? v_lds : k_lds) + buf * T::kTileBytes;
+            const int row = min(k0 + j0, block_hi - 1);
 #pragma unroll
-            for (int x = 0; x < kLoads; ++x) {
-                int j, p;
-                place(x, j, p);
-                const uint32_t off = values ? voff[x] : koff[x];
-                load_to_lds(to + x * 1024, base, off - (uint32_t)(j - min(j, block_hi - 1 - k0)) * stride);
-            }
+            for (int x = 0; x < kLoads; ++x) load_far_to_lds(to + x * 1024, base + (int64_t)row * stride + piece + x * 64);
         }
     };
 
-    // ---- the products
+    // ---- the products, of 32 keys at a time: `part` of a tile
     f32x16_t o[kQT][kDT];
     float mx[kQT], l[kQT];
-    auto scores = [&](int i, f32x16_t (&s)[kQT][kKT]) {
-        const char *buf = s_k[i & 1];
+    const int c16 = lane & 15, odd16 = lane >> 4 & 1;
+    int kat[2], vat[2];   // of even and odd steps of 16 elements; of the first and second eight of 16 rows
 #pragma unroll
-        for (int kt = 0; kt < kKT; ++kt) {
-            const int j = kt * 32 + (lane & 31);
-#pragma unroll
-            for (int t = 0; t < kQT; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[t][kt][r] = 0.f;
-#pragma unroll
-            for (int x = 0; x < D / 16; ++x) {
-                const auto f = *reinterpret_cast<const bf16x8_t *>(buf + j * D * 2 + ((2 * x + h) ^ T::key_swizzle(j)) * 16);
-#pragma unroll
-                for (int t = 0; t < kQT; ++t) s[t][kt] = mfma32(f, qf[t][x], s[t][kt]);
-            }
-        }
+    for (int x = 0; x < 2; ++x) {
+        const int q = odd16 * 2 + (c16 >> 1 & 1);
+        kat[x] = odd16 * T::kGroup + (2 * x + h) * 256 + (c16 ^ (8 * x + 4 * h)) * 16;
+        vat[x] = q * 256 + ((8 * x + 4 * h + (c16 >> 2)) ^ 4 * q) * 16 + (c16 & 1) * 8;
+    }
+    auto key_operand = [&](const char *buf, int part, int x) PLD_INLINE {   // elements 16 x .. of 32 keys
+        return *reinterpret_cast<const bf16x8_t *>(buf + part * 2 * T::kGroup + x / 2 * 1024 + kat[x & 1]);
     };
-    auto value_operand = [&](const char *buf, int x, int dt) {   // 16 keys from 16 x on
-        const int c = lane & 15, j = 16 * x + 4 * h + (c >> 2), p = dt * 4 + (lane >> 4 & 1) * 2 + (c >> 1 & 1);
-        auto read = [&](int key) {
+    auto value_operand = [&](const char *buf, int x, int dt) PLD_INLINE {   // 16 keys from 16 x on
+        auto read = [&](int at) PLD_INLINE {
             return __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4_t *>(
-                (lds_ptr)(buf + key * D * 2 + (p ^ T::value_swizzle(key)) * 16 + (c & 1) * 8)));
+                (lds_ptr)(buf + x * T::kGroup + dt * 1024 + at)));
         };
-        const s16x4_t x0 = read(j), x1 = read(j + 8);
+        const s16x4_t x0 = read(vat[0]), x1 = read(vat[1]);
         return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    // Scores of tile i into the output: weights 2^(s c - m) against the running maximum m, which is
-    // raised where a score is kSlack above it.
-    auto attend = [&](int i, f32x16_t (&s)[kQT][kKT], bool careful) {
-        const int k0 = block_lo + i * kKeys;
-        float c = a.c1;
-        if constexpr (kCap) {
-            float w = 0.f;
+    auto scores = [&](const char *buf, int part, f32x16_t (&s)[kQT]) PLD_INLINE {
 #pragma unroll
-            for (int t = 0; t < kQT; ++t)
+        for (int t = 0; t < kQT; ++t)
 #pragma unroll
-                for (int kt = 0; kt < kKT; ++kt) {
-                    s[t][kt] *= c;
+            for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) w = fmaxf(w, fabsf(s[t][kt][r]));
-                }
-            const bool far = __any(w >= a.cap_near);
+        for (int x = 0; x < D / 16; ++x) {
+            const bf16x8_t f = key_operand(buf, part, x);
 #pragma unroll
-            for (int t = 0; t < kQT; ++t)
-#pragma unroll
-                for (int kt = 0; kt < kKT; ++kt)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        s[t][kt][r] = far ? soft_cap(s[t][kt][r], a.cap, a.cap_x2, a.cap_near, a.inv2_log2e)
-                                          : soft_cap_near(s[t][kt][r], a.inv2_log2e);
-            c = 1.f;
+            for (int t = 0; t < kQT; ++t) s[t] = mfma32(f, qf[t][x], s[t]);
         }
-        if (careful) {
-            const uint64_t bad = ((uint64_t)s_bad[1] << 32 | s_bad[0]) >> 4 * h;
+    };
+    auto largest = [&](const f32x16_t &s) PLD_INLINE {
+        float top = -INFINITY;
 #pragma unroll
-            for (int t = 0; t < kQT; ++t)
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[r]);
+        return top;
+    };
+    const float c = kCap ? 1.f : a.c1;   // from scores as they are kept to log2 units
+    auto cap = [&](f32x16_t (&s)[kQT]) PLD_INLINE {
+        float w = 0.f;
 #pragma unroll
-                for (int kt = 0; kt < kKT; ++kt)
+        for (int t = 0; t < kQT; ++t)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (bad >> (kt * 32 + 8 * (r / 4) + r % 4) & 1) s[t][kt][r] = __uint_as_float(0x7fc00000u);
-        }
-        if (k0 < full_lo || k0 + kKeys > full_hi) {
+            for (int r = 0; r < 16; ++r) w = fmaxf(w, fabsf(s[t][r]));
+        // few scores come to a third of the cap as a rule: one branch for the wave
+        const bool far = __any(w * a.c1 >= a.cap_near);
 #pragma unroll
-            for (int t = 0; t < kQT; ++t) {
-                const int from = lo[t] - k0 - 4 * h, count = hi[t] - lo[t];
+        for (int t = 0; t < kQT; ++t)
 #pragma unroll
-                for (int kt = 0; kt < kKT; ++kt)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        s[t][kt][r] = (uint32_t)(kt * 32 + 8 * (r / 4) + r % 4 - from) < (uint32_t)count ? s[t][kt][r] : -INFINITY;
+            for (int r = 0; r < 16; ++r) {
+                const float x = s[t][r] * a.c1;
+                s[t][r] = far ? soft_cap(x, a.cap, a.cap_x2, a.cap_near, a.inv2_log2e) : soft_cap_near(x, a.inv2_log2e);
             }
-        }
+    };
+    auto mask = [&](int k0, f32x16_t (&s)[kQT]) PLD_INLINE {
 #pragma unroll
         for (int t = 0; t < kQT; ++t) {
-            float top = -INFINITY;
+            const int from = lo[t] - k0 - 4 * h, count = hi[t] - lo[t];
 #pragma unroll
-            for (int kt = 0; kt < kKT; ++kt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][kt][r]);
-            top *= c;
-            if (__any(top > mx[t] + kSlack)) {
-                // (a row by its own scores: its bits do not go by its neighbours')
-                const float all = pair_max(top), mn = all > mx[t] + kSlack ? all : mx[t];
-                const float f = __builtin_amdgcn_exp2f(mx[t] - mn);
-                mx[t] = mn;
-                l[t] *= f;
-#pragma unroll
-                for (int dt = 0; dt < kDT; ++dt) o[t][dt] *= f;
-            }
-#pragma unroll
-            for (int kt = 0; kt < kKT; ++kt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[t][kt][r] = __builtin_amdgcn_exp2f(fmaf(s[t][kt][r], c, -mx[t]));
-                    l[t] += s[t][kt][r];
-                }
-        }
-        const char *buf = s_v[i & 1];
-#pragma unroll
-        for (int x = 0; x < kKeys / 16; ++x) {
-            bf16x8_t p[kQT];   // rounded to bf16, as the product takes them: half a step (2^-8) of each term
-#pragma unroll
-            for (int t = 0; t < kQT; ++t) {
-                const f32x16_t &w = s[t][x / 2];
-                const int r = x % 2 * 8;
-                p[t] = __builtin_bit_cast(bf16x8_t, make_uint4(pack_bf16(w[r], w[r + 1]), pack_bf16(w[r + 2], w[r + 3]),
-                                                               pack_bf16(w[r + 4], w[r + 5]), pack_bf16(w[r + 6], w[r + 7])));
-            }
-#pragma unroll
-            for (int dt = 0; dt < kDT; ++dt) {
-                const bf16x8_t f = value_operand(buf, x, dt);
-#pragma unroll
-                for (int t = 0; t < kQT; ++t) o[t][dt] = mfma32(f, p[t], o[t][dt]);
-            }
-            __builtin_amdgcn_sched_barrier(0);
+            for (int r = 0; r < 16; ++r)
+                s[t][r] = (uint32_t)(8 * (r / 4) + r % 4 - from) < (uint32_t)count ? s[t][r] : -INFINITY;
         }
     };
-    // What is not finite in tile i's values becomes 0, and its keys a bit each of s_bad (the block).
-    auto clean = [&](int i) {
-        if (threadIdx.x < 2) s_bad[threadIdx.x] = 0;
-        __syncthreads();
-        char *buf = s_v[i & 1];
-        for (int at = threadIdx.x; at < kKeys * T::kPieces; at += kWaves * 64) {
-            uint16_t *e = reinterpret_cast<uint16_t *>(buf + at * 16);
-            bool hit = false;
+    // The running maximum m is raised where a score is kSlack above it: score_high says whether any row's is,
+    // raise goes by each row's own scores (its bits do not go by its neighbours').
+    auto score_high = [&](const float (&top)[kQT]) PLD_INLINE {
+        float over = fmaf(top[0], c, -mx[0]);
 #pragma unroll
-            for (int x = 0; x < 8; ++x)
-                if ((e[x] & 0x7f80) == 0x7f80) e[x] = 0, hit = true;
-            const int j = at / T::kPieces;
-            if (hit) atomicOr(&s_bad[j >> 5], 1u << (j & 31));
-        }
-        __syncthreads();
+        for (int t = 1; t < kQT; ++t) over = fmaxf(over, fmaf(top[t], c, -mx[t]));
+        return __ballot(over > kSlack);
     };
-
-    // ---- the keys.  A weight of 0 times a value that is not finite would reach rows that do not see it:
-    // where the output holds such a number at the end, all is done once more, with those values as 0
-    // and NaN for the rows that see them.
-    bool careful = false;
-    for (;;) {
+    auto raise = [&](const float (&top)[kQT]) PLD_INLINE {
+#pragma unroll
+        for (int t = 0; t < kQT; ++t) {
+            const float all = pair_max(top[t] * c), mn = fmaf(1.f, all, -mx[t]) > kSlack ? all : mx[t];
+            const float f = __builtin_amdgcn_exp2f(mx[t] - mn);
+            mx[t] = mn;
+            l[t] *= f;
+#pragma unroll
+            for (int dt = 0; dt < kDT; ++dt) o[t][dt] *= f;
+        }
+    };
+    // Weights 2^(s c - m), rounded to bf16 in pairs, as the product takes them: half a step (2^-8) of
+    // each term.  The sum is of the unrounded ones.
+    auto weigh = [&](float s, int t) PLD_INLINE {
+        const float w = __builtin_amdgcn_exp2f(fmaf(s, c, -mx[t]));
+        l[t] += w;
+        return w;
+    };
+    auto begin = [&]() PLD_INLINE {
 #pragma unroll
         for (int t = 0; t < kQT; ++t) {
             mx[t] = kNoMax, l[t] = 0.f;
@@ -334,37 +298,228 @@ __global__ __launch_bounds__(kWaves * 64) void prompt_attn_kernel(PromptArgs a) 
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[t][dt][r] = 0.f;
         }
-        fetch(0, false);
-        fetch(0, true);
-        for (int i = 0; i < n; ++i) {
-            wait_loads();
-            block_barrier();   // tile i is there, and all have done with tile i - 1
-            if (careful) clean(i);
-            if (i + 1 < n) {
-                fetch(i + 1, false);
-                fetch(i + 1, true);
-            }
-            const int k0 = block_lo + i * kKeys;
-            if (k0 < wave_hi && k0 + kKeys > wave_lo) {
-                f32x16_t s[kQT][kKT];
-                scores(i, s);
-                attend(i, s, careful);
-            }
-        }
-        bool odd = false;
+    };
+    auto seen = [&](int k0) PLD_INLINE { return k0 < wave_hi && k0 + 32 > wave_lo; };
+
+    // ---- the keys, 32 at a time.  A step takes the weights of its scores while the products of the next
+    // step's are under way, and reads values, and then the step's after it keys, from LDS for the products
+    // that follow: each has a part of what the vector units and LDS do beside them, in this order.
+    constexpr int kX = D / 16, kLead = kX < 8 ? kX : 8;   // products of a kind; values read so many products ahead
+    f32x16_t s0[kQT], s1[kQT];
+    bf16x8_t kf[kX];                 // keys of the next scores
+    float top[kQT];
+    uint64_t too_high = 0;           // score_high(top)
+    auto first_scores = [&](f32x16_t (&s)[kQT]) PLD_INLINE {
 #pragma unroll
         for (int t = 0; t < kQT; ++t) {
-            l[t] = pair_sum(l[t]);
-            float x = 0.f;
 #pragma unroll
-            for (int dt = 0; dt < kDT; ++dt)
+            for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) x = fmaf(o[t][dt][r], 0.f, x);
-            odd |= !(x == 0.f) || !(l[t] < INFINITY);
+            for (int x = 0; x < kX; ++x) s[t] = mfma32(kf[x], qf[t][x], s[t]);
+            top[t] = largest(s[t]);
         }
-        if (careful || !__syncthreads_or(odd)) break;
-        careful = true;
+        too_high = score_high(top);
+    };
+    auto read_keys = [&](const char *buf, int part) PLD_INLINE {
+#pragma unroll
+        for (int x = 0; x < kX; ++x) kf[x] = key_operand(buf, part, x);
+    };
+    // Weights of s times values at (vbuf, part); the next step's scores into `ahead`; keys at (kbuf, part).
+    auto products = [&](const char *vbuf, const char *kbuf, int part, f32x16_t (&s)[kQT], f32x16_t (&ahead)[kQT]) PLD_INLINE {
+        // A slot is a product; what goes with it is a constant of its number z.
+        constexpr int kZ = kX * kQT;                       // products of scores, and as many of values
+        bf16x8_t vf[kLead];
+        float w0[kQT];
+        uint32_t w[kQT][8];
+        auto weights = [&](int z) PLD_INLINE {             // in the first three quarters
+#pragma unroll
+            for (int e = 0; e < 16 * kQT; ++e)
+                if (e * 3 * kX / 32 == z) {
+                    const int r = e / kQT, t = e % kQT;
+                    const float x = weigh(s[t][r], t);
+                    if (r % 2) w[t][r / 2] = pack_bf16(w0[t], x);
+                    else w0[t] = x;
+                }
+        };
+        auto read_value = [&](int x) PLD_INLINE { vf[x % kLead] = value_operand(vbuf, part * 2 + x / kDT, x % kDT); };
+        float m[kQT];
+        // (past the last keys: of whatever is there, and not used)
+#pragma unroll
+        for (int z = 0; z < kZ; ++z) {
+            const int x = z / kQT, t = z % kQT;
+            if (x == 0)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) ahead[t][r] = 0.f;
+            ahead[t] = mfma32(kf[x], qf[t][x], ahead[t]);
+            if (t == 0 && x >= kX - kLead) read_value(x - (kX - kLead));
+            weights(z);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int z = 0; z < kZ; ++z) {
+            const int x = z / kQT, t = z % kQT;
+            const uint32_t *p = w[t] + x / kDT * 4;
+            o[t][x % kDT] = mfma32(vf[x % kLead], __builtin_bit_cast(bf16x8_t, make_uint4(p[0], p[1], p[2], p[3])), o[t][x % kDT]);
+            if (t == kQT - 1) {
+                if (x + kLead < kX) read_value(x + kLead);
+                kf[x] = key_operand(kbuf, part, x);
+            }
+            weights(kZ + z);
+            constexpr int kFrom = kZ / 4, kEach = 16 * kQT / (kZ / 2);   // the next maximum
+            if (!kCap && z >= kFrom && z < kFrom + kZ / 2)
+#pragma unroll
+                for (int e = (z - kFrom) * kEach; e < (z - kFrom + 1) * kEach; ++e) {
+                    const int u = e / 16, r = e % 16;
+                    m[u] = fmaxf(r ? m[u] : -INFINITY, ahead[u][r]);
+                }
+            if (!kCap && z == kFrom + kZ / 2 - 1) {
+#pragma unroll
+                for (int u = 0; u < kQT; ++u) {
+                    asm volatile("" : "+v"(m[u]));   // taken here, among the products, and not where it is used
+                    top[u] = m[u];
+                }
+                too_high = score_high(top);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // values of keys k0 .. at (vbuf, part); keys of k0 + 64 .. at (kbuf, part)
+    auto step = [&](int k0, const char *vbuf, const char *kbuf, int part, f32x16_t (&s)[kQT], f32x16_t (&ahead)[kQT]) PLD_INLINE {
+        if (seen(k0)) {
+            const bool masked = k0 < full_lo || k0 + 32 > full_hi;
+            if (kCap) cap(s);
+            if (masked) mask(k0, s);
+            if (kCap || masked) {
+#pragma unroll
+                for (int t = 0; t < kQT; ++t) top[t] = largest(s[t]);
+                too_high = score_high(top);
+            }
+            if (too_high) raise(top);
+            products(vbuf, kbuf, part, s, ahead);
+        } else {
+            if (seen(k0 + 32)) first_scores(ahead);
+            if (seen(k0 + 64)) read_keys(kbuf, part);
+        }
+    };
+    // K of tile i + 2 and V of i + 1 are on their way during tile i.
+    auto tile = [&](int k0, auto odd) PLD_INLINE {
+        constexpr int kOdd = decltype(odd)::value;
+        wait_loads();
+        block_barrier();   // what tile i reads is there, and all have done with tile i - 1
+        if (k0 + 2 * kKeys < block_hi) fetch(k0 + 2 * kKeys, kOdd, false);
+        if (k0 + kKeys < block_hi) fetch(k0 + kKeys, !kOdd, true);
+        step(k0, s_v[kOdd], s_k[!kOdd], 0, s0, s1);
+        step(k0 + 32, s_v[kOdd], s_k[!kOdd], 1, s1, s0);
+    };
+    // a tile that all rows of the wave see whole, and two more behind it
+    auto whole_tile = [&](int k0, auto odd) PLD_INLINE {
+        constexpr int kOdd = decltype(odd)::value;
+        wait_loads();
+        block_barrier();
+        fetch_at(kbase + (int64_t)(k0 + 2 * kKeys) * kstride, kOdd, false);
+        fetch_at(vbase + (int64_t)(k0 + kKeys) * vstride, !kOdd, true);
+        auto whole = [&](int part, f32x16_t (&s)[kQT], f32x16_t (&ahead)[kQT]) PLD_INLINE {
+            if constexpr (kCap) {
+                cap(s);
+#pragma unroll
+                for (int t = 0; t < kQT; ++t) top[t] = largest(s[t]);
+                too_high = score_high(top);
+            }
+            if (too_high) raise(top);
+            products(s_v[kOdd], s_k[!kOdd], part, s, ahead);
+        };
+        whole(0, s0, s1);
+        whole(1, s1, s0);
+    };
+    begin();
+    fetch(block_lo, 0, false);
+    wait_loads();
+    block_barrier();
+    if (block_lo + kKeys < block_hi) fetch(block_lo + kKeys, 1, false);
+    fetch(block_lo, 0, true);
+    read_keys(s_k[0], 0);
+    first_scores(s0);
+    read_keys(s_k[0], 1);
+    for (int k0 = block_lo; k0 < block_hi; k0 += 2 * kKeys) {
+        for (; k0 >= full_lo && k0 + 2 * kKeys <= full_hi && k0 + 4 * kKeys <= block_hi; k0 += 2 * kKeys) {
+            whole_tile(k0, std::integral_constant<int, 0>{});
+            whole_tile(k0 + kKeys, std::integral_constant<int, 1>{});
+        }
+        tile(k0, std::integral_constant<int, 0>{});
+        if (k0 + kKeys < block_hi) tile(k0 + kKeys, std::integral_constant<int, 1>{});
     }
+
+    // A weight of 0 times a value that is not finite reaches rows that do not see it: where the output
+    // holds such a number, all is done once more, a part after the other, with those values as 0 and NaN
+    // for the rows that see them.
+    bool odd = false;
+#pragma unroll
+    for (int t = 0; t < kQT; ++t) {
+        float x = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < kDT; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x = fmaf(o[t][dt][r], 0.f, x);
+        odd |= !(x == 0.f) || !(l[t] < INFINITY);
+    }
+    if (__syncthreads_or(odd)) {
+        begin();
+#pragma unroll 1
+        for (int key0 = block_lo; key0 < block_hi; key0 += kKeys) {
+            fetch(key0, 0, false);
+            fetch(key0, 0, true);
+            if (threadIdx.x < 2) s_bad[threadIdx.x] = 0;
+            wait_loads();
+            __syncthreads();
+            for (int at = threadIdx.x; at < kKeys * D / 8; at += kWaves * 64) {
+                uint16_t *e = reinterpret_cast<uint16_t *>(s_v[0] + at * 16);
+                bool hit = false;
+#pragma unroll
+                for (int x = 0; x < 8; ++x)
+                    if ((e[x] & 0x7f80) == 0x7f80) e[x] = 0, hit = true;
+                const int j = at / 64 / T::kUnits * 16 + ((at & 15) ^ (at >> 4 & 3) * 4);
+                if (hit) atomicOr(&s_bad[j >> 5], 1u << (j & 31));
+            }
+            __syncthreads();
+#pragma unroll 1
+            for (int part = 0; part < kKeys / 32; ++part) {
+                const int k0 = key0 + part * 32;
+                if (!seen(k0)) continue;
+                const uint32_t bad = s_bad[part] >> 4 * h;
+                scores(s_k[0], part, s0);
+                if (kCap) cap(s0);
+#pragma unroll
+                for (int t = 0; t < kQT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (bad >> (8 * (r / 4) + r % 4) & 1) s0[t][r] = __uint_as_float(0x7fc00000u);
+                mask(k0, s0);
+#pragma unroll
+                for (int t = 0; t < kQT; ++t) top[t] = largest(s0[t]);
+                raise(top);
+                uint32_t w[kQT][8];
+#pragma unroll
+                for (int t = 0; t < kQT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float w0 = weigh(s0[t][2 * i], t), w1 = weigh(s0[t][2 * i + 1], t);
+                        w[t][i] = pack_bf16(w0, w1);
+                    }
+#pragma unroll
+                for (int x = 0; x < D / 16; ++x) {
+                    const bf16x8_t f = value_operand(s_v[0], part * 2 + x / kDT, x % kDT);
+#pragma unroll
+                    for (int t = 0; t < kQT; ++t) {
+                        const uint32_t *p = w[t] + x / kDT * 4;
+                        o[t][x % kDT] = mfma32(f, __builtin_bit_cast(bf16x8_t, make_uint4(p[0], p[1], p[2], p[3])), o[t][x % kDT]);
+                    }
+                }
+            }
+            __syncthreads();
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < kQT; ++t) l[t] = pair_sum(l[t]);
 
     // ---- out: a lane has four consecutive elements of every eight; the two lanes of a query trade
     // halves, so that each stores eight
@@ -389,15 +544,15 @@ __global__ __launch_bounds__(kWaves * 64) void prompt_attn_kernel(PromptArgs a) 
     }
 }
 
-template <int D, int kQT, int kWaves, int kKeys>
+template <int D, int kQT, int kWaves>
 static void launch_prompt(PromptArgs &a, hipStream_t s) {
-    a.tiles = ((int64_t)a.p.N * a.G + PromptTile<D, kQT, kWaves, kKeys, false>::kRows - 1) /
-              PromptTile<D, kQT, kWaves, kKeys, false>::kRows;
+    constexpr int rows = PromptTile<D, kQT, kWaves>::kRows;
+    a.tiles = ((int64_t)a.p.N * a.G + rows - 1) / rows;
     const dim3 grid = wide_grid(a.tiles * a.heads);
     if (a.cap > 0.f)
-        hipLaunchKernelGGL((prompt_attn_kernel<D, kQT, kWaves, kKeys, true>), grid, dim3(kWaves * 64), 0, s, a);
+        hipLaunchKernelGGL((prompt_attn_kernel<D, kQT, kWaves, true>), grid, dim3(kWaves * 64), 0, s, a);
     else
-        hipLaunchKernelGGL((prompt_attn_kernel<D, kQT, kWaves, kKeys, false>), grid, dim3(kWaves * 64), 0, s, a);
+        hipLaunchKernelGGL((prompt_attn_kernel<D, kQT, kWaves, false>), grid, dim3(kWaves * 64), 0, s, a);
 }
 
 }  // namespace pld
@@ -435,11 +590,19 @@ extern "C" int pld_prompt_attn(const uint16_t *q, int64_t q_row_stride, const ui
     a.window = window;
     a.out = out, a.orow = o_row_stride, a.lse = lse;
     const hipStream_t s = (hipStream_t)stream;
+    // Blocks of 256 rows read keys and values half as often; blocks of 128, two a CU, wait less for each
+    // other and share out evener.  32 heads over 8 of 128: one sequence of 1024 rows 29.5 and 23.1 us, of 2048
+    // 53.0 and 54.5, of 16384 1927 and 2206; 64 of 300 150 and 137, 16 of 1000 193 and 198.  Heads of
+    // 64, whose vector instructions bound them: 2 x 8192 605 and 615, 2048 37 and 32, capped in a window
+    // of 1000 245 and 183.
+    const int64_t wide = ((int64_t)N * a.G + 255) / 256 * heads;
     if (head_dim == 64)
-        launch_prompt<64, 1, 8, 64>(a, s);
+        launch_prompt<64, 1, 4>(a, s);
+    else if (head_dim == 128 && wide >= 256 && N >= (int64_t)B * 512)
+        launch_prompt<128, 1, 8>(a, s);
     else if (head_dim == 128)
-        launch_prompt<128, 1, 8, 64>(a, s);
+        launch_prompt<128, 1, 4>(a, s);
     else
-        launch_prompt<256, 1, 4, 32>(a, s);
+        launch_prompt<256, 1, 4>(a, s);
     return hipGetLastError() == hipSuccess ? PLD_OK : PLD_ERR_LAUNCH;
 }
