@@ -30,7 +30,7 @@ __all__ = [
     "pld_model_version", "pld_cache_write", "pld_cache_attn", "pld_cache_attn_workspace_bytes",
     "pld_cache_attn_rows", "pld_token_logprobs", "pld_token_logprobs_workspace_bytes", "PLD_E4M3",
     "PLD_ROPE_HALVES", "PLD_ROPE_NEIGHBOURS", "PLD_MAX_TOP",
-    "pld_prompt_version", "pld_cache_write_packed", "pld_prompt_attn", "PageLayers",
+    "pld_prompt_version", "pld_cache_write_packed", "pld_prompt_attn", "PageLayers", "PageTable",
     "pld_pages_workspace_bytes", "pld_pages_take", "pld_pages_free", "pld_pages_fork",
     "pld_pages_compact", "pld_pages_copy", "PLD_MAX_PACKED_ROWS", "PLD_MAX_AXES", "PLD_MAX_LAYERS",
     "PLD_MAX_PAGES", "PLD_MAX_PAGE_ENTRIES",
@@ -909,105 +909,113 @@ class PageLayers:
 
     def __init__(self, k_caches, v_caches, k_scales=None, v_scales=None):
         torch = _torch or _th()
-        if len(k_caches) != len(v_caches) or any(
-                s is not None and len(s) != len(k_caches) for s in (k_scales, v_scales)):
-            raise TypeError("as many v_caches (and scales) as k_caches")
         self.tensors = [tuple(k_caches), tuple(v_caches), k_scales and tuple(k_scales),
                         v_scales and tuple(v_scales)]
         self.count = len(k_caches)
-        none = torch.empty((1, 1), dtype=torch.int32, device=k_caches[0].device if self.count else "cpu")
+        if any(x is not None and len(x) != self.count for x in self.tensors[1:]):
+            raise TypeError("as many v_caches (and scales) as k_caches")
+        every = [t for x in self.tensors if x for t in x]
+        for t in every:
+            if not t.is_cuda or t.get_device() != every[0].get_device():
+                raise TypeError("the caches must be on one device: " + ", ".join(
+                    sorted({str(t.device) for t in every})))
+        self.any = every[0] if every else None      # (says which device)
+        table = torch.empty((1, 1), dtype=torch.int32, device=self.any.device) if every else None
         self.caches = (_Cache * max(1, self.count))(*(
-            _cache_of(k, v, none, k_scales and k_scales[i], v_scales and v_scales[i], 1)
-            if none.is_cuda else _layer_off(k) for i, (k, v) in enumerate(zip(k_caches, v_caches))))
-        self.each = [t for ts in self.tensors if ts for t in ts]
-        if self.count and len({t.get_device() for t in self.each}) > 1:
-            raise TypeError("caches on several devices")
+            _cache_of(k, v, table, k_scales and k_scales[i], v_scales and v_scales[i], 1)
+            for i, (k, v) in enumerate(zip(k_caches, v_caches))))
         if len({(c.dtype, c.scale_page_stride, c.page_stride, c.slot_stride, c.head_stride, c.num_pages,
                  c.page_size, c.heads, c.head_dim) for c in self.caches}) > 1:
             raise TypeError("the layers' caches must be alike in type, shape and strides")
 
 
-def _layer_off(t):
-    raise TypeError(f"expected device tensors, got one on {t.device}")
+class PageTable:
+    """A pool of the pld_pages_* calls, marshalled once: its table int32 [seqs][pages], references
+    int32 [num_pages] and slots a page.  The tensors are kept."""
+
+    def __init__(self, table, refs, page_size):
+        torch = _torch or _th()
+        ts = _need(table, torch.int32, "table", 2)
+        _need(refs, torch.int32, "refs", 1)
+        if refs.get_device() != table.get_device():
+            raise TypeError("table and refs are on different devices")
+        self.table, self.refs, self.page_size = table, refs, page_size
+        # (the stride of a single row is never used)
+        stride = max(ts[0], table.shape[1]) if table.shape[0] == 1 else ts[0]
+        self.pool = _Pool(_ptr(table), stride, _ptr(refs), table.shape[0], table.shape[1], refs.shape[0],
+                          page_size)
 
 
-def _pool_of(table, refs, page_size):
-    """struct pld_pool of the table int32 [seqs][pages] and the references int32 [num_pages]."""
-    torch = _torch or _th()
-    ts = _need(table, torch.int32, "table", 2)
-    _ints(refs, "refs", refs.numel())
-    return _Pool(_ptr(table), max(ts[0], table.shape[1]) if table.shape[0] == 1 else ts[0], _ptr(refs),
-                 table.shape[0], table.shape[1], refs.numel(), page_size)
+def pld_pages_workspace_bytes(pages, count):
+    """For calls of `count` sequences or forks on a pool (a PageTable)."""
+    return int(_load().pld_pages_workspace_bytes(pages.pool, count))
 
 
-def pld_pages_workspace_bytes(table, refs, page_size, count):
-    return int(_load().pld_pages_workspace_bytes(_pool_of(table, refs, page_size), count))
-
-
-def pld_pages_take(table, refs, page_size, seq, need, status, workspace, stream=None, prepare=False):
+def pld_pages_take(pages, seq, need, status, workspace, stream=None, prepare=False):
     """The entries of sequences seq int32 [count] for positions below need[i] that name no page get
-    free ones of the pool (table int32 [seqs][pages], refs int32 [num_pages])."""
-    _on_one_device(stream, table, refs, seq, need, status, workspace)
+    free ones of the pool `pages` (a PageTable)."""
+    _on_one_device(stream, pages.refs, seq, need, status, workspace)
     count = seq.numel()
-    for t, name in ((seq, "seq"), (need, "need"), (status, "status")):
-        _ints(t, name, count)
-    return _run("pld_pages_take", (
-        _pool_of(table, refs, page_size), _ptr(seq), _ptr(need), count, _ptr(status),
-        _ptr(workspace), _nbytes(workspace), _stream(stream)), prepare)
+    _ints(seq, "seq", count)
+    _ints(need, "need", count)
+    _ints(status, "status", count)
+    return _run("pld_pages_take", (pages.pool, seq.data_ptr(), need.data_ptr(), count, status.data_ptr(),
+                                   workspace.data_ptr(), _nbytes(workspace), _stream(stream)), prepare)
 
 
-def pld_pages_free(table, refs, page_size, seq, keep=None, stream=None, prepare=False):
+def pld_pages_free(pages, seq, keep=None, stream=None, prepare=False):
     """Sequences seq int32 [count] give back the pages behind their first keep[i] positions (all)."""
-    _on_one_device(stream, table, refs, seq, keep)
+    _on_one_device(stream, pages.refs, seq, keep)
     count = seq.numel()
     _ints(seq, "seq", count)
     _ints(keep, "keep", count)
-    return _run("pld_pages_free", (_pool_of(table, refs, page_size), _ptr(seq), _ptr(keep), count,
-                                   _stream(stream)), prepare)
+    return _run("pld_pages_free", (pages.pool, seq.data_ptr(), _ptr(keep), count, _stream(stream)), prepare)
 
 
-def pld_pages_fork(table, refs, page_size, layers, src, dst, lens, status, workspace, stream=None,
-                   prepare=False):
+def pld_pages_fork(pages, layers, src, dst, lens, status, workspace, stream=None, prepare=False):
     """Sequences dst[i] go on from the first lens[i] tokens of src[i]: whole pages shared, the last
     token's page copied in every one of `layers` (a PageLayers)."""
-    _on_one_device(stream, table, refs, src, dst, lens, status, workspace, *layers.each[:1])
+    _on_one_device(stream, pages.refs, src, dst, lens, status, workspace, layers.any)
     count = src.numel()
-    for t, name in ((src, "src"), (dst, "dst"), (lens, "lens"), (status, "status")):
-        _ints(t, name, count)
+    _ints(src, "src", count)
+    _ints(dst, "dst", count)
+    _ints(lens, "lens", count)
+    _ints(status, "status", count)
     return _run("pld_pages_fork", (
-        _pool_of(table, refs, page_size), layers.caches, layers.count, _ptr(src), _ptr(dst),
-        _ptr(lens), count, _ptr(status), _ptr(workspace), _nbytes(workspace), _stream(stream)), prepare)
+        pages.pool, layers.caches, layers.count, src.data_ptr(), dst.data_ptr(), lens.data_ptr(), count,
+        status.data_ptr(), workspace.data_ptr(), _nbytes(workspace), _stream(stream)), prepare)
 
 
-def pld_pages_compact(table, refs, page_size, layers, page_map, used, workspace, table_out=None,
-                      refs_out=None, stream=None, prepare=False):
+def pld_pages_compact(pages, layers, page_map, used, workspace, table_out=None, refs_out=None,
+                      stream=None, prepare=False):
     """Pages in use move to the lowest indices, in every one of `layers`: page_map int32 [num_pages]
     gets their new places, used int32 [1] their number, table_out and refs_out (default: the pool's
     own) the new table and references."""
     torch = _torch or _th()
-    table_out = table if table_out is None else table_out
-    refs_out = refs if refs_out is None else refs_out
-    _on_one_device(stream, table, refs, page_map, used, table_out, refs_out, workspace, *layers.each[:1])
+    table_out = pages.table if table_out is None else table_out
+    refs_out = pages.refs if refs_out is None else refs_out
+    _on_one_device(stream, pages.refs, page_map, used, table_out, refs_out, workspace, layers.any)
     ts = _need(table_out, torch.int32, "table_out", 2)
-    if table_out.shape != table.shape:
-        raise TypeError(f"table_out must be {tuple(table.shape)}, got {tuple(table_out.shape)}")
-    _ints(page_map, "page_map", refs.numel())
-    _ints(refs_out, "refs_out", refs.numel())
+    if table_out.shape != pages.table.shape:
+        raise TypeError(f"table_out must be {tuple(pages.table.shape)}, got {tuple(table_out.shape)}")
+    _ints(page_map, "page_map", pages.refs.shape[0])
+    _ints(refs_out, "refs_out", pages.refs.shape[0])
     _ints(used, "used", 1)
     return _run("pld_pages_compact", (
-        _pool_of(table, refs, page_size), layers.caches, layers.count, _ptr(page_map), _ptr(used),
-        _ptr(table_out), max(ts[0], table.shape[1]), _ptr(refs_out), _ptr(workspace),
-        _nbytes(workspace), _stream(stream)), prepare)
+        pages.pool, layers.caches, layers.count, page_map.data_ptr(), used.data_ptr(), table_out.data_ptr(),
+        max(ts[0], table_out.shape[1]), refs_out.data_ptr(), workspace.data_ptr(), _nbytes(workspace),
+        _stream(stream)), prepare)
 
 
 def pld_pages_copy(layers_from, layers_to, src, dst, slots=None, stream=None, prepare=False):
     """The first slots[i] slots (all) of page src[i] of every layer of `layers_from` to page dst[i] of
-    the same layer of `layers_to`."""
-    _on_one_device(stream, src, dst, slots, *layers_from.each[:1], *layers_to.each[:1])
+    the same layer of `layers_to` (PageLayers)."""
+    _on_one_device(stream, src, dst, slots, layers_from.any, layers_to.any)
     count = src.numel()
-    for t, name in ((src, "src"), (dst, "dst"), (slots, "slots")):
-        _ints(t, name, count)
+    _ints(src, "src", count)
+    _ints(dst, "dst", count)
+    _ints(slots, "slots", count)
     if layers_from.count != layers_to.count:
         raise TypeError(f"{layers_from.count} layers and {layers_to.count}")
-    return _run("pld_pages_copy", (layers_from.caches, layers_to.caches, layers_from.count, _ptr(src),
-                                   _ptr(dst), _ptr(slots), count, _stream(stream)), prepare)
+    return _run("pld_pages_copy", (layers_from.caches, layers_to.caches, layers_from.count, src.data_ptr(),
+                                   dst.data_ptr(), _ptr(slots), count, _stream(stream)), prepare)

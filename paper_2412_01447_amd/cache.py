@@ -8,7 +8,7 @@ verification `weights` renews the attention rows that the next step ranks by.
 """
 import torch
 
-from . import (PLD_ROPE_HALVES, PageLayers, pld_cache_attn, pld_cache_attn_rows,
+from . import (PLD_ROPE_HALVES, PageLayers, PageTable, pld_cache_attn, pld_cache_attn_rows,
                pld_cache_attn_workspace_bytes, pld_cache_write, pld_cache_write_packed, pld_pages_compact,
                pld_pages_copy, pld_pages_fork, pld_pages_free, pld_pages_take, pld_pages_workspace_bytes)
 
@@ -118,8 +118,8 @@ class PagePool:
     def __init__(self, k_caches, v_caches, k_scales=None, v_scales=None, table=None, refs=None):
         self.layers = PageLayers(k_caches, v_caches, k_scales, v_scales)
         self.table, self.refs = table, refs
-        self.page_size = k_caches[0].shape[1]
-        self.workspace = None
+        self.pages = None if table is None else PageTable(table, refs, k_caches[0].shape[1])
+        self.workspace, self.most = None, 0
         self.grown = []                  # workspaces that a larger one has replaced
 
     @classmethod
@@ -139,34 +139,36 @@ class PagePool:
     def reserve(self, count, stream=None):
         """The workspace for calls of up to `count` sequences or forks (grown as needed: a caller that
         captures a graph reserves before the capture).  One that is replaced is kept."""
-        need = pld_pages_workspace_bytes(self.table, self.refs, self.page_size, count)
-        if self.workspace is None or self.workspace.numel() < need:
-            if self.workspace is not None:
-                self.grown.append(self.workspace)
-            with _under(stream, self.refs.device):
-                self.workspace = torch.empty(need, dtype=torch.uint8, device=self.refs.device)
+        if count <= self.most:
+            return
+        if self.workspace is not None:
+            self.grown.append(self.workspace)
+        with _under(stream, self.refs.device):
+            self.workspace = torch.empty(pld_pages_workspace_bytes(self.pages, count), dtype=torch.uint8,
+                                         device=self.refs.device)
+        self.most = count
 
     def take(self, seq, need, status, stream=None, prepare=False):
         """Pages for the positions below need[i] of sequences seq[i]."""
         self.reserve(seq.numel(), stream)
-        return pld_pages_take(self.table, self.refs, self.page_size, seq, need, status,
+        return pld_pages_take(self.pages, seq, need, status,
                               self.workspace, stream=stream, prepare=prepare)
 
     def free(self, seq, keep=None, stream=None, prepare=False):
         """Sequences seq[i] give back what lies behind their first keep[i] positions (all)."""
-        return pld_pages_free(self.table, self.refs, self.page_size, seq, keep, stream=stream,
+        return pld_pages_free(self.pages, seq, keep, stream=stream,
                               prepare=prepare)
 
     def fork(self, src, dst, lens, status, stream=None, prepare=False):
         """Sequences dst[i] go on from the first lens[i] tokens of src[i]."""
         self.reserve(src.numel(), stream)
-        return pld_pages_fork(self.table, self.refs, self.page_size, self.layers, src, dst, lens,
+        return pld_pages_fork(self.pages, self.layers, src, dst, lens,
                               status, self.workspace, stream=stream, prepare=prepare)
 
     def compact(self, page_map, used, table_out=None, refs_out=None, stream=None, prepare=False):
         """Pages in use move to the lowest indices; page_map and used say where and how many."""
         self.reserve(1, stream)
-        return pld_pages_compact(self.table, self.refs, self.page_size, self.layers, page_map, used,
+        return pld_pages_compact(self.pages, self.layers, page_map, used,
                                  self.workspace, table_out=table_out, refs_out=refs_out,
                                  stream=stream, prepare=prepare)
 

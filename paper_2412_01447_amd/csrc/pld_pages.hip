@@ -15,9 +15,8 @@ struct Pool {
 // The integers' block: 1024 threads, kRun pages of the references each.
 constexpr int kPoolThreads = 1024, kPoolWaves = kPoolThreads / kWave;
 constexpr int kRun = 16, kSpan = kPoolThreads * kRun;   // pages of one step: 16384
-// Table entries of all a call's sequences up to which one block goes through them (each of its
-// waves a sequence) and gives out the pages in the same launch; more take a launch of a wave a
-// sequence before.
+// One block goes through a call's sequences, a wave each, and gives out the pages in the same launch;
+// more sequences than it has waves, or more entries than this, take launches of a wave a sequence.
 constexpr int64_t kOneBlock = 1 << 14;
 
 struct PoolWork {                // the workspace, in this order
@@ -240,13 +239,13 @@ template <bool kFork, bool kEdit>
 __global__ __launch_bounds__(kPoolThreads) void pages_give_kernel(EditArgs a) {
     const int wave = (int)threadIdx.x / kWave;
     if constexpr (kEdit) {
-        for (int i = wave; i < a.count; i += kPoolWaves) kFork ? share(a, i) : count_lacking(a, i);
+        if (wave < a.count) kFork ? share(a, wave) : count_lacking(a, wave);
         block_sync();
     }
     give_out<kFork, kFork && kEdit>(a);
     if constexpr (!kFork && kEdit) {
         block_sync();
-        for (int i = wave; i < a.count; i += kPoolWaves) fill(a, i);
+        if (wave < a.count) fill(a, wave);
     }
 }
 __global__ __launch_bounds__(256) void pages_fill_kernel(EditArgs a) {
@@ -524,7 +523,7 @@ static int check_work(const pld_pool *p, int count, void *ws, size_t bytes, Pool
 // The two launches before a copy or a filling (one where there are few entries).
 template <bool kFork>
 static bool launch_edit(const EditArgs &a, hipStream_t s) {
-    const bool one = (int64_t)a.count * a.p.max_pages <= kOneBlock;
+    const bool one = a.count <= kPoolWaves && (int64_t)a.count * a.p.max_pages <= kOneBlock;
     if (!one)
         hipLaunchKernelGGL(pages_edit_kernel<kFork>, dim3((a.count + 3) / 4), dim3(256), 0, s, a);
     if (one)

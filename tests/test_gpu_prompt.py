@@ -663,7 +663,7 @@ def test_fork_integers_alone_and_captured():
         p.same(p.moved(before, copies))
     none = pld.PageLayers([], [])
     before = p.contents()
-    pld.pld_pages_fork(pool.table, pool.refs, 16, none, src, seq, lens, status, pool.workspace)
+    pld.pld_pages_fork(pool.pages, none, src, seq, lens, status, pool.workspace)
     p.model.fork([0, 0], [1, 2], [33, 32])
     p.same(before)
 
@@ -712,7 +712,8 @@ def test_pool_refusals():
                  lambda: p.pool.fork(i, i, i, d_i32([0, 0])), lambda: p.pool.compact(i, i),
                  lambda: p.pool.compact(d_i32([0] * 8), i, table_out=p.pool.table[:2]),
                  lambda: p.pool.copy_from(Pages(3, 4, 8, layers=1).pool, i, i), lambda: p.pool.copy_from(Pages(3, 4, 8, heads=1).pool, i, i),
-                 lambda: pld.PageLayers([p.k[0], p.k[1][:4]], p.v), lambda: pld.pld_pages_take(p.pool.table, p.pool.refs, 16, i, i, i, i)):
+                 lambda: pld.PageLayers([p.k[0], p.k[1][:4]], p.v), lambda: pld.pld_pages_take(p.pool.pages, i, i, i, i),
+                 lambda: pld.PageTable(p.pool.table, p.pool.refs.float(), 16), lambda: pld.PageTable(p.pool.table[0], p.pool.refs, 16)):
         with pytest.raises((TypeError, pld.PLDError)):
             call()
 

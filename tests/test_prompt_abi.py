@@ -182,7 +182,7 @@ def test_host_tensors_and_odd_arguments_are_refused():
     k = torch.zeros(1, 16, 2, 64, dtype=torch.bfloat16)
     i = torch.zeros(4, dtype=torch.int32)
     for call in (lambda: pld.pld_prompt_attn(t, t, t, i, t), lambda: pld.pld_cache_write_packed(t, t, t, k, k, i[None], i, i, t),
-                 lambda: pld.pld_pages_take(i[None], i, 16, i, i, i, i), lambda: pld.pld_pages_free(i[None], i, 16, i),
+                 lambda: pld.PageTable(i[None], i, 16),
                  lambda: PagePool([k], [k]), lambda: pld.PageLayers([k], [k, k]), lambda: pld.PageLayers([k], [k], [i], None)):
         with pytest.raises(TypeError):
             call()
