@@ -365,8 +365,23 @@ struct CopyArgs {
 };
 enum { kPairs, kForks, kMoves };
 
-// A block's part of a copy: 16 KB of a page's keys or values, or its scales.  Bound by memory.
-constexpr int kCopyThreads = 256, kCopyEach = 4, kCopyPieces = kCopyThreads * kCopyEach;
+// A block's part of a copy: 32 KB of a page's keys or values, or its scales.  Bound by memory; read and
+// written past the caches where each page is read once (kOnce): what a compaction moves (32 sequences, 8
+// layers in e4m3, 2.7 GB) 550 us without and 504 with it; forks read a prompt's page several times, 64 us
+// without and 80 with it (56 of 8 prompts, 16 layers).  With 16 KB a part 595 us, with 64 KB 555.
+constexpr int kCopyThreads = 256, kCopyEach = 8, kCopyPieces = kCopyThreads * kCopyEach;
+template <bool kOnce>
+__device__ __forceinline__ u32x4_t load16(const void *p) {
+    const u32x4_t *q = reinterpret_cast<const u32x4_t *>(p);
+    return kOnce ? __builtin_nontemporal_load(q) : *q;
+}
+template <bool kOnce>
+__device__ __forceinline__ void store16(void *p, u32x4_t v) {
+    u32x4_t *q = reinterpret_cast<u32x4_t *>(p);
+    if (kOnce) __builtin_nontemporal_store(v, q);
+    else *q = v;
+}
+template <bool kOnce>
 __device__ __forceinline__ void copy_part(const CopyArgs &a, int layer, bool value, int chunk, int src, int dst, int slots) {
     const CopyLayer &l = a.layer[layer];
     if (chunk == a.chunks) {
@@ -382,26 +397,27 @@ __device__ __forceinline__ void copy_part(const CopyArgs &a, int layer, bool val
     const int pieces = slots * a.heads << a.row, first = chunk * kCopyPieces + (int)threadIdx.x;
     if (chunk * kCopyPieces >= pieces) return;
     u32x4_t v[kCopyEach];
+    // (past the end: the last piece again, which is not stored)
     if (a.linear && (!a.by_head || slots == 1 << a.shift)) {
 #pragma unroll
-        for (int k = 0; k < kCopyEach; ++k) v[k] = reinterpret_cast<const u32x4_t *>(f)[min(first + k * kCopyThreads, pieces - 1)];
+        for (int k = 0; k < kCopyEach; ++k) v[k] = load16<kOnce>(f + (int64_t)min(first + k * kCopyThreads, pieces - 1) * 16);
 #pragma unroll
         for (int k = 0; k < kCopyEach; ++k)
-            if (first + k * kCopyThreads < pieces) reinterpret_cast<u32x4_t *>(t)[first + k * kCopyThreads] = v[k];
+            if (first + k * kCopyThreads < pieces) store16<kOnce>(t + (int64_t)(first + k * kCopyThreads) * 16, v[k]);
         return;
     }
     int64_t to[kCopyEach];
 #pragma unroll
     for (int k = 0; k < kCopyEach; ++k) {
-        const int i = min(first + k * kCopyThreads, pieces - 1);   // (past the end: the last one again)
+        const int i = min(first + k * kCopyThreads, pieces - 1);
         const int r = i >> a.row, inner = a.by_head ? slots : a.heads, q = r / inner, m = r - q * inner;
         const int64_t slot = a.by_head ? m : q, head = a.by_head ? q : m, piece = (i - (r << a.row)) * 16;
-        v[k] = *reinterpret_cast<const u32x4_t *>(f + slot * a.from.slot + head * a.from.head + piece);
+        v[k] = load16<kOnce>(f + slot * a.from.slot + head * a.from.head + piece);
         to[k] = slot * a.to.slot + head * a.to.head + piece;
     }
 #pragma unroll
     for (int k = 0; k < kCopyEach; ++k)
-        if (first + k * kCopyThreads < pieces) *reinterpret_cast<u32x4_t *>(t + to[k]) = v[k];
+        if (first + k * kCopyThreads < pieces) store16<kOnce>(t + to[k], v[k]);
 }
 
 // Parts are dealt to the grid's blocks in turn, in order of (page, layer, keys or values, chunk).
@@ -438,7 +454,7 @@ __global__ __launch_bounds__(kCopyThreads) void pages_copy_kernel(CopyArgs a, Ed
             if ((uint32_t)src >= (uint32_t)a.num_from || (uint32_t)dst >= (uint32_t)a.num_to) continue;
             if (a.slots && (uint32_t)a.slots[m] < (uint32_t)slots) slots = a.slots[m];
         }
-        copy_part(a, layer, value, chunk, src, dst, slots);
+        copy_part<kMode != kForks>(a, layer, value, chunk, src, dst, slots);
     }
 }
 
@@ -495,11 +511,12 @@ static void fill_layers(CopyArgs &a, const pld_cache *f, const pld_cache *t, int
     }
 }
 
-// Eight blocks a CU at most: 128 KB of a CU's loads under way.
-constexpr int kCopyBlocks = 2048;
+// Past the caches two blocks a CU, 64 KB of its loads under way, are best (2.7 GB moved in 504 us, 514 with
+// four and 522 with eight), through them eight.
 template <int kMode>
 static int launch_copy(CopyArgs &a, const EditArgs &e, const CompactArgs &c, const pld_cache *f, const pld_cache *t,
                        int n_layers, int64_t most, int ints, hipStream_t s) {
+    constexpr int kCopyBlocks = kMode == kForks ? 2048 : 512;
     if (n_layers) fill_geometry(a, f[0], t[0]);
     for (int first = 0; first < n_layers || first == 0; first += kCopyLayers) {
         const int n = n_layers - first < kCopyLayers ? n_layers - first : kCopyLayers;
