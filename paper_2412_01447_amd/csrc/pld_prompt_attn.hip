@@ -68,12 +68,11 @@ template <int kAhead>   // a distance of both addresses
 __device__ __forceinline__ void load_to_lds(uint32_t to, const void *base, uint32_t off) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3" ::"s"(to), "v"(off), "s"(base), "n"(kAhead) : "memory");
 }
-__device__ __forceinline__ void load_far_to_lds(uint32_t to, const void *from) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
-}
+// Before a barrier: what this wave loads into LDS is there, and what it reads from LDS is read, so that
+// after it other waves may read the one and load over the other.
 __device__ __forceinline__ void wait_loads() {
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0), in a form that the compiler counts by too
+    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0), in a form that the compiler counts by too
     asm volatile("" ::: "memory");
 }
 __device__ __forceinline__ void block_barrier() {
@@ -124,25 +123,29 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
     const int h = lane >> 5;
 
     // ---- the rows: what each sees, [lo, hi), and its query
-    int row[kQT], head[kQT], lo[kQT], hi[kQT];
+    auto row_of = [&](int t, int over, int &row, int &head) PLD_INLINE {
+        const uint32_t m = (uint32_t)(over + (wave * kQT + t) * 32 + (lane & 31));
+        const int r = (int)(m / (uint32_t)a.G);
+        row = (int)first + r;
+        head = kv * a.G + (int)m - r * a.G;
+    };
+    int lo[kQT], hi[kQT];   // (none: 0 and 0)
     bf16x8_t qf[kQT][D / 16];
     int wave_lo = INT32_MAX, wave_hi = 0, full_lo = 0, full_hi = INT32_MAX;
 #pragma unroll
     for (int t = 0; t < kQT; ++t) {
-        const uint32_t m = (uint32_t)(over + (wave * kQT + t) * 32 + (lane & 31));
-        const int r = (int)(m / (uint32_t)a.G);
-        row[t] = (int)first + r;
-        head[t] = kv * a.G + (int)m - r * a.G;
-        const bool in = row[t] < a.p.N;
-        if (!in) row[t] = a.p.N - 1;
-        const uint4 *src = reinterpret_cast<const uint4 *>(a.q + row[t] * a.qr + (int64_t)head[t] * D);
+        int row, head;
+        row_of(t, over, row, head);
+        const bool in = row < a.p.N;
+        if (!in) row = a.p.N - 1;
+        const uint4 *src = reinterpret_cast<const uint4 *>(a.q + row * a.qr + (int64_t)head * D);
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) qf[t][s] = __builtin_bit_cast(bf16x8_t, src[2 * s + h]);
-        const Span sp = spans_of(a.p, row[t]);
+        const Span sp = spans_of(a.p, row);
         lo[t] = hi[t] = 0;
         if (in && sp.b >= 0) {
-            hi[t] = row[t] + 1;
-            lo[t] = min(max(max(sp.begin, 0), a.window ? hi[t] - a.window : 0), row[t]);
+            hi[t] = row + 1;
+            lo[t] = min(max(max(sp.begin, 0), a.window ? hi[t] - a.window : 0), row);
             wave_lo = min(wave_lo, lo[t]);
             wave_hi = max(wave_hi, hi[t]);
             full_lo = max(full_lo, lo[t]);
@@ -172,9 +175,9 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
     const uint32_t koff = (uint32_t)j0 * kstride + piece, voff = (uint32_t)j0 * vstride + piece;
     const uint32_t k_lds = (uint32_t)(uintptr_t)(lds_ptr)&s_k[0][0] + unit0 * 1024;
     const uint32_t v_lds = (uint32_t)(uintptr_t)(lds_ptr)&s_v[0][0] + unit0 * 1024;
-    // keys or values of 64 rows from `from` on to a buffer
-    auto fetch_at = [&](const char *from, int buf, bool values) PLD_INLINE {
-        const uint32_t to = (values ? v_lds : k_lds) + buf * T::kTileBytes, off = values ? voff : koff;
+    // keys or values to a buffer: a lane's from `from` + off on
+    auto fetch_at = [&](const char *from, uint32_t off, int buf, bool values) PLD_INLINE {
+        const uint32_t to = (values ? v_lds : k_lds) + buf * T::kTileBytes;
         load_to_lds<0>(to, from, off);
         if constexpr (kLoads > 1) load_to_lds<64>(to + 960, from, off);
         if constexpr (kLoads > 2) load_to_lds<128>(to + 1920, from, off), load_to_lds<192>(to + 2880, from, off);
@@ -183,18 +186,10 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
             load_to_lds<384>(to + 5760, from, off), load_to_lds<448>(to + 6720, from, off);
         }
     };
-    // the same from row k0 on; for rows outside the block's the nearest one stands in
+    // those of the rows from k0 on, which the block has; for rows past its last that one stands in
     auto fetch = [&](int k0, int buf, bool values) PLD_INLINE {
-        const uint32_t stride = values ? vstride : kstride;
-        const char *base = values ? vbase : kbase;
-        if (k0 + kKeys <= block_hi) {
-            fetch_at(uniform(base + (int64_t)k0 * stride), buf, values);
-        } else {
-            const uint32_t to = (values ? v_lds : k_lds) + buf * T::kTileBytes;
-            const int row = min(k0 + j0, block_hi - 1);
-#pragma unroll
-            for (int x = 0; x < kLoads; ++x) load_far_to_lds(to + x * 1024, base + (int64_t)row * stride + piece + x * 64);
-        }
+        const uint32_t stride = values ? vstride : kstride, off = (uint32_t)min(j0, block_hi - 1 - k0) * stride + piece;
+        fetch_at(uniform((values ? vbase : kbase) + (int64_t)k0 * stride), off, buf, values);
     };
 
     // ---- the products, of 32 keys at a time: `part` of a tile
@@ -245,14 +240,18 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
 #pragma unroll
             for (int r = 0; r < 16; ++r) w = fmaxf(w, fabsf(s[t][r]));
         // few scores come to a third of the cap as a rule: one branch for the wave
-        const bool far = __any(w * a.c1 >= a.cap_near);
+        if (__any(w * a.c1 >= a.cap_near)) {
 #pragma unroll
-        for (int t = 0; t < kQT; ++t)
+            for (int t = 0; t < kQT; ++t)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float x = s[t][r] * a.c1;
-                s[t][r] = far ? soft_cap(x, a.cap, a.cap_x2, a.cap_near, a.inv2_log2e) : soft_cap_near(x, a.inv2_log2e);
-            }
+                for (int r = 0; r < 16; ++r)
+                    s[t][r] = soft_cap(s[t][r] * a.c1, a.cap, a.cap_x2, a.cap_near, a.inv2_log2e);
+        } else {
+#pragma unroll
+            for (int t = 0; t < kQT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[t][r] = soft_cap_near(s[t][r] * a.c1, a.inv2_log2e);
+        }
     };
     auto mask = [&](int k0, f32x16_t (&s)[kQT]) PLD_INLINE {
 #pragma unroll
@@ -304,7 +303,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
     // ---- the keys, 32 at a time.  A step takes the weights of its scores while the products of the next
     // step's are under way, and reads values, and then the step's after it keys, from LDS for the products
     // that follow: each has a part of what the vector units and LDS do beside them, in this order.
-    constexpr int kX = D / 16, kLead = kX < 8 ? kX : 8;   // products of a kind; values read so many products ahead
+    constexpr int kX = D / 16, kLead = kQT == 2 ? 2 : kX < 8 ? kX : 8;   // products of a kind; values are read so many ahead
     f32x16_t s0[kQT], s1[kQT];
     bf16x8_t kf[kX];                 // keys of the next scores
     float top[kQT];
@@ -416,8 +415,8 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
         constexpr int kOdd = decltype(odd)::value;
         wait_loads();
         block_barrier();
-        fetch_at(kbase + (int64_t)(k0 + 2 * kKeys) * kstride, kOdd, false);
-        fetch_at(vbase + (int64_t)(k0 + kKeys) * vstride, !kOdd, true);
+        fetch_at(kbase + (int64_t)(k0 + 2 * kKeys) * kstride, koff, kOdd, false);
+        fetch_at(vbase + (int64_t)(k0 + kKeys) * vstride, voff, !kOdd, true);
         auto whole = [&](int part, f32x16_t (&s)[kQT], f32x16_t (&ahead)[kQT]) PLD_INLINE {
             if constexpr (kCap) {
                 cap(s);
@@ -460,7 +459,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
         for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) x = fmaf(o[t][dt][r], 0.f, x);
-        odd |= !(x == 0.f) || !(l[t] < INFINITY);
+        odd |= lo[t] < hi[t] && (!(x == 0.f) || !(l[t] < INFINITY));
     }
     if (__syncthreads_or(odd)) {
         begin();
@@ -523,11 +522,15 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
 
     // ---- out: a lane has four consecutive elements of every eight; the two lanes of a query trade
     // halves, so that each stores eight
+    int over_again = over;   // (taken again, so that no register keeps rows all along)
+    asm volatile("" : "+s"(over_again));
 #pragma unroll
     for (int t = 0; t < kQT; ++t) {
         if (lo[t] >= hi[t]) continue;   // (both lanes of a query alike)
+        int row, head;
+        row_of(t, over_again, row, head);
         const float inv = 1.f / l[t];
-        uint16_t *dst = a.out + row[t] * a.orow + (int64_t)head[t] * D;
+        uint16_t *dst = a.out + row * a.orow + (int64_t)head * D;
 #pragma unroll
         for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
@@ -540,7 +543,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
                 *reinterpret_cast<uint4 *>(dst + dt * 32 + r * 2 + h * 8) = make_uint4(y0[0], y1[0], y0[1], y1[1]);
             }
         if (a.lse && h == 0)
-            a.lse[(int64_t)row[t] * a.G * a.heads + head[t]] = fmaf(mx[t], a.nat, __log2f(l[t]) * kLn2);
+            a.lse[(int64_t)row * a.G * a.heads + head] = fmaf(mx[t], a.nat, __log2f(l[t]) * kLn2);
     }
 }
 
@@ -593,10 +596,13 @@ extern "C" int pld_prompt_attn(const uint16_t *q, int64_t q_row_stride, const ui
     // Blocks of 256 rows read keys and values half as often; blocks of 128, two a CU, wait less for each
     // other and share out evener.  32 heads over 8 of 128: one sequence of 1024 rows 29.5 and 23.1 us, of 2048
     // 53.0 and 54.5, of 16384 1927 and 2206; 64 of 300 150 and 137, 16 of 1000 193 and 198.  Heads of
-    // 64, whose vector instructions bound them: 2 x 8192 605 and 615, 2048 37 and 32, capped in a window
-    // of 1000 245 and 183.
+    // 64, whose vector instructions bound them, gain where a wave of 64 rows reads each value once for two
+    // products: 2 x 8192 538 and 597, 4 x 4096 319 and 341, one of 4096 95 and 91, 2048 39 and 32, 16 x 1000
+    // 111 and 107, capped in a window of 1000 187 and 176.
     const int64_t wide = ((int64_t)N * a.G + 255) / 256 * heads;
-    if (head_dim == 64)
+    if (head_dim == 64 && wide >= 1024 && N >= (int64_t)B * 3000)
+        launch_prompt<64, 2, 4>(a, s);
+    else if (head_dim == 64)
         launch_prompt<64, 1, 4>(a, s);
     else if (head_dim == 128 && wide >= 256 && N >= (int64_t)B * 512)
         launch_prompt<128, 1, 8>(a, s);
