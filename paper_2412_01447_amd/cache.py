@@ -139,6 +139,7 @@ class PagePool:
     def reserve(self, count, stream=None):
         """The workspace for calls of up to `count` sequences or forks (grown as needed: a caller that
         captures a graph reserves before the capture).  One that is replaced is kept."""
+        count = max(1, count)
         if count <= self.most:
             return
         if self.workspace is not None:
@@ -151,28 +152,25 @@ class PagePool:
     def take(self, seq, need, status, stream=None, prepare=False):
         """Pages for the positions below need[i] of sequences seq[i]."""
         self.reserve(seq.numel(), stream)
-        return pld_pages_take(self.pages, seq, need, status,
-                              self.workspace, stream=stream, prepare=prepare)
+        return pld_pages_take(self.pages, seq, need, status, self.workspace, stream=stream,
+                              prepare=prepare)
 
     def free(self, seq, keep=None, stream=None, prepare=False):
         """Sequences seq[i] give back what lies behind their first keep[i] positions (all)."""
-        return pld_pages_free(self.pages, seq, keep, stream=stream,
-                              prepare=prepare)
+        return pld_pages_free(self.pages, seq, keep, stream=stream, prepare=prepare)
 
     def fork(self, src, dst, lens, status, stream=None, prepare=False):
         """Sequences dst[i] go on from the first lens[i] tokens of src[i]."""
         self.reserve(src.numel(), stream)
-        return pld_pages_fork(self.pages, self.layers, src, dst, lens,
-                              status, self.workspace, stream=stream, prepare=prepare)
+        return pld_pages_fork(self.pages, self.layers, src, dst, lens, status, self.workspace,
+                              stream=stream, prepare=prepare)
 
     def compact(self, page_map, used, table_out=None, refs_out=None, stream=None, prepare=False):
         """Pages in use move to the lowest indices; page_map and used say where and how many."""
         self.reserve(1, stream)
-        return pld_pages_compact(self.pages, self.layers, page_map, used,
-                                 self.workspace, table_out=table_out, refs_out=refs_out,
-                                 stream=stream, prepare=prepare)
+        return pld_pages_compact(self.pages, self.layers, page_map, used, self.workspace,
+                                 table_out=table_out, refs_out=refs_out, stream=stream, prepare=prepare)
 
     def copy_from(self, other, src, dst, slots=None, stream=None, prepare=False):
         """Page src[i] of another pool (its first slots[i] slots) to page dst[i] of this one."""
-        return pld_pages_copy(other.layers, self.layers, src, dst, slots, stream=stream,
-                              prepare=prepare)
+        return pld_pages_copy(other.layers, self.layers, src, dst, slots, stream=stream, prepare=prepare)

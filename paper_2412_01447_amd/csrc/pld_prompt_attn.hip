@@ -50,17 +50,6 @@ __device__ __forceinline__ const char *uniform(const char *p) {
     return (const char *)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 |
                           (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
 }
-__device__ __forceinline__ int wave_min(int v) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v = min(v, __shfl_xor(v, o));
-    return __builtin_amdgcn_readfirstlane(v);
-}
-__device__ __forceinline__ int wave_max(int v) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v = max(v, __shfl_xor(v, o));
-    return __builtin_amdgcn_readfirstlane(v);
-}
-
 // 16 bytes a lane from base + off to LDS, lane after lane from `to` on, without a register between
 // (a lane's place in LDS is fixed, so the swizzle is in the addresses it reads).  The caller waits
 // (vmcnt): the compiler does not know of these loads.
@@ -122,7 +111,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
     const int h = lane >> 5;
 
-    // ---- the rows: what each sees, [lo, hi), and its query
+    // ---- the rows: what each sees, [lo, hi)
     auto row_of = [&](int t, int over, int &row, int &head) PLD_INLINE {
         const uint32_t m = (uint32_t)(over + (wave * kQT + t) * 32 + (lane & 31));
         const int r = (int)(m / (uint32_t)a.G);
@@ -130,7 +119,6 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
         head = kv * a.G + (int)m - r * a.G;
     };
     int lo[kQT], hi[kQT];   // (none: 0 and 0)
-    bf16x8_t qf[kQT][D / 16];
     int wave_lo = INT32_MAX, wave_hi = 0, full_lo = 0, full_hi = INT32_MAX;
 #pragma unroll
     for (int t = 0; t < kQT; ++t) {
@@ -138,22 +126,22 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
         row_of(t, over, row, head);
         const bool in = row < a.p.N;
         if (!in) row = a.p.N - 1;
-        const uint4 *src = reinterpret_cast<const uint4 *>(a.q + row * a.qr + (int64_t)head * D);
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) qf[t][s] = __builtin_bit_cast(bf16x8_t, src[2 * s + h]);
         const Span sp = spans_of(a.p, row);
         lo[t] = hi[t] = 0;
         if (in && sp.b >= 0) {
             hi[t] = row + 1;
             lo[t] = min(max(max(sp.begin, 0), a.window ? hi[t] - a.window : 0), row);
-            wave_lo = min(wave_lo, lo[t]);
-            wave_hi = max(wave_hi, hi[t]);
-            full_lo = max(full_lo, lo[t]);
-            full_hi = min(full_hi, hi[t]);
+        }
+        // both grow from row to row: a wave's range is between its first and its last row that has one
+        const uint32_t some = (uint32_t)__ballot(hi[t] > 0);
+        if (some) {
+            const int i = __builtin_ctz(some), j = 31 - __builtin_clz(some);
+            wave_lo = min(wave_lo, __builtin_amdgcn_readlane(lo[t], i));
+            wave_hi = max(wave_hi, __builtin_amdgcn_readlane(hi[t], j));
+            full_lo = max(full_lo, __builtin_amdgcn_readlane(lo[t], j));
+            full_hi = min(full_hi, __builtin_amdgcn_readlane(hi[t], i));
         }
     }
-    wave_lo = wave_min(wave_lo), wave_hi = wave_max(wave_hi);
-    full_lo = wave_max(full_lo), full_hi = wave_min(full_hi);
     if (lane == 0) s_range[wave][0] = wave_lo, s_range[wave][1] = wave_hi;
     __syncthreads();
     int block_lo = INT32_MAX, block_hi = 0;
@@ -193,6 +181,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
     };
 
     // ---- the products, of 32 keys at a time: `part` of a tile
+    bf16x8_t qf[kQT][D / 16];
     f32x16_t o[kQT][kDT];
     float mx[kQT], l[kQT];
     const int c16 = lane & 15, odd16 = lane >> 4 & 1;
@@ -432,6 +421,15 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
     };
     begin();
     fetch(block_lo, 0, false);
+    // the queries, on their way with the first keys
+#pragma unroll
+    for (int t = 0; t < kQT; ++t) {
+        int row, head;
+        row_of(t, over, row, head);
+        const uint4 *src = reinterpret_cast<const uint4 *>(a.q + min(row, a.p.N - 1) * a.qr + (int64_t)head * D);
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) qf[t][s] = __builtin_bit_cast(bf16x8_t, src[2 * s + h]);
+    }
     wait_loads();
     block_barrier();
     if (block_lo + kKeys < block_hi) fetch(block_lo + kKeys, 1, false);

@@ -705,6 +705,36 @@ def test_copy_far_pages():
     assert torch.equal(v[699], v[3]) and (v[2] == 0).all()
 
 
+def test_prepared_page_calls():
+    """Calls marshalled once, issued again and again."""
+    p = Pages(4, 4, 20)
+    pool, one = p.pool, d_i32([0])
+    seq, lens, status = d_i32([1, 2]), d_i32([40, 33]), torch.zeros(2, dtype=torch.int32, device=dev())
+    page_map, used = torch.zeros(20, dtype=torch.int32, device=dev()), torch.zeros(1, dtype=torch.int32, device=dev())
+    p.take([0], [60])
+    src, need, to, keep, taken = d_i32([0, 0]), d_i32([60]), d_i32([19]), d_i32([40]), d_i32([9])
+    calls = [pool.fork(src, seq, lens, status, prepare=True), pool.free(one, keep, prepare=True),
+             pool.compact(page_map, used, prepare=True), pool.take(one, need, taken, prepare=True)]
+    copy = pool.copy_from(pool, one, to, prepare=True)
+    pool.reserve(50)                       # (the calls keep the workspace that they were made with)
+    for _ in range(3):
+        before = p.contents()
+        calls[0]()
+        want, copies = p.model.fork([0, 0], [1, 2], [40, 33])
+        assert status.tolist() == want == [0, 0]
+        p.same(p.moved(before, copies))
+        calls[1](), p.model.free([0], [40])
+        calls[2]()
+        new, n, moves = p.model.compact()
+        p.same(p.contents())               # (contents in test_pages_in_random_order)
+        assert np.array_equal(page_map.cpu().numpy(), new) and used.item() == n
+        calls[3]()
+        assert p.model.take([0], [60]) == taken.tolist() == [0]
+        before = p.contents()
+        copy()
+        p.same(p.moved(before, [(0, 19, 16)]))
+
+
 def test_pool_refusals():
     p = Pages(3, 4, 8)
     i = d_i32([0])

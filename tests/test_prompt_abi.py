@@ -186,3 +186,23 @@ def test_host_tensors_and_odd_arguments_are_refused():
                  lambda: PagePool([k], [k]), lambda: pld.PageLayers([k], [k, k]), lambda: pld.PageLayers([k], [k], [i], None)):
         with pytest.raises(TypeError):
             call()
+
+
+def test_prepared_page_calls_keep_their_structs():
+    """A prepared page call holds its pool and its array of caches by itself."""
+    import gc
+    pool = pld._Pool(0x7700, 8, 0x7800, 4, 8, 9, 16)
+    layers = (pld._Cache * 2)(_cache(k=0x7770), _cache(k=0x7780))
+    calls = [pld.Prepared("pld_pages_fork", (pool, layers, 2, 1, 1, 1, 1, 1, 1, 1, 0)),
+             pld.Prepared("pld_pages_compact", (pool, layers, 2, 1, 1, 1, 8, 1, 1, 1, 0)),
+             pld.Prepared("pld_pages_copy", (layers, layers, 2, 1, 1, 1, 1, 0)),
+             pld.Prepared("pld_pages_take", (pool, 1, 1, 1, 1, 1, 1, 0)),
+             pld.Prepared("pld_pages_free", (pool, 1, 1, 1, 0))]
+    del pool, layers
+    gc.collect()
+    [_cache(k=i) for i in range(1000)]
+    for c in calls:
+        if c.name != "pld_pages_copy":
+            assert c.args[0].contents.table == 0x7700 and c.args[0].contents.page_size == 16
+    for a in (calls[0].args[1], calls[1].args[1], calls[2].args[0], calls[2].args[1]):
+        assert [a[i].k for i in range(2)] == [0x7770, 0x7780]
