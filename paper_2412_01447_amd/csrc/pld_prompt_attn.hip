@@ -14,6 +14,7 @@ struct PromptArgs {
     int64_t tiles;                 // of a key head's rows
     float c1;                      // products to scores in log2 units
     float cap, cap_x2, cap_near, inv2_log2e;   // as in AttnArgs
+    float inv_cap;                 // from products to parts y of the cap
     float nat;                     // from log2 units to natural ones
     int window;
     uint16_t *out;
@@ -222,25 +223,26 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
         return top;
     };
     const float c = kCap ? 1.f : a.c1;   // from scores as they are kept to log2 units
-    auto cap = [&](f32x16_t (&s)[kQT]) PLD_INLINE {
-        float w = 0.f;
-#pragma unroll
-        for (int t = 0; t < kQT; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) w = fmaxf(w, fabsf(s[t][r]));
-        // few scores come to a third of the cap as a rule: one branch for the wave
-        if (__any(w * a.c1 >= a.cap_near)) {
-#pragma unroll
-            for (int t = 0; t < kQT; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    s[t][r] = soft_cap(s[t][r] * a.c1, a.cap, a.cap_x2, a.cap_near, a.inv2_log2e);
-        } else {
-#pragma unroll
-            for (int t = 0; t < kQT; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[t][r] = soft_cap_near(s[t][r] * a.c1, a.inv2_log2e);
-        }
+    // Capped scores, x tanh(y) / y with y = x / cap.  They stay products s, and where all are near
+    // (soft_cap_near's) fit[], its polynomial with the scale in it, is multiplied in the weight's own fma: five
+    // instructions a score and not eight.  Where one is not, all are made s - m before (`settle`), with fit and
+    // base 1 and 0 for the step: either way a score's bits go by it alone.  4 x 4096 of 32 heads of 64, 464
+    // to 425 us.
+    float fit[4], base[kQT];
+    auto set_fit = [&](bool is_near) PLD_INLINE {
+        fit[0] = is_near ? a.c1 : 1.f;
+        fit[1] = is_near ? a.c1 * -0.33332663f : 0.f;
+        fit[2] = is_near ? a.c1 * 0.13299825f : 0.f;
+        fit[3] = is_near ? a.c1 * -0.0491485f : 0.f;
+    };
+    auto near = [&](float s) PLD_INLINE {
+        const float y = s * a.inv_cap, u = fminf(fmaxf(y * y, 0.f), 1.f);   // (of -inf as well)
+        return fmaf(u, fmaf(u, fmaf(u, fit[3], fit[2]), fit[1]), fit[0]);
+    };
+    auto capped = [&](float s, float less) PLD_INLINE {
+        const float x = s * a.c1, e = __builtin_amdgcn_exp2f(fabsf(x) * a.inv2_log2e);
+        const float far = copysignf(a.cap - a.cap_x2 * __builtin_amdgcn_rcpf(e + 1.f), x) - less;
+        return s == -INFINITY ? s : fabsf(x) >= a.cap_near ? far : fmaf(s, near(s), -less);
     };
     auto mask = [&](int k0, f32x16_t (&s)[kQT]) PLD_INLINE {
 #pragma unroll
@@ -270,10 +272,27 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
             for (int dt = 0; dt < kDT; ++dt) o[t][dt] *= f;
         }
     };
+    // Capped scores: the largest, from the largest product; and the scores themselves, after raise.
+    auto settle_top = [&](float (&top)[kQT], bool far) PLD_INLINE {
+        set_fit(true);
+#pragma unroll
+        for (int t = 0; t < kQT; ++t) top[t] = far ? capped(top[t], 0.f) : top[t] * near(top[t]);
+    };
+    auto settle = [&](f32x16_t (&s)[kQT], bool far) PLD_INLINE {
+#pragma unroll
+        for (int t = 0; t < kQT; ++t) base[t] = far ? 0.f : mx[t];
+        if (far) {
+#pragma unroll
+            for (int t = 0; t < kQT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[t][r] = capped(s[t][r], mx[t]);
+            set_fit(false);
+        }
+    };
     // Weights 2^(s c - m), rounded to bf16 in pairs, as the product takes them: half a step (2^-8) of
     // each term.  The sum is of the unrounded ones.
     auto weigh = [&](float s, int t) PLD_INLINE {
-        const float w = __builtin_amdgcn_exp2f(fmaf(s, c, -mx[t]));
+        const float w = __builtin_amdgcn_exp2f(fmaf(s, kCap ? near(s) : c, kCap ? -base[t] : -mx[t]));
         l[t] += w;
         return w;
     };
@@ -297,7 +316,22 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
     bf16x8_t kf[kX];                 // keys of the next scores
     float top[kQT];
     uint64_t too_high = 0;           // score_high(top)
+    bool far = false;                // of capped scores: some are not near
+    // from the largest products `top`, and those of either sign
+    auto look = [&](const float (&most)[kQT]) PLD_INLINE {
+        if constexpr (kCap) {
+            float x = most[0];
+#pragma unroll
+            for (int t = 1; t < kQT; ++t) x = fmaxf(x, most[t]);
+            far = __any(x * a.c1 >= a.cap_near);
+            set_fit(true);
+#pragma unroll
+            for (int t = 0; t < kQT; ++t) top[t] *= near(top[t]);
+        }
+        too_high = score_high(top);
+    };
     auto first_scores = [&](f32x16_t (&s)[kQT]) PLD_INLINE {
+        float most[kQT];
 #pragma unroll
         for (int t = 0; t < kQT; ++t) {
 #pragma unroll
@@ -305,8 +339,11 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
 #pragma unroll
             for (int x = 0; x < kX; ++x) s[t] = mfma32(kf[x], qf[t][x], s[t]);
             top[t] = largest(s[t]);
+            most[t] = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) most[t] = fmaxf(most[t], fabsf(s[t][r]));
         }
-        too_high = score_high(top);
+        look(most);
     };
     auto read_keys = [&](const char *buf, int part) PLD_INLINE {
 #pragma unroll
@@ -330,7 +367,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
                 }
         };
         auto read_value = [&](int x) PLD_INLINE { vf[x % kLead] = value_operand(vbuf, part * 2 + x / kDT, x % kDT); };
-        float m[kQT];
+        float m[kQT], most[kQT];
         // (past the last keys: of whatever is there, and not used)
 #pragma unroll
         for (int z = 0; z < kZ; ++z) {
@@ -341,7 +378,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
             ahead[t] = mfma32(kf[x], qf[t][x], ahead[t]);
             if (t == 0 && x >= kX - kLead) read_value(x - (kX - kLead));
             weights(z);
-            __builtin_amdgcn_sched_barrier(0);
+            if (!kCap || z % 2) __builtin_amdgcn_sched_barrier(0);   // (two slots: a cap is a chain of instructions)
         }
 #pragma unroll
         for (int z = 0; z < kZ; ++z) {
@@ -354,35 +391,37 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
             }
             weights(kZ + z);
             constexpr int kFrom = kZ / 4, kEach = 16 * kQT / (kZ / 2);   // the next maximum
-            if (!kCap && z >= kFrom && z < kFrom + kZ / 2)
+            if (z >= kFrom && z < kFrom + kZ / 2)
 #pragma unroll
                 for (int e = (z - kFrom) * kEach; e < (z - kFrom + 1) * kEach; ++e) {
                     const int u = e / 16, r = e % 16;
                     m[u] = fmaxf(r ? m[u] : -INFINITY, ahead[u][r]);
+                    if (kCap) most[u] = fmaxf(r ? most[u] : 0.f, fabsf(ahead[u][r]));
                 }
-            if (!kCap && z == kFrom + kZ / 2 - 1) {
+            if (z == kFrom + kZ / 2 - 1) {
 #pragma unroll
                 for (int u = 0; u < kQT; ++u) {
                     asm volatile("" : "+v"(m[u]));   // taken here, among the products, and not where it is used
                     top[u] = m[u];
                 }
-                too_high = score_high(top);
+                look(most);
             }
-            __builtin_amdgcn_sched_barrier(0);
+            if (!kCap || z % 2) __builtin_amdgcn_sched_barrier(0);
         }
     };
     // values of keys k0 .. at (vbuf, part); keys of k0 + 64 .. at (kbuf, part)
     auto step = [&](int k0, const char *vbuf, const char *kbuf, int part, f32x16_t (&s)[kQT], f32x16_t (&ahead)[kQT]) PLD_INLINE {
         if (seen(k0)) {
             const bool masked = k0 < full_lo || k0 + 32 > full_hi;
-            if (kCap) cap(s);
             if (masked) mask(k0, s);
-            if (kCap || masked) {
+            if (masked || (kCap && far)) {
 #pragma unroll
                 for (int t = 0; t < kQT; ++t) top[t] = largest(s[t]);
+                if (kCap) settle_top(top, far);
                 too_high = score_high(top);
             }
             if (too_high) raise(top);
+            if (kCap) settle(s, far);
             products(vbuf, kbuf, part, s, ahead);
         } else {
             if (seen(k0 + 32)) first_scores(ahead);
@@ -407,13 +446,14 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
         fetch_at(kbase + (int64_t)(k0 + 2 * kKeys) * kstride, koff, kOdd, false);
         fetch_at(vbase + (int64_t)(k0 + kKeys) * vstride, voff, !kOdd, true);
         auto whole = [&](int part, f32x16_t (&s)[kQT], f32x16_t (&ahead)[kQT]) PLD_INLINE {
-            if constexpr (kCap) {
-                cap(s);
+            if (kCap && far) {
 #pragma unroll
                 for (int t = 0; t < kQT; ++t) top[t] = largest(s[t]);
+                settle_top(top, true);
                 too_high = score_high(top);
             }
             if (too_high) raise(top);
+            if (kCap) settle(s, far);
             products(s_v[kOdd], s_k[!kOdd], part, s, ahead);
         };
         whole(0, s0, s1);
@@ -484,7 +524,6 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
                 if (!seen(k0)) continue;
                 const uint32_t bad = s_bad[part] >> 4 * h;
                 scores(s_k[0], part, s0);
-                if (kCap) cap(s0);
 #pragma unroll
                 for (int t = 0; t < kQT; ++t)
 #pragma unroll
@@ -493,7 +532,9 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
                 mask(k0, s0);
 #pragma unroll
                 for (int t = 0; t < kQT; ++t) top[t] = largest(s0[t]);
+                if (kCap) settle_top(top, true);
                 raise(top);
+                if (kCap) settle(s0, true);
                 uint32_t w[kQT][8];
 #pragma unroll
                 for (int t = 0; t < kQT; ++t)
@@ -545,15 +586,11 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
     }
 }
 
-template <int D, int kQT, int kWaves>
+template <int D, int kQT, int kWaves, bool kCap>
 static void launch_prompt(PromptArgs &a, hipStream_t s) {
     constexpr int rows = PromptTile<D, kQT, kWaves>::kRows;
     a.tiles = ((int64_t)a.p.N * a.G + rows - 1) / rows;
-    const dim3 grid = wide_grid(a.tiles * a.heads);
-    if (a.cap > 0.f)
-        hipLaunchKernelGGL((prompt_attn_kernel<D, kQT, kWaves, true>), grid, dim3(kWaves * 64), 0, s, a);
-    else
-        hipLaunchKernelGGL((prompt_attn_kernel<D, kQT, kWaves, false>), grid, dim3(kWaves * 64), 0, s, a);
+    hipLaunchKernelGGL((prompt_attn_kernel<D, kQT, kWaves, kCap>), wide_grid(a.tiles * a.heads), dim3(kWaves * 64), 0, s, a);
 }
 
 }  // namespace pld
@@ -584,6 +621,7 @@ extern "C" int pld_prompt_attn(const uint16_t *q, int64_t q_row_stride, const ui
     a.G = Hq / heads, a.heads = heads;
     a.c1 = scale * kLog2E;
     a.cap = softcap * kLog2E, a.cap_x2 = 2.f * a.cap, a.cap_near = kCapNear * a.cap;
+    a.inv_cap = softcap > 0.f ? (float)((double)scale / softcap) : 0.f;
     a.inv2_log2e = softcap > 0.f ? (float)(2. * kLog2E / a.cap) : 0.f;
     // (the way back from log2 units is by the rounded factor that led there)
     a.nat = softcap > 0.f ? (float)((double)softcap / a.cap) : (float)((double)scale / a.c1);
@@ -596,17 +634,19 @@ extern "C" int pld_prompt_attn(const uint16_t *q, int64_t q_row_stride, const ui
     // 53.0 and 54.5, of 16384 1927 and 2206; 64 of 300 150 and 137, 16 of 1000 193 and 198.  Heads of
     // 64, whose vector instructions bound them, gain where a wave of 64 rows reads each value once for two
     // products: 2 x 8192 538 and 597, 4 x 4096 319 and 341, one of 4096 95 and 91, 2048 39 and 32, 16 x 1000
-    // 111 and 107, capped in a window of 1000 187 and 176.
+    // 111 and 107, in a window of 1000 187 and 176.  Not with a cap, whose instructions come on top: 4 x 4096
+    // 470 and 450.
     const int64_t wide = ((int64_t)N * a.G + 255) / 256 * heads;
-    if (head_dim == 64 && wide >= 1024 && N >= (int64_t)B * 3000)
-        launch_prompt<64, 2, 4>(a, s);
+    const bool cap = softcap > 0.f, wide128 = wide >= 256 && N >= (int64_t)B * 512;
+    if (head_dim == 64 && !cap && wide >= 1024 && N >= (int64_t)B * 3000)
+        launch_prompt<64, 2, 4, false>(a, s);
     else if (head_dim == 64)
-        launch_prompt<64, 1, 4>(a, s);
-    else if (head_dim == 128 && wide >= 256 && N >= (int64_t)B * 512)
-        launch_prompt<128, 1, 8>(a, s);
+        cap ? launch_prompt<64, 1, 4, true>(a, s) : launch_prompt<64, 1, 4, false>(a, s);
+    else if (head_dim == 128 && wide128)
+        cap ? launch_prompt<128, 1, 8, true>(a, s) : launch_prompt<128, 1, 8, false>(a, s);
     else if (head_dim == 128)
-        launch_prompt<128, 1, 4>(a, s);
+        cap ? launch_prompt<128, 1, 4, true>(a, s) : launch_prompt<128, 1, 4, false>(a, s);
     else
-        launch_prompt<256, 1, 4>(a, s);
+        cap ? launch_prompt<256, 1, 4, true>(a, s) : launch_prompt<256, 1, 4, false>(a, s);
     return hipGetLastError() == hipSuccess ? PLD_OK : PLD_ERR_LAUNCH;
 }

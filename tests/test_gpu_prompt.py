@@ -100,6 +100,20 @@ def test_attn_long(D, Hq, heads):
     assert p.check(rows=rows, window=1000, softcap=20.0) == len(rows) * Hq
 
 
+def test_attn_long_of_narrow_heads():
+    """Heads of 64 where a wave has 64 rows: the ends of tiles and sequences, a window, what is not finite."""
+    p = Prompt([5000, 1101], 48, 8, 64, 3, 11, seed=6)
+    rows = {0, 3, 4, 66, 67, 68, 130, 131, 1026, 3000, 4999, 5002, 5003, 5004, 5066, 5067, 6000, 6102, 6103, 6113}
+    assert p.check(rows=rows) == (len(rows) - 2) * 48
+    a, la = p.attend(window=1000)
+    assert p.check(rows=rows, window=1000) == (len(rows) - 2) * 48
+    p.v[1], p.k[2], p.v[500], p.k[6105] = INF, NAN, NAN, INF
+    b, lb = p.attend(window=1000)
+    seen = torch.ones(p.N, dtype=torch.bool, device=dev())
+    seen[500:1500] = False                          # (rows that see the NaN)
+    assert torch.equal(a[seen], b[seen]) and torch.equal(la[seen], lb[seen]) and b[500:1500].isnan().all()
+
+
 def test_attn_random_shapes():
     rng, iters = random_plan(11, 24)
     for it in range(iters):
@@ -173,6 +187,20 @@ def test_attn_in_place_and_without_lse():
     kept = torch.cat([q[:1], q[161:]])
     a.attend(lse=False, out=a.q)
     assert (bits(a.q[1:161]) == bits(o[1:161])).all() and torch.equal(torch.cat([a.q[:1], a.q[161:]]), kept)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_attn_capped_scores_go_by_themselves(D):
+    """Far scores beside a row's own, or unseen ones of the same tiles, do not change its bits."""
+    p = Prompt([40, 100, 300], Hq=6, heads=2, D=D, seed=4)
+    a, la = p.attend(softcap=30.0)
+    p.q[140:] *= 40.0
+    b, lb = p.attend(softcap=30.0)
+    assert torch.equal(a[:140], b[:140]) and torch.equal(la[:140], lb[:140])
+    p.k[100:140] *= 60.0                            # far for the rows that see them, not for those before
+    c, lc = p.attend(softcap=30.0)
+    assert torch.equal(a[:100], c[:100]) and torch.equal(la[:100], lc[:100]) and not torch.equal(a[100:140], c[100:140])
+    p.check(softcap=30.0)
 
 
 def test_attn_many_empty_sequences():
