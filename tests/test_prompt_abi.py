@@ -77,6 +77,14 @@ def test_write_refusals():
 
 
 @no_gpu
+def test_write_refuses_outputs_over_inputs():
+    fn, c = pld._load().pld_cache_write_packed, _cache()
+    apart = {**WRITE, **dict(k=P(0x20000), v=P(0x30000), out=P(0x40000), ko=P(0x50000))}
+    for bad in (dict(out=P(0x20000)), dict(out=P(0x30000)), dict(ko=WRITE["q"]), dict(ko=P(0x30000)), dict(ko=P(0x40000))):
+        assert fn(c, *{**apart, **bad}.values()) == 1, bad
+
+
+@no_gpu
 def test_attn_refusals():
     fn = pld._load().pld_prompt_attn
 
