@@ -58,12 +58,13 @@ int pld_prompt_version(void);
  *   positions   int32, axis a's row r at a*axis_stride + r; NULL: the cache's
  *               position on every axis (axes and pair_axis are not used)
  *   axes        1 .. PLD_MAX_AXES;  axis_stride >= N
- *   pair_axis   int32 [rot_dim/2], 16-byte aligned, values in [0, axes-1]; NULL: axis 0.  An entry
- *               out of range counts as axis 0
+ *   pair_axis   int32 [rot_dim/2], 16-byte aligned, values in [0, axes-1] (others count as 0);
+ *               NULL: axis 0
  *   starts, first   int32 [B+1] and [B];  B 1 .. 65535
  *   q_out       bf16 [N][Hq][head_dim]; may be q itself with q's stride
  *   k_out       bf16 [N][heads][head_dim], the finished keys as pld_prompt_attn
- *               takes them; may be k itself with k's stride; or NULL
+ *               takes them; may be k itself with k's stride; or NULL.  Outputs overlap nothing
+ *               else
  * Device-side rule: a row whose position in the cache is negative or past the table
  * of pages, whose page is bad, or one of whose pairs' positions is outside [0, n_pos)
  * (with rope), is not stored, and its q_out and k_out are NaN.  Two rows of one call
@@ -92,10 +93,10 @@ int pld_cache_write_packed(const pld_cache *cache, const uint16_t *q, int64_t q_
  *               multiples of 8 elements
  *   heads       1 .. 1024;  Hq a multiple of it, up to 4096;  head_dim 64, 128 or 256
  *   scale, softcap, window   as pld_cache_attn
- *   out         bf16 [N][Hq][head_dim]; may be q itself with q's stride
+ *   out         bf16 [N][Hq][head_dim]; may be q itself with q's stride, not k or v
  *   lse         fp32 [N][Hq] or NULL
  * Device-side rules: rows that a row does not see do not affect it, whatever they
- * hold.  Where a query, or a key or value that a row sees, is not finite, that head of
+ * hold; a row's bits are the same from run to run.  Where a query, or a key or value that a row sees, is not finite, that head of
  * its out, and its lse, may be NaN as a whole.  The ranges of values and scores are
  * pld_cache_attn's: values up to 2^89, and a score above -1e29 for every row.  (A
  * block of rows that meets what is not finite is computed twice.)
@@ -120,7 +121,7 @@ int pld_prompt_attn(const uint16_t *q, int64_t q_row_stride, const uint16_t *k,
 typedef struct pld_pool {
     int32_t *table;        /* [seqs][table_stride] */
     int64_t table_stride;  /* >= max_pages */
-    int32_t *refs;         /* [num_pages] */
+    int32_t *refs;         /* [num_pages], 16-byte aligned */
     int seqs;              /* 1 .. 2^20 */
     int max_pages;         /* table entries per sequence; max_pages*page_size <= 2^30 */
     int num_pages;         /* 1 .. PLD_MAX_PAGES */
@@ -183,7 +184,8 @@ int pld_pages_fork(const pld_pool *pool, const pld_cache *layers, int n_layers, 
  *   map         int32 [num_pages], written: a page's new index, -1 for a free one
  *   used        int32 [1], written: n
  *   table_out, refs_out   the new table ([seqs][table_out_stride]; entries that name no
- *               page as they were) and references; may be the pool's own
+ *               page as they were, -1 for those that name a free one) and references; may be
+ *               the pool's own
  *   workspace   as pld_pages_take with count 1
  */
 int pld_pages_compact(const pld_pool *pool, const pld_cache *layers, int n_layers, int32_t *map,
