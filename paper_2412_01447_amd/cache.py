@@ -116,6 +116,8 @@ class PagePool:
     Calls on one pool follow each other (one stream, or events between): there is one workspace."""
 
     def __init__(self, k_caches, v_caches, k_scales=None, v_scales=None, table=None, refs=None):
+        if not k_caches or (table is None) != (refs is None):
+            raise TypeError("a pool has caches, and a table and references or neither")
         self.layers = PageLayers(k_caches, v_caches, k_scales, v_scales)
         self.table, self.refs = table, refs
         self.pages = None if table is None else PageTable(table, refs, k_caches[0].shape[1])

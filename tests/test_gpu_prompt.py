@@ -733,6 +733,29 @@ def test_copy_far_pages():
     assert torch.equal(v[699], v[3]) and (v[2] == 0).all()
 
 
+def test_compacting_and_copying_captured():
+    """The same graph over other contents of the pool, eager calls between the replays."""
+    p = Pages(5, 4, 24, layers=2, seed=2)
+    page_map, used = torch.zeros(24, dtype=torch.int32, device=dev()), torch.zeros(1, dtype=torch.int32, device=dev())
+    p.pool.reserve(5)
+    src, dst, slots = d_i32([0, 1]), d_i32([22, 23]), d_i32([16, 3])
+    g, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(g, stream=s):
+        p.pool.compact(page_map, used)
+        p.pool.copy_from(p.pool, src, dst, slots)
+    for ended in ([0], [1, 3], [], [2, 4], [0, 1, 2, 3, 4]):
+        p.take([0, 1, 2, 3, 4], [60, 17, 33, 1, 64])
+        if ended:                      # (a call names one at least)
+            p.free(ended)
+        before = p.contents()
+        g.replay()
+        new, n, moves = p.model.compact()
+        p.moved(before, [(a, b, 1 << 20) for a, b in moves])
+        p.same(p.moved(before, [(0, 22, 16), (1, 23, 3)]))
+        assert np.array_equal(page_map.cpu().numpy(), new) and used.item() == n
+
+
 def test_prepared_page_calls():
     """Calls marshalled once, issued again and again."""
     p = Pages(4, 4, 20)

@@ -196,6 +196,13 @@ def test_host_tensors_and_odd_arguments_are_refused():
             call()
 
 
+def test_pools_that_are_not_whole():
+    t, r, k = torch.zeros(1, 1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros(1, 16, 1, 64, dtype=torch.bfloat16)
+    for args in (([], [], None, None, t, r), ([k], [k], None, None, t, None), ([k], [k], None, None, None, r)):
+        with pytest.raises(TypeError):
+            PagePool(*args)
+
+
 def test_prepared_page_calls_keep_their_structs():
     """A prepared page call holds its pool and its array of caches by itself."""
     import gc
