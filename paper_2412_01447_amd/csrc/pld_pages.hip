@@ -21,9 +21,11 @@ struct Pool {
 // The integers' block: 1024 threads, kRun pages of the references each.
 constexpr int kPoolThreads = 1024, kPoolWaves = kPoolThreads / kWave;
 constexpr int kRun = 16, kSpan = kPoolThreads * kRun;   // pages of one step: 16384
-// One block goes through a call's sequences, a wave each, and gives out the pages in the same launch;
-// more sequences than it has waves, or more entries than this, take launches of a wave a sequence.
-constexpr int64_t kOneBlock = 1 << 14;
+// One block goes through a call's sequences, a wave each, and gives out the pages in the same launch, up to as
+// many as it has waves: a take of one and of 16 sequences 3.6 us, 8.4 with launches of their own, of 16 with 16384
+// entries each 10.4 and 12.6.  A fork changes every entry, and so up to this many of all sequences: one of 4096 11.8 and
+// 12.4 us, 16 of 64 12.8 and 12.9, but 16 of 1024 15.6 and 13.2, of 4096 31 and 17.
+constexpr int64_t kOneBlock = 1 << 12;
 
 struct PoolWork {                // the workspace, in this order
     int32_t *head;               // [16]: pages in use, moves
@@ -64,9 +66,17 @@ __device__ __forceinline__ void block_sync() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __syncthreads();
 }
-// References change by atomics, at the L2: not read from a CU's own cache.
-__device__ __forceinline__ int refs_at(const int32_t *p) {
-    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+
+// Table entries that a wave takes at a time, eight a lane: their loads are under way together.  A fork of one sequence
+// of 16384 entries, with a page taken, 83 us with one a lane by one wave, 22 with eight a lane by 32 waves.
+constexpr int kRow = 8, kEntries = kWave * kRow;
+// Those of a sequence from p0 on, below end; behind it: page 0.
+__device__ __forceinline__ void load_entries(const int32_t *e, int p0, int end, int (&v)[kRow]) {
+#pragma unroll
+    for (int k = 0; k < kRow; ++k) {
+        const int p = p0 + k * kWave + lane_id();
+        v[k] = p < end ? e[p] : 0;
+    }
 }
 
 // Whether `seq` is named by any entry of `by` but the i-th (a wave).
@@ -84,36 +94,45 @@ __device__ __forceinline__ void count_lacking(const EditArgs &a, int i) {
     if ((uint32_t)s < (uint32_t)a.p.seqs && pages <= a.p.max_pages && !named_by(a.seq, a.count, s, i)) {
         const int32_t *e = entries_of(a.p, s);
         n = 0;
-#pragma unroll 4
-        for (int p = lane_id(); p < (int)pages; p += kWave) n += !is_page(a.p, e[p]);
+        for (int p0 = 0; p0 < (int)pages; p0 += kEntries) {
+            int v[kRow];
+            load_entries(e, p0, (int)pages, v);
+#pragma unroll
+            for (int k = 0; k < kRow; ++k) n += !is_page(a.p, v[k]);
+        }
         n = wave_sum_i32(n);
     }
     if (lane_id() == 0) a.w.lacks[i] = n;
 }
 
-// fork, entry i (a wave): what the sequence had is given back, whole pages are shared.
-__device__ __forceinline__ void share(const EditArgs &a, int i) {
+// fork, entry i (a wave, one of `parts`): what the sequence had is given back, whole pages are shared.
+__device__ __forceinline__ void share(const EditArgs &a, int i, int part, int parts) {
     const int s = a.src[i], d = a.seq[i], T = a.lens[i], last = T > 0 ? (T - 1) >> a.p.shift : -1;
     const bool ok = (uint32_t)s < (uint32_t)a.p.seqs && (uint32_t)d < (uint32_t)a.p.seqs && T >= 0 &&
                     last < a.p.max_pages && !named_by(a.seq, a.count, d, i) &&
                     !named_by(a.src, a.count, d, -1);
     const int tail = ok && T > 0 ? entries_of(a.p, s)[last] : -1;
     if (!ok || (T > 0 && !is_page(a.p, tail))) {
-        if (lane_id() == 0) a.w.lacks[i] = -1;
+        if (part == 0 && lane_id() == 0) a.w.lacks[i] = -1;
         return;
     }
     const int32_t *from = entries_of(a.p, s);
     int32_t *e = entries_of(a.p, d);
-#pragma unroll 4
-    for (int p = lane_id(); p < a.p.max_pages; p += kWave) {
-        const int old = e[p];
-        int x = p < last ? from[p] : -1;
-        if (!is_page(a.p, x)) x = -1;
-        if (is_page(a.p, old)) atomicSub(a.p.refs + old, 1);
-        if (x >= 0) atomicAdd(a.p.refs + x, 1);
-        if (x != old) e[p] = x;
+    for (int p0 = part * kEntries; p0 < a.p.max_pages; p0 += parts * kEntries) {
+        int old[kRow], x[kRow];
+        load_entries(e, p0, a.p.max_pages, old);
+        load_entries(from, p0, max(last, 0), x);
+#pragma unroll
+        for (int k = 0; k < kRow; ++k) {
+            const int p = p0 + k * kWave + lane_id();
+            if (p >= a.p.max_pages) break;
+            if (p >= last || !is_page(a.p, x[k])) x[k] = -1;
+            if (is_page(a.p, old[k])) atomicSub(a.p.refs + old[k], 1);
+            if (x[k] >= 0) atomicAdd(a.p.refs + x[k], 1);
+            if (x[k] != old[k]) e[p] = x[k];
+        }
     }
-    if (lane_id() == 0) {
+    if (part == 0 && lane_id() == 0) {
         a.w.lacks[i] = T > 0;
         a.w.from[i] = tail;
         a.w.slots[i] = T > 0 ? ((T - 1) & ((1 << a.p.shift) - 1)) + 1 : 0;
@@ -146,10 +165,9 @@ __device__ __forceinline__ T block_excl_scan(T v, T &total, T *s_w) {
 }
 
 // Which of a thread's run of pages are in use: a bit each (none past the end).
-template <bool kFresh>
 __device__ __forceinline__ uint32_t used_bits(const Pool &p, int x0) {
     uint32_t bits = 0;
-    if (!kFresh && x0 + kRun <= p.num_pages) {
+    if (x0 + kRun <= p.num_pages) {
         int4 v[kRun / 4];
 #pragma unroll
         for (int k = 0; k < kRun / 4; ++k) v[k] = reinterpret_cast<const int4 *>(p.refs + x0)[k];
@@ -159,14 +177,14 @@ __device__ __forceinline__ uint32_t used_bits(const Pool &p, int x0) {
     } else {
 #pragma unroll
         for (int k = 0; k < kRun; ++k)
-            if (x0 + k < p.num_pages) bits |= (uint32_t)((kFresh ? refs_at(p.refs + x0 + k) : p.refs[x0 + k]) > 0) << k;
+            if (x0 + k < p.num_pages) bits |= (uint32_t)(p.refs[x0 + k] > 0) << k;
     }
     return bits;
 }
 
 // The pages that entries lack, lowest first, into `list`; each entry's place in it, and status
-// (a block).  kFresh: the references were changed in this launch.
-template <bool kFork, bool kFresh>
+// (a block).
+template <bool kFork>
 __device__ __forceinline__ void give_out(const EditArgs &a) {
     __shared__ int s_w[kPoolWaves], s_served;
     __shared__ int64_t s_wide[kPoolWaves];
@@ -180,7 +198,7 @@ __device__ __forceinline__ void give_out(const EditArgs &a) {
     if (threadIdx.x == 0) s_served = 0;
     for (int x = 0; x < a.p.num_pages && found < total; x += kSpan) {
         const int x0 = x + (int)threadIdx.x * kRun;
-        uint32_t bits = x0 < a.p.num_pages ? used_bits<kFresh>(a.p, x0) : 0;
+        uint32_t bits = x0 < a.p.num_pages ? used_bits(a.p, x0) : 0;
         const int n = min(kRun, a.p.num_pages - x0);
         bits = n > 0 ? ~bits & ((1u << n) - 1) : 0;
         int here, k = found + block_excl_scan((int)__popc(bits), here, s_w);
@@ -208,12 +226,16 @@ __device__ __forceinline__ void fill(const EditArgs &a, int i) {
     if (at < 0) return;
     int32_t *e = entries_of(a.p, a.seq[i]);
     const int pages = (int)(((int64_t)a.lens[i] + (1 << a.p.shift) - 1) >> a.p.shift);
-    for (int p0 = 0; p0 < pages; p0 += kWave) {
-        const int p = p0 + lane_id();
-        const bool lacks = p < pages && !is_page(a.p, e[p]);
-        const uint64_t all = __ballot(lacks);
-        if (lacks) e[p] = a.w.list[at + __popcll(all & lanemask_lt())];
-        at += __popcll(all);
+    for (int p0 = 0; p0 < pages; p0 += kEntries) {
+        int v[kRow];
+        load_entries(e, p0, pages, v);
+#pragma unroll
+        for (int k = 0; k < kRow; ++k) {
+            const bool lacks = !is_page(a.p, v[k]);
+            const uint64_t all = __ballot(lacks);
+            if (lacks) e[p0 + k * kWave + lane_id()] = a.w.list[at + __popcll(all & lanemask_lt())];
+            at += __popcll(all);
+        }
     }
 }
 
@@ -233,22 +255,26 @@ __device__ __forceinline__ void finish_fork(const EditArgs &a, int i) {
     }
 }
 
-// A wave a sequence.
+// A wave a sequence; of a fork, gridDim.y of them.
 template <bool kFork>
 __global__ __launch_bounds__(256) void pages_edit_kernel(EditArgs a) {
     const int i = (int)(blockIdx.x * 4 + threadIdx.x / kWave);
     if (i >= a.count) return;
-    kFork ? share(a, i) : count_lacking(a, i);
+    kFork ? share(a, i, blockIdx.y, gridDim.y) : count_lacking(a, i);
 }
-// One block: with kEdit the sequences' part too, a wave for each in turn.
+// One block: with kEdit the sequences' part too, a wave each, or of forks as many as there are.
 template <bool kFork, bool kEdit>
 __global__ __launch_bounds__(kPoolThreads) void pages_give_kernel(EditArgs a) {
     const int wave = (int)threadIdx.x / kWave;
     if constexpr (kEdit) {
-        if (wave < a.count) kFork ? share(a, wave) : count_lacking(a, wave);
+        const int parts = kFork ? min(kPoolWaves / a.count, (a.p.max_pages + kEntries - 1) / kEntries) : 1;
+        const int part = wave / a.count;
+        if (part < parts) kFork ? share(a, wave - part * a.count, part, parts) : count_lacking(a, wave);
         block_sync();
+        // references change by atomics, at the L2: what this CU's own cache holds of them is old
+        if constexpr (kFork) __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
     }
-    give_out<kFork, kFork && kEdit>(a);
+    give_out<kFork>(a);
     if constexpr (!kFork && kEdit) {
         block_sync();
         if (wave < a.count) fill(a, wave);
@@ -259,7 +285,8 @@ __global__ __launch_bounds__(256) void pages_fill_kernel(EditArgs a) {
     if (i < a.count) fill(a, i);
 }
 
-// Entries are exchanged, so that one that two name is given back once.
+// Entries are exchanged, so that one that two name is given back once.  A thread an entry, for up to 16384 of a sequence:
+// four took 2 to 3 us more (1024 entries taken and given back, 11.3 us).
 __global__ __launch_bounds__(256) void pages_free_kernel(Pool p, const int32_t *seq, const int32_t *keep) {
     const int s = seq[blockIdx.x];
     if ((uint32_t)s >= (uint32_t)p.seqs) return;
@@ -283,7 +310,7 @@ __global__ __launch_bounds__(kPoolThreads) void pages_span_kernel(Pool p, PoolWo
     __shared__ int s_w[kPoolWaves];
     const int x0 = (int)(blockIdx.x * kPoolThreads + threadIdx.x) * kRun;
     int total;
-    block_excl_scan(x0 < p.num_pages ? (int)__popc(used_bits<false>(p, x0)) : 0, total, s_w);
+    block_excl_scan(x0 < p.num_pages ? (int)__popc(used_bits(p, x0)) : 0, total, s_w);
     if (threadIdx.x == 0) w.spans[blockIdx.x] = total;
 }
 __global__ __launch_bounds__(kPoolThreads) void pages_rank_kernel(Pool p, PoolWork w) {
@@ -295,7 +322,7 @@ __global__ __launch_bounds__(kPoolThreads) void pages_rank_kernel(Pool p, PoolWo
         block_excl_scan(threadIdx.x < blockIdx.x ? mine : 0, before, s_w);
     }
     const int x0 = (int)(blockIdx.x * kPoolThreads + threadIdx.x) * kRun;
-    const uint32_t bits = x0 < p.num_pages ? used_bits<false>(p, x0) : 0;
+    const uint32_t bits = x0 < p.num_pages ? used_bits(p, x0) : 0;
     int here;
     int r = before + block_excl_scan((int)__popc(bits), here, s_w);
     if (gridDim.x == 1) n = here;
@@ -543,12 +570,13 @@ static int check_work(const pld_pool *p, int count, void *ws, size_t bytes, Pool
     return PLD_OK;
 }
 
-// The two launches before a copy or a filling (one where there are few entries).
+// The launches before a copy or a filling: two, or one (kOneBlock).
 template <bool kFork>
 static bool launch_edit(const EditArgs &a, hipStream_t s) {
-    const bool one = a.count <= kPoolWaves && (int64_t)a.count * a.p.max_pages <= kOneBlock;
+    const bool one = a.count <= kPoolWaves && (!kFork || (int64_t)a.count * a.p.max_pages <= kOneBlock);
+    const int parts = kFork ? std::min((a.p.max_pages + kEntries - 1) / kEntries, 64) : 1;
     if (!one)
-        hipLaunchKernelGGL(pages_edit_kernel<kFork>, dim3((a.count + 3) / 4), dim3(256), 0, s, a);
+        hipLaunchKernelGGL(pages_edit_kernel<kFork>, dim3((a.count + 3) / 4, parts), dim3(256), 0, s, a);
     if (one)
         hipLaunchKernelGGL((pages_give_kernel<kFork, true>), dim3(1), dim3(kPoolThreads), 0, s, a);
     else
@@ -586,7 +614,7 @@ extern "C" int pld_pages_free(const pld_pool *pool, const int32_t *seq, const in
     if (const int rc = check_pool(pool, p); rc != PLD_OK) return rc;
     if (!seq || count < 1 || count > PLD_MAX_PAGE_ENTRIES) return PLD_ERR_INVALID;
     if (((uintptr_t)seq | (uintptr_t)keep) % 4) return PLD_ERR_ALIGN;
-    const int parts = (p.max_pages + 1023) / 1024;
+    const int parts = (p.max_pages + 255) / 256;
     hipLaunchKernelGGL(pages_free_kernel, dim3(count, parts < 64 ? parts : 64), dim3(256), 0, (hipStream_t)stream, p, seq, keep);
     return hipGetLastError() == hipSuccess ? PLD_OK : PLD_ERR_LAUNCH;
 }

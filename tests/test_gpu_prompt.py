@@ -656,6 +656,31 @@ def test_pages_of_a_large_pool():
     assert p.take([5], [3200]) == [0]
 
 
+@pytest.mark.parametrize("n", [1, 3, 20])
+def test_pages_of_long_sequences(n):
+    """More entries a sequence than a wave takes at a time, by one block's waves and by launches of their own."""
+    p = Pages(3 * n, 1500, 2200 * n, layers=1, heads=1, seed=n)
+    rng, own, new = p.rng, list(range(n)), list(range(n, 2 * n))
+    assert p.take(own, [int(x) for x in rng.integers(513 * 16, 1100 * 16, n)]) == [0] * n
+    held = [int((p.model.table[s] >= 0).sum()) for s in own]
+    lens = [int(rng.integers((h - 20) * 16, h * 16)) for h in held]
+    assert p.fork(own, new, lens) == [0] * n
+    assert p.take(new, [x + 700 for x in lens]) == [0] * n
+    p.free(own, [int(rng.integers(0, 600 * 16)) for _ in own])
+    p.model.table[new[0], 5:700:3] = -1                             # entries that name no page, some out of range
+    p.model.table[new[0], 6:700:9] = 1 << 30
+    p.pool.table.copy_(d_i32(p.model.table))
+    used = np.unique(p.model.table[(p.model.table >= 0) & (p.model.table < p.model.P)], return_counts=True)
+    p.model.refs[:] = 0
+    p.model.refs[used[0]] = used[1]
+    p.pool.refs.copy_(d_i32(p.model.refs))
+    assert p.fork(new, list(range(2 * n, 3 * n)), lens) == [0] * n
+    p.take(list(range(2 * n, 3 * n)), [1500 * 16] * n)              # whole tables, as far as there are pages
+    p.take(new, [x + 3000 for x in lens])
+    p.compact(apart=True)
+    p.free(list(range(3 * n)), [600 * 16] * 3 * n)
+
+
 def test_pages_held_by_the_caller():
     """A page with a reference of the caller's own stays in use, and moves."""
     p = Pages(2, 3, 9)
