@@ -255,7 +255,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
     auto capped = [&](float s, float less) PLD_INLINE {
         const float x = s * a.c1, e = __builtin_amdgcn_exp2f(fabsf(x) * a.inv2_log2e);
         const float far = copysignf(a.cap - a.cap_x2 * __builtin_amdgcn_rcpf(e + 1.f), x) - less;
-        return s == -INFINITY ? s : fabsf(x) >= a.cap_near ? far : fmaf(s, near(s), -less);
+        return fabsf(x) >= a.cap_near ? far : fmaf(s, near(s), -less);
     };
     auto mask = [&](int k0, f32x16_t (&s)[kQT]) PLD_INLINE {
 #pragma unroll
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
     auto settle_top = [&](float (&top)[kQT], bool far) PLD_INLINE {
         set_fit(true);
 #pragma unroll
-        for (int t = 0; t < kQT; ++t) top[t] = far ? capped(top[t], 0.f) : top[t] * near(top[t]);
+        for (int t = 0; t < kQT; ++t) top[t] = far && top[t] > -INFINITY ? capped(top[t], 0.f) : top[t] * near(top[t]);
     };
     auto settle = [&](f32x16_t (&s)[kQT], bool far) PLD_INLINE {
 #pragma unroll
@@ -435,6 +435,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
             }
             if (too_high) raise(top);
             if (kCap) settle(s, far);
+            if (kCap && far && masked) mask(k0, s);   // (once more: an infinite score is capped, and no mask)
             products(vbuf, kbuf, part, s, ahead);
         } else {
             if (seen(k0 + 32)) first_scores(ahead);
@@ -547,7 +548,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
                 for (int t = 0; t < kQT; ++t) top[t] = largest(s0[t]);
                 if (kCap) settle_top(top, true);
                 raise(top);
-                if (kCap) settle(s0, true);
+                if (kCap) settle(s0, true), mask(k0, s0);
                 uint32_t w[kQT][8];
 #pragma unroll
                 for (int t = 0; t < kQT; ++t)

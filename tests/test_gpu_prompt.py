@@ -203,6 +203,31 @@ def test_attn_capped_scores_go_by_themselves(D):
     p.check(softcap=30.0)
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("sign,cap", [(1, 5.0), (-1, 0.5)])
+def test_attn_infinite_capped_scores(D, sign, cap):
+    """A key that makes scores infinite: the cap on either side, or NaN for the head as a whole."""
+    p = Prompt([200], Hq=4, heads=2, D=D, seed=8)
+    p.k[70, :, 3] = sign * INF
+    o, L = p.attend(softcap=cap)
+    q, k, v, o, L = f64(p.q), f64(p.k), f64(p.v), f64(o), L.cpu().numpy()
+    met = 0
+    for r in range(200):
+        for h in range(4):
+            s = cap * np.tanh(k[:r + 1, h // 2] @ q[r, h] * D ** -0.5 / cap)
+            w = np.exp(s - s.max())
+            want, size = w @ v[:r + 1, h // 2] / w.sum(), w @ np.abs(v[:r + 1, h // 2]) / w.sum()
+            if r >= 70 and np.isnan(L[r, h]):
+                assert np.isnan(o[r, h]).all()
+                continue
+            met += r >= 70
+            # a weight's rounding, the output's, and the scores': (D + 8) 2^-24 of products whose sizes sum to 160 at most
+            tol = (D + 8) * U * 160
+            assert np.all(np.abs(o[r, h] - want) <= 2.0 ** -8 * (np.abs(want) + size) + 4 * tol * size)
+            assert abs(L[r, h] - (np.log(w.sum()) + s.max())) <= 2 * tol + 1e-5
+    say("infinite scores met", met)
+
+
 def test_attn_many_empty_sequences():
     lens = np.zeros(60000, int)
     lens[[0, 7, 30000, 30001, 59998]] = [5, 70, 1, 40, 3]
