@@ -277,7 +277,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
     auto raise = [&](const float (&top)[kQT]) PLD_INLINE {
 #pragma unroll
         for (int t = 0; t < kQT; ++t) {
-            const float all = pair_max(top[t] * c), mn = fmaf(1.f, all, -mx[t]) > kSlack ? all : mx[t];
+            const float all = pair_max(top[t]), mn = fmaf(all, c, -mx[t]) > kSlack ? all * c : mx[t];   // (as score_high)
             const float f = __builtin_amdgcn_exp2f(mx[t] - mn);
             mx[t] = mn;
             l[t] *= f;
