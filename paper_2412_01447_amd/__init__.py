@@ -1001,10 +1001,11 @@ def pld_pages_compact(pages, layers, page_map, used, workspace, table_out=None, 
     _ints(page_map, "page_map", pages.refs.shape[0])
     _ints(refs_out, "refs_out", pages.refs.shape[0])
     _ints(used, "used", 1)
+    # (the stride of a single row is never used; rows that overlap are refused)
+    stride = max(ts[0], table_out.shape[1]) if table_out.shape[0] == 1 else ts[0]
     return _run("pld_pages_compact", (
         pages.pool, layers.caches, layers.count, page_map.data_ptr(), used.data_ptr(), table_out.data_ptr(),
-        max(ts[0], table_out.shape[1]), refs_out.data_ptr(), workspace.data_ptr(), _nbytes(workspace),
-        _stream(stream)), prepare)
+        stride, refs_out.data_ptr(), workspace.data_ptr(), _nbytes(workspace), _stream(stream)), prepare)
 
 
 def pld_pages_copy(layers_from, layers_to, src, dst, slots=None, stream=None, prepare=False):

@@ -849,6 +849,17 @@ def test_pool_refusals():
             call()
 
 
+def test_compact_refuses_rows_that_overlap():
+    p = Pages(3, 4, 8)
+    page_map, used = d_i32([9] * 8), d_i32([9])
+    for t in (d_i32([0] * 4).expand(3, 4), d_i32([0] * 12).as_strided((3, 4), (3, 1))):
+        with pytest.raises(pld.PLDError):
+            p.pool.compact(page_map, used, table_out=t)
+        with pytest.raises(pld.PLDError):
+            PagePool(p.k, p.v, table=t, refs=p.pool.refs).compact(page_map, used)
+    assert (page_map == 9).all() and used.item() == 9
+
+
 # ------------------------------------------------------------- a run of them
 @pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
 def test_prompts_forks_and_verification(dtype):

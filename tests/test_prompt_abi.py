@@ -221,3 +221,40 @@ def test_prepared_page_calls_keep_their_structs():
             assert c.args[0].contents.table == 0x7700 and c.args[0].contents.page_size == 16
     for a in (calls[0].args[1], calls[1].args[1], calls[2].args[0], calls[2].args[1]):
         assert [a[i].k for i in range(2)] == [0x7770, 0x7780]
+
+
+@pytest.fixture
+def on_host(monkeypatch):
+    """The bindings with host tensors: what they hand to the library, whose host checks come before any launch."""
+    monkeypatch.setattr(pld, "_need", lambda t, dtype, name, dims: t.stride())
+    monkeypatch.setattr(pld, "_on_one_device", lambda *a: None)
+    monkeypatch.setattr(pld, "_stream", lambda stream: 0)
+
+
+def _host_pool(seqs=3, per=4, pages=9):
+    """A PageTable, and no layers, of host tensors."""
+    table, refs = torch.full((seqs, per), -1, dtype=torch.int32), torch.zeros(pages + 4, dtype=torch.int32)
+    refs = refs[-refs.data_ptr() % 16 // 4:][:pages]
+    return pld.PageTable(table, refs, 16)
+
+
+@no_gpu
+@pytest.mark.parametrize("seqs", [1, 3])
+def test_compact_takes_the_stride_of_its_table(on_host, seqs):
+    """A new table whose rows overlap is refused, as its size is not what the kernels would write."""
+    p = _host_pool(seqs)
+    ints = lambda n: torch.zeros(n, dtype=torch.int32)
+    layers, ws = pld.PageLayers([], []), torch.zeros(1 << 16, dtype=torch.uint8)
+
+    def call(table_out):
+        return pld.pld_pages_compact(p, layers, ints(9), ints(1), ws, table_out=table_out, prepare=True)
+
+    assert call(ints(64)[:seqs * 12].view(seqs, 12)[:, :4]).args[6].value == 12
+    overlapping = [ints(4).expand(seqs, 4), ints(64).as_strided((seqs, 4), (3, 1))]
+    for t in overlapping:
+        c = call(t)
+        assert c.args[6].value == (4 if seqs == 1 else t.stride(0))
+        if seqs > 1:
+            with pytest.raises(pld.PLDError) as e:
+                c()
+            assert e.value.status == 1
