@@ -8,9 +8,10 @@ verification `weights` renews the attention rows that the next step ranks by.
 """
 import torch
 
-from . import (PLD_ROPE_HALVES, PageLayers, PageTable, pld_cache_attn, pld_cache_attn_rows,
-               pld_cache_attn_workspace_bytes, pld_cache_write, pld_cache_write_packed, pld_pages_compact,
-               pld_pages_copy, pld_pages_fork, pld_pages_free, pld_pages_take, pld_pages_workspace_bytes)
+from . import (PLD_ERR_INVALID, PLD_ROPE_HALVES, PageLayers, PageTable, PLDError, pld_cache_attn,
+               pld_cache_attn_rows, pld_cache_attn_workspace_bytes, pld_cache_write, pld_cache_write_packed,
+               pld_pages_compact, pld_pages_copy, pld_pages_fork, pld_pages_free, pld_pages_take,
+               pld_pages_workspace_bytes)
 
 
 def _under(stream, device):
@@ -144,12 +145,14 @@ class PagePool:
         count = max(1, count)
         if count <= self.most:
             return
+        need = pld_pages_workspace_bytes(self.pages, count)
+        if need == 0:                    # (no call takes so many)
+            raise PLDError("pld_pages_workspace_bytes", PLD_ERR_INVALID)
+        with _under(stream, self.refs.device):
+            workspace = torch.empty(need, dtype=torch.uint8, device=self.refs.device)
         if self.workspace is not None:
             self.grown.append(self.workspace)
-        with _under(stream, self.refs.device):
-            self.workspace = torch.empty(pld_pages_workspace_bytes(self.pages, count), dtype=torch.uint8,
-                                         device=self.refs.device)
-        self.most = count
+        self.workspace, self.most = workspace, count
 
     def take(self, seq, need, status, stream=None, prepare=False):
         """Pages for the positions below need[i] of sequences seq[i]."""

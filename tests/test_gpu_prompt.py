@@ -860,6 +860,21 @@ def test_compact_refuses_rows_that_overlap():
     assert (page_map == 9).all() and used.item() == 9
 
 
+def test_a_refused_page_call_leaves_the_pool_usable():
+    """More entries than a call takes are refused; the calls that follow are as without it."""
+    p = Pages(6, 4, 20)
+    many = d_i32([0] * (pld.PLD_MAX_PAGE_ENTRIES + 1))
+    for call in (lambda: p.pool.take(many, many, many), lambda: p.pool.fork(many, many, many, many), lambda: p.pool.free(many)):
+        with pytest.raises(pld.PLDError):
+            call()
+    assert p.take([0, 1], [40, 17]) == [0, 0]
+    with pytest.raises(pld.PLDError):
+        p.pool.take(many, many, many)
+    assert p.fork([0, 1], [2, 3], [40, 9]) == [0, 0]
+    p.free([0])
+    assert p.compact() > 0
+
+
 # ------------------------------------------------------------- a run of them
 @pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
 def test_prompts_forks_and_verification(dtype):

@@ -9,6 +9,7 @@ import pytest
 import torch
 
 import paper_2412_01447_amd as pld
+from paper_2412_01447_amd import cache
 from paper_2412_01447_amd.cache import PagePool
 from test_model_abi import BAD_CACHES, MIS, NULL, Q8, F, P, _cache
 
@@ -258,3 +259,24 @@ def test_compact_takes_the_stride_of_its_table(on_host, seqs):
             with pytest.raises(pld.PLDError) as e:
                 c()
             assert e.value.status == 1
+
+
+def test_a_refused_reservation_leaves_the_pool_as_it_was(on_host, monkeypatch):
+    """More sequences than a call takes: refused, and calls of fewer keep their workspace."""
+    monkeypatch.setattr(cache, "PageLayers", lambda *a: pld.PageLayers([], []))
+    k = torch.zeros(9, 16, 1, 64, dtype=torch.bfloat16)
+    pages = _host_pool()
+    pool = PagePool([k], [k], table=pages.table, refs=pages.refs)
+    for before in (0, 3):
+        if before:
+            pool.reserve(before)
+        kept, most = pool.workspace, pool.most
+        i = torch.zeros(pld.PLD_MAX_PAGE_ENTRIES + 1, dtype=torch.int32)
+        for call in (lambda: pool.reserve(len(i)), lambda: pool.take(i, i, i), lambda: pool.fork(i, i, i, i)):
+            with pytest.raises(pld.PLDError):
+                call()
+            assert pool.workspace is kept and pool.most == most and pool.grown == []
+    pool.reserve(2)
+    assert pool.workspace is kept
+    pool.reserve(pld.PLD_MAX_PAGE_ENTRIES)
+    assert pool.grown == [kept] and pool.workspace.numel() == pld.pld_pages_workspace_bytes(pool.pages, pld.PLD_MAX_PAGE_ENTRIES)
