@@ -285,11 +285,15 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
             for (int dt = 0; dt < kDT; ++dt) o[t][dt] *= f;
         }
     };
-    // Capped scores: the largest, from the largest product; and the scores themselves, after raise.
-    auto settle_top = [&](float (&top)[kQT], bool far) PLD_INLINE {
+    // Capped scores: the largest, from the largest product; and the scores themselves, after raise.  Where all
+    // the row's products with the keys from k0 on that it sees are -inf, they are scores of -cap and no masks.
+    auto settle_top = [&](float (&top)[kQT], bool far, int k0) PLD_INLINE {
         set_fit(true);
 #pragma unroll
-        for (int t = 0; t < kQT; ++t) top[t] = far && top[t] > -INFINITY ? capped(top[t], 0.f) : top[t] * near(top[t]);
+        for (int t = 0; t < kQT; ++t) {
+            const bool sees = lo[t] < k0 + 32 && hi[t] > k0;
+            top[t] = far && sees ? capped(top[t], 0.f) : top[t] * near(top[t]);
+        }
     };
     auto settle = [&](f32x16_t (&s)[kQT], bool far) PLD_INLINE {
 #pragma unroll
@@ -430,7 +434,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
             if (masked || (kCap && far)) {
 #pragma unroll
                 for (int t = 0; t < kQT; ++t) top[t] = largest(s[t]);
-                if (kCap) settle_top(top, far);
+                if (kCap) settle_top(top, far, k0);
                 too_high = score_high(top);
             }
             if (too_high) raise(top);
@@ -463,7 +467,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
             if (kCap && far) {
 #pragma unroll
                 for (int t = 0; t < kQT; ++t) top[t] = largest(s[t]);
-                settle_top(top, true);
+                settle_top(top, true, k0 + part * 32);
                 too_high = score_high(top);
             }
             if (too_high) raise(top);
@@ -546,7 +550,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
                 mask(k0, s0);
 #pragma unroll
                 for (int t = 0; t < kQT; ++t) top[t] = largest(s0[t]);
-                if (kCap) settle_top(top, true);
+                if (kCap) settle_top(top, true, k0);
                 raise(top);
                 if (kCap) settle(s0, true), mask(k0, s0);
                 uint32_t w[kQT][8];

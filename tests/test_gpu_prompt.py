@@ -228,6 +228,42 @@ def test_attn_infinite_capped_scores(D, sign, cap):
     say("infinite scores met", met)
 
 
+@pytest.mark.parametrize("D,Hq,heads,lens,cap,window", [
+    (64, 4, 2, [1, 31, 33, 64, 200], 30.0, 0), (128, 4, 2, [1, 31, 33, 64, 200], 30.0, 0), (256, 4, 2, [1, 31, 33, 64, 200], 30.0, 0),
+    (128, 6, 2, [700], 0.5, 0), (64, 2, 1, [700], 5.0, 40), (128, 32, 8, [2300], 30.0, 0), (256, 4, 1, [900], 5.0, 300)])
+def test_attn_capped_scores_of_minus_infinity(D, Hq, heads, lens, cap, window):
+    """Finite queries and keys whose products pass fp32's range: scores of the cap, of either sign from head to head,
+    where they are a row's first keys, all of a step, or all that it sees, as well."""
+    p = Prompt(lens, Hq, heads, D, at=2, pad=3, seed=12)
+    p.q[..., 0] = torch.tensor([-1.0, 1.0] * Hq)[:Hq].to(dev()) * 2.0 ** 65
+    p.k[..., 0] = 0.0
+    far = np.zeros(p.N, bool)
+    for i, (a, b) in enumerate(prompt_ref.sequences(p.starts, p.N)):
+        for lo, hi in ((0, 1 + 13 * i), (100, 170), (300, 650)):
+            far[a + lo:min(b, a + hi)] = True
+    p.k[torch.from_numpy(far).to(dev())] = 0.0
+    p.k[torch.from_numpy(far).to(dev()), :, 0] = 2.0 ** 65
+    o, L = p.attend(softcap=cap, window=window)
+    q, k, v, o, L = f64(p.q), f64(p.k), f64(p.v), f64(o), L.cpu().numpy()
+    near, met = {0, 1, 30, 31, 32, 33, 63, 64, 65, 100, 127, 128, 169, 170, 255, 256, 299, 300, 340, 649, 650}, 0
+    for a, b in prompt_ref.sequences(p.starts, p.N):
+        for r in range(a, b):
+            if b - a > 300 and r - a not in near and r % 97:
+                continue
+            lo = max(a, r + 1 - window) if window else a
+            for h in range(Hq):
+                kk, vv = k[lo:r + 1, h // (Hq // heads)], v[lo:r + 1, h // (Hq // heads)]
+                s = cap * np.tanh(kk @ q[r, h] * D ** -0.5 / cap)
+                size = np.abs(kk[:, 1:]) @ np.abs(q[r, h, 1:]) * D ** -0.5
+                tol = (D + 8) * U * size.max() + 16 * U * cap
+                want = s.max() + math.log(np.exp(s - s.max()).sum())
+                w = np.exp(s - want)
+                assert abs(L[r, h] - want) <= ref.lse_bound(tol, want, r + 1 - lo), (r, h, L[r, h], want)
+                assert np.all(np.abs(o[r, h] - w @ vv) <= ref.out_bound(w @ vv, w @ np.abs(vv), tol)), (r, h)
+                met += far[lo:r + 1].any()
+    assert met > 0
+
+
 def test_attn_many_empty_sequences():
     lens = np.zeros(60000, int)
     lens[[0, 7, 30000, 30001, 59998]] = [5, 70, 1, 40, 3]
