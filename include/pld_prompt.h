@@ -99,7 +99,9 @@ int pld_cache_write_packed(const pld_cache *cache, const uint16_t *q, int64_t q_
  * hold; a row's bits are the same from run to run.  Where a query, or a key or value that a row sees, is not finite, that head of
  * its out, and its lse, may be NaN as a whole.  The ranges of values and scores are
  * pld_cache_attn's: values up to 2^89, and a score above -1e29 for every row.  (A
- * block of rows that meets what is not finite is computed twice.)
+ * block of rows that meets what is not finite is computed twice.)  out is summed in fp32,
+ * 16 keys at a time: up to 2^22 keys of a row the roundings stay below that to bf16; of more,
+ * whose weights and values are alike, out may be off by more (2% at 2^24), lse not.
  * Errors: PLD_ERR_INVALID, PLD_ERR_ALIGN, PLD_ERR_LAUNCH.
  */
 int pld_prompt_attn(const uint16_t *q, int64_t q_row_stride, const uint16_t *k,

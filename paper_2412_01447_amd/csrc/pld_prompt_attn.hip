@@ -197,7 +197,8 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
     // ---- the products, of 32 keys at a time: `part` of a tile
     bf16x8_t qf[kQT][D / 16];
     f32x16_t o[kQT][kDT];
-    float mx[kQT], l[kQT];
+    float mx[kQT];
+    double l;   // of this lane's keys; with two tiles the whole of tile h's row
     const int c16 = lane & 15, odd16 = lane >> 4 & 1;
     int kat[2], vat[2];   // of even and odd steps of 16 elements; of the first and second eight of 16 rows
 #pragma unroll
@@ -280,7 +281,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
             const float all = pair_max(top[t]), mn = fmaf(all, c, -mx[t]) > kSlack ? all * c : mx[t];   // (as score_high)
             const float f = __builtin_amdgcn_exp2f(mx[t] - mn);
             mx[t] = mn;
-            l[t] *= f;
+            if (kQT == 1 || h == t) l *= (double)f;
 #pragma unroll
             for (int dt = 0; dt < kDT; ++dt) o[t][dt] *= f;
         }
@@ -307,16 +308,25 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
         }
     };
     // Weights 2^(s c - m), rounded to bf16 in pairs, as the product takes them: half a step (2^-8) of
-    // each term.  The sum is of the unrounded ones.
+    // each term.  The sum is of the unrounded ones: a lane's sixteen of a step in fp32, the steps' in 64
+    // bits.  Equal weights that are added one by one in fp32 round one way all along: 10^-4 of the sum at
+    // 32768 keys, 10^-2 at 4 million, 2 10^-6 of it this way (+-0.6% of the time, most 16384 rows).
     auto weigh = [&](float s, int t) PLD_INLINE {
-        const float w = __builtin_amdgcn_exp2f(fmaf(s, kCap ? near(s) : c, kCap ? -base[t] : -mx[t]));
-        l[t] += w;
-        return w;
+        return __builtin_amdgcn_exp2f(fmaf(s, kCap ? near(s) : c, kCap ? -base[t] : -mx[t]));
+    };
+    // the sums of a step; of two tiles, the rows' halves trade places, so that a lane has one sum and not two
+    auto add_up = [&](const float (&sum)[kQT]) PLD_INLINE {
+        if constexpr (kQT == 1) {
+            l += (double)sum[0];
+        } else {
+            const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum[0]), __float_as_uint(sum[1]), false, false);
+            l += (double)(__uint_as_float(a[0]) + __uint_as_float(a[1]));
+        }
     };
     auto begin = [&]() PLD_INLINE {
 #pragma unroll
         for (int t = 0; t < kQT; ++t) {
-            mx[t] = kNoMax, l[t] = 0.f;
+            mx[t] = kNoMax, l = 0.;
 #pragma unroll
             for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
@@ -371,7 +381,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
         // A slot is a product; what goes with it is a constant of its number z.
         constexpr int kZ = kX * kQT;                       // products of scores, and as many of values
         bf16x8_t vf[kLead];
-        float w0[kQT];
+        float w0[kQT], sum[kQT];
         uint32_t w[kQT][8];
         auto weights = [&](int z) PLD_INLINE {             // in the first three quarters
 #pragma unroll
@@ -379,6 +389,8 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
                 if (e * 3 * kX / 32 == z) {
                     const int r = e / kQT, t = e % kQT;
                     const float x = weigh(s[t][r], t);
+                    sum[t] = r ? sum[t] + x : x;
+                    if (e == 16 * kQT - 1) add_up(sum);
                     if (r % 2) w[t][r / 2] = pack_bf16(w0[t], x);
                     else w0[t] = x;
                 }
@@ -515,7 +527,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
         for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) x = fmaf(o[t][dt][r], 0.f, x);
-        odd |= lo[t] < hi[t] && (!(x == 0.f) || !(l[t] < INFINITY));
+        odd |= lo[t] < hi[t] && (!(x == 0.f) || (!(l < (double)INFINITY) && (kQT == 1 || h == t)));
     }
     if (__syncthreads_or(odd)) {
         begin();
@@ -554,13 +566,16 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
                 raise(top);
                 if (kCap) settle(s0, true), mask(k0, s0);
                 uint32_t w[kQT][8];
+                float sum[kQT];
 #pragma unroll
                 for (int t = 0; t < kQT; ++t)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const float w0 = weigh(s0[t][2 * i], t), w1 = weigh(s0[t][2 * i + 1], t);
+                        sum[t] = (i ? sum[t] : 0.f) + w0 + w1;
                         w[t][i] = pack_bf16(w0, w1);
                     }
+                add_up(sum);
 #pragma unroll
                 for (int x = 0; x < D / 16; ++x) {
                     const bf16x8_t f = value_operand(s_v[0], part * 2 + x / kDT, x % kDT);
@@ -574,8 +589,13 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
             __syncthreads();
         }
     }
-#pragma unroll
-    for (int t = 0; t < kQT; ++t) l[t] = pair_sum(l[t]);
+    float total[kQT];
+    if constexpr (kQT == 1) {
+        total[0] = pair_sum((float)l);
+    } else {
+        const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint((float)l), __float_as_uint((float)l), false, false);
+        total[0] = __uint_as_float(a[0]), total[1] = __uint_as_float(a[1]);
+    }
 
     // ---- out: a lane has four consecutive elements of every eight; the two lanes of a query trade
     // halves, so that each stores eight
@@ -586,7 +606,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
         if (lo[t] >= hi[t]) continue;   // (both lanes of a query alike)
         int row, head;
         row_of(t, over_again, row, head);
-        const float inv = 1.f / l[t];
+        const float inv = 1.f / total[t];
         uint16_t *dst = a.out + row * a.orow + (int64_t)head * D;
 #pragma unroll
         for (int dt = 0; dt < kDT; ++dt)
@@ -600,7 +620,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void prompt_attn_ker
                 *reinterpret_cast<uint4 *>(dst + dt * 32 + r * 2 + h * 8) = make_uint4(y0[0], y1[0], y0[1], y1[1]);
             }
         if (a.lse && h == 0)
-            a.lse[(int64_t)row * a.G * a.heads + head] = fmaf(mx[t], a.nat, __log2f(l[t]) * kLn2);
+            a.lse[(int64_t)row * a.G * a.heads + head] = fmaf(mx[t], a.nat, __log2f(total[t]) * kLn2);
     }
 }
 

@@ -180,6 +180,35 @@ def test_attn_falling_and_rising_scores():
         p.check(rows={0, 63, 64, 65, 128, 200, 255, 256, 320, 399})
 
 
+@pytest.mark.parametrize("D,B,cap", [(64, 1, 0), (64, 64, 0), (64, 1, 30.0), (128, 1, 0), (128, 300, 0), (128, 1, 30.0), (128, 300, 30.0),
+                                     (256, 1, 0), (256, 1, 30.0)])
+def test_attn_sums_of_equal_weights(D, B, cap):
+    """A long sequence whose first keys score 5 below many equal ones: weights that are summed one by one round
+    one way all along.  (Empty sequences behind it: the other block shapes.)"""
+    N, first = 100000, 40
+    p = Prompt([N] + [0] * (B - 1), 2, 1, D, seed=7)
+    p.q.fill_(1.0)
+    p.k.fill_(5 / math.sqrt(D))
+    p.k[:first] = 0.0
+    p.v.copy_(1 + torch.rand(p.v.shape, generator=torch.Generator(device=dev()).manual_seed(1), device=dev()))
+    o, L = p.attend(softcap=float(cap))
+    x = float(p.k[first, 0].double().sum()) * D ** -0.5
+    tol = (D + 8) * U * x
+    if cap:
+        x, tol = cap * math.tanh(x / cap), tol + 16 * U * cap
+    n = torch.arange(1, N + 1, dtype=torch.float64, device=dev())
+    low, high = n.clamp(max=first), (n - first).clamp(min=0)
+    total = low + high * math.exp(x)
+    v = p.v[:, 0].double().cumsum(0)
+    want = (v[:first][(low - 1).long()] + (v - v[first - 1]) * (high > 0)[:, None] * math.exp(x)) / total[:, None]
+    lse = total.log()
+    bound = tol + 8 * U * (lse.abs() + 1) + ((n + 1).log2() + 64) * 2 * U          # (model_ref.lse_bound)
+    assert ((L.double() - lse[:, None]).abs() <= bound[:, None]).all(), (L.double() - lse[:, None]).abs().max()
+    # model_ref.out_bound, and half a step of fp32 for each product of 16 keys
+    bound = (2.0 ** -8 * 2.02 + 4 * tol + 2.0 ** -16 + n / 16 * U)[:, None, None] * want[:, None]
+    assert ((o.double() - want[:, None]).abs() <= bound).all(), (o.double() / want[:, None] - 1).abs().max()
+
+
 def test_attn_in_place_and_without_lse():
     a = Prompt([100, 60], 8, 2, 128, 1, 3, seed=2, split=True)
     o, L = a.attend()
