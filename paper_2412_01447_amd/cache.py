@@ -135,9 +135,10 @@ class PagePool:
         table = torch.full((seqs, per), -1, dtype=torch.int32, device=c.k.device)
         refs = torch.zeros(c.k.shape[0], dtype=torch.int32, device=c.k.device)
         scales = (None, None) if c.k_scale is None else ([x.k_scale for x in caches], [x.v_scale for x in caches])
-        for x in caches:
+        pool = cls([x.k for x in caches], [x.v for x in caches], *scales, table=table, refs=refs)
+        for x in caches:                 # (not before the pool has found them alike)
             x.table = table
-        return cls([x.k for x in caches], [x.v for x in caches], *scales, table=table, refs=refs)
+        return pool
 
     def reserve(self, count, stream=None):
         """The workspace for calls of up to `count` sequences or forks (grown as needed: a caller that

@@ -940,6 +940,18 @@ def test_a_refused_page_call_leaves_the_pool_usable():
     assert p.compact() > 0
 
 
+@pytest.mark.parametrize("other", [dict(num_pages=9), dict(heads=1), dict(dtype=E4M3), dict(page_size=32)])
+def test_a_refused_pool_leaves_its_caches_as_they_were(other):
+    make = lambda **kw: PagedCache(**{**dict(B=2, max_len=40, heads=2, head_dim=64, page_size=16), **kw})
+    caches = [make(), make(**other)]
+    tables = [c.table for c in caches]
+    with pytest.raises(TypeError):
+        PagePool.of_caches(caches, seqs=3)
+    assert all(c.table is t for c, t in zip(caches, tables))
+    pool = PagePool.of_caches(caches[:1], seqs=3)
+    assert caches[0].table is pool.table and pool.table.shape == (3, 3)
+
+
 # ------------------------------------------------------------- a run of them
 @pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
 def test_prompts_forks_and_verification(dtype):

@@ -280,3 +280,11 @@ def test_a_refused_reservation_leaves_the_pool_as_it_was(on_host, monkeypatch):
     assert pool.workspace is kept
     pool.reserve(pld.PLD_MAX_PAGE_ENTRIES)
     assert pool.grown == [kept] and pool.workspace.numel() == pld.pld_pages_workspace_bytes(pool.pages, pld.PLD_MAX_PAGE_ENTRIES)
+
+
+def test_a_refused_pool_leaves_its_caches_as_they_were():
+    caches = [cache.PagedCache(2, 40, 1, 64, page_size=16, device="cpu") for _ in range(2)]     # (host tensors are refused)
+    tables = [c.table for c in caches]
+    with pytest.raises(TypeError):
+        PagePool.of_caches(caches, seqs=3)
+    assert all(c.table is t for c, t in zip(caches, tables))
