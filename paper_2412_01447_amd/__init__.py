@@ -915,6 +915,8 @@ class PageLayers:
         if any(x is not None and len(x) != self.count for x in self.tensors[1:]):
             raise TypeError("as many v_caches (and scales) as k_caches")
         every = [t for x in self.tensors if x for t in x]
+        if any(t is None for t in every):
+            raise TypeError("scales of every layer, or of none")
         for t in every:
             if not t.is_cuda or t.get_device() != every[0].get_device():
                 raise TypeError("the caches must be on one device: " + ", ".join(

@@ -113,7 +113,7 @@ class PagePool:
     Lists of [pages][slots][heads][D] tensors for keys and values, and of [pages][heads][slots]
     scales, one a layer (of_caches: PagedCache objects, which get the pool's table); table int32
     [seqs][pages], with -1 for entries that name no page, and refs int32 [pages], how many entries
-    name a page.  Left out, both are absent: such a pool only copies.
+    name a page.  Left out, both are absent: such a pool only copies.  A call has at least one entry.
     Calls on one pool follow each other (one stream, or events between): there is one workspace."""
 
     def __init__(self, k_caches, v_caches, k_scales=None, v_scales=None, table=None, refs=None):
@@ -140,13 +140,18 @@ class PagePool:
             x.table = table
         return pool
 
+    def _paged(self):
+        if self.pages is None:
+            raise TypeError("the pool has no table and references: it only copies")
+        return self.pages
+
     def reserve(self, count, stream=None):
         """The workspace for calls of up to `count` sequences or forks (grown as needed: a caller that
         captures a graph reserves before the capture).  One that is replaced is kept."""
         count = max(1, count)
         if count <= self.most:
             return
-        need = pld_pages_workspace_bytes(self.pages, count)
+        need = pld_pages_workspace_bytes(self._paged(), count)
         if need == 0:                    # (no call takes so many)
             raise PLDError("pld_pages_workspace_bytes", PLD_ERR_INVALID)
         with _under(stream, self.refs.device):
@@ -158,23 +163,23 @@ class PagePool:
     def take(self, seq, need, status, stream=None, prepare=False):
         """Pages for the positions below need[i] of sequences seq[i]."""
         self.reserve(seq.numel(), stream)
-        return pld_pages_take(self.pages, seq, need, status, self.workspace, stream=stream,
+        return pld_pages_take(self._paged(), seq, need, status, self.workspace, stream=stream,
                               prepare=prepare)
 
     def free(self, seq, keep=None, stream=None, prepare=False):
         """Sequences seq[i] give back what lies behind their first keep[i] positions (all)."""
-        return pld_pages_free(self.pages, seq, keep, stream=stream, prepare=prepare)
+        return pld_pages_free(self._paged(), seq, keep, stream=stream, prepare=prepare)
 
     def fork(self, src, dst, lens, status, stream=None, prepare=False):
         """Sequences dst[i] go on from the first lens[i] tokens of src[i]."""
         self.reserve(src.numel(), stream)
-        return pld_pages_fork(self.pages, self.layers, src, dst, lens, status, self.workspace,
+        return pld_pages_fork(self._paged(), self.layers, src, dst, lens, status, self.workspace,
                               stream=stream, prepare=prepare)
 
     def compact(self, page_map, used, table_out=None, refs_out=None, stream=None, prepare=False):
         """Pages in use move to the lowest indices; page_map and used say where and how many."""
         self.reserve(1, stream)
-        return pld_pages_compact(self.pages, self.layers, page_map, used, self.workspace,
+        return pld_pages_compact(self._paged(), self.layers, page_map, used, self.workspace,
                                  table_out=table_out, refs_out=refs_out, stream=stream, prepare=prepare)
 
     def copy_from(self, other, src, dst, slots=None, stream=None, prepare=False):

@@ -288,3 +288,21 @@ def test_a_refused_pool_leaves_its_caches_as_they_were():
     with pytest.raises(TypeError):
         PagePool.of_caches(caches, seqs=3)
     assert all(c.table is t for c, t in zip(caches, tables))
+
+
+def test_a_pool_that_only_copies_says_so(on_host, monkeypatch):
+    """Without a table and references: calls that need them are refused with the reason."""
+    monkeypatch.setattr(cache, "PageLayers", lambda *a: pld.PageLayers([], []))
+    i = torch.zeros(2, dtype=torch.int32)
+    pool = PagePool([i], [i])
+    for call in (lambda: pool.take(i, i, i), lambda: pool.free(i), lambda: pool.fork(i, i, i, i), lambda: pool.compact(i, i),
+                 lambda: pool.reserve(3)):
+        with pytest.raises(TypeError, match="only copies"):
+            call()
+    assert pool.workspace is None and pool.most == 0
+
+
+def test_scales_of_some_layers_alone_are_refused():
+    k = torch.zeros(1, 16, 1, 64, dtype=torch.bfloat16)
+    with pytest.raises(TypeError, match="scales"):
+        pld.PageLayers([k, k], [k, k], [k[..., 0], None], [k[..., 0], None])
