@@ -10,8 +10,9 @@
  * starts is int32 [B+1] on the device, non-decreasing with 0 <= starts[0] and
  * starts[B] <= N, and row r belongs to sequence b where starts[b] <= r <
  * starts[b+1]; sequences may be empty.  Rows before starts[0] and from starts[B]
- * on belong to none and are neither read nor written.  (Starts that break the
- * rule give unspecified rows, and no access outside the buffers.)
+ * on belong to none: they change no result and are not written, but like all N rows
+ * (and their positions) they have to be memory that can be read.  (Starts that break
+ * the rule give unspecified rows, and no access outside the buffers.)
  *
  * A prompt's layer: pld_cache_write_packed finishes queries and keys and puts
  * keys and values into the layer's cache, pld_prompt_attn attends, straight from
