@@ -257,6 +257,30 @@ def test_attn_infinite_capped_scores(D, sign, cap):
     say("infinite scores met", met)
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("sign,cap", [(1, 5.0), (-1, 0.5)])
+def test_attn_every_infinite_score_is_capped(D, sign, cap):
+    """All rows that see a key which makes scores infinite of either sign: the cap's weight, and nothing of a mask's."""
+    p = Prompt([200], Hq=4, heads=2, D=D, seed=8)
+    p.k[70, :, 3] = sign * INF
+    o, L = p.attend(softcap=cap)
+    q, k, v, o, L = f64(p.q), f64(p.k), f64(p.v), f64(o), L.cpu().numpy()
+    assert (q[70:, :, 3] != 0).all() and (q[70:, :, 3] > 0).any() and (q[70:, :, 3] < 0).any()
+    met = 0
+    for r in range(70, 200):
+        for h in range(4):
+            kk, vv = k[:r + 1, h // 2], v[:r + 1, h // 2]
+            s = cap * np.tanh(kk @ q[r, h] * D ** -0.5 / cap)
+            size = np.abs(np.delete(kk, 70, 0)) @ np.abs(q[r, h]) * D ** -0.5
+            tol = (D + 8) * U * size.max() + 16 * U * cap
+            want = s.max() + math.log(np.exp(s - s.max()).sum())
+            w = np.exp(s - want)
+            assert abs(L[r, h] - want) <= ref.lse_bound(tol, want, r + 1), (r, h, L[r, h], want)
+            assert np.all(np.abs(o[r, h] - w @ vv) <= ref.out_bound(w @ vv, w @ np.abs(vv), tol)), (r, h)
+            met += 1
+    assert met == 130 * 4
+
+
 @pytest.mark.parametrize("D,Hq,heads,lens,cap,window", [
     (64, 4, 2, [1, 31, 33, 64, 200], 30.0, 0), (128, 4, 2, [1, 31, 33, 64, 200], 30.0, 0), (256, 4, 2, [1, 31, 33, 64, 200], 30.0, 0),
     (128, 6, 2, [700], 0.5, 0), (64, 2, 1, [700], 5.0, 40), (128, 32, 8, [2300], 30.0, 0), (256, 4, 1, [900], 5.0, 300)])
@@ -579,6 +603,49 @@ def test_write_many_sequences_and_captured():
         assert w.check() == lens.sum()
 
 
+@pytest.mark.parametrize("kw", [
+    # two heads a lane group, and four: head counts that they do not divide, groups that straddle queries, keys and values
+    dict(lens=[1500, 1, 0, 1399], Hq=7, heads=1, D=128, axes=3, sections=turns(128, 3), norm=True, at=3, pad=5),
+    dict(lens=[700, 560], Hq=6, heads=3, D=256, axes=2, sections=sections(256, 2), halves=False, dtype=E4M3, page=32),
+    dict(lens=[2400, 30, 1200], Hq=21, heads=7, D=256, axes=3, sections=turns(256, 3), norm=True, dtype=E4M3, pad=1, page=64),
+    dict(lens=[3000, 700], Hq=26, heads=13, D=256, axes=1, rot=128, norm=True, at=1, halves=False, page=128)])
+def test_write_several_heads_a_lane_group(kw):
+    """Many rows, of which some are not stored: against 64 bits, and by the bits of calls of few rows (a head a lane
+    group) into the same cache; in place as well."""
+    w = Write(seed=21, n_pos=4000, **kw)
+    lanes = w.N * (kw["Hq"] + 2 * kw["heads"]) * w.D // 8
+    assert lanes >= 4000000 if kw["Hq"] > 20 else 400000 <= lanes < 4000000        # (where the forms begin)
+    # an inner page of the longest sequence, and positions out of the table of angles
+    lost = (len(w.table[0]) // 2, w.starts[0] + 5, w.starts[0] + 900 if kw["lens"][0] > 900 else w.starts[1] + 9)
+    w.table[0, lost[0]] = -1
+    w.cache.table = d_i32(w.table)
+    w.positions[0, lost[1]], w.positions[0, lost[2]] = -1, 4000
+    q, k = w.q.clone(), w.k.clone()
+    w.write()
+    assert sum(kw["lens"]) - w.cache.page_size - 2 <= w.check() < sum(kw["lens"])
+    outs = lambda: [bits(t) for t in (w.q_out, w.k_out, w.cache.k, w.cache.v, w.cache.k_scale, w.cache.v_scale) if t is not None]
+    big = outs()
+    for t in (w.cache.k, w.cache.v):
+        t.view(torch.int16 if t.dtype == torch.bfloat16 else torch.uint8).zero_()
+    w.q_out.fill_(7.0), w.k_out.fill_(7.0)
+    step = 390000 * w.N // lanes
+    for b, (a, e) in enumerate(prompt_ref.sequences(w.starts, w.N)):
+        for x in range(a, e, step):
+            y = min(e, x + step)
+            w.cache.table = d_i32(w.table[b:b + 1])
+            w.write(q=q[x:y], k=k[x:y], v=w.v[x:y], starts=d_i32([0, y - x]), first=d_i32([w.first[b] + x - a]), q_out=w.q_out[x:y],
+                    k_out=w.k_out[x:y], positions=w.positions[:, x:y].contiguous())
+    for x, y in zip(big, outs()):
+        assert np.array_equal(x, y)
+    w.cache.table = d_i32(w.table)
+    w.write(q_out=w.q, k_out=w.k)
+    for x, y, before in ((w.q, big[0], q), (w.k, big[1], k)):
+        assert np.array_equal(bits(x)[w.starts[0]:w.starts[-1]], y[w.starts[0]:w.starts[-1]])
+        assert torch.equal(x[:w.starts[0]], before[:w.starts[0]]) and torch.equal(x[w.starts[-1]:], before[w.starts[-1]:])
+    for x, y in zip(big[2:], outs()[2:]):
+        assert np.array_equal(x, y)
+
+
 def test_write_refusals():
     w = Write([10], axes=2, sections=turns(64, 2))
     for kw in (dict(q=w.q[:, :1]), dict(starts=w.d_starts[:1]), dict(positions=w.positions.long()), dict(positions=w.positions[:, :5]),
@@ -832,6 +899,80 @@ def test_copy_between_layouts(a, b, dtype):
         torch.cuda.synchronize()
         for got, t in zip(y.contents(), want):
             assert np.array_equal(got, t)
+
+
+def _layers(layout, dtype, P, page, heads, D, seed):
+    """Two layers' keys, values and scales in one of several layouts."""
+    g = torch.Generator(device=dev()).manual_seed(seed)
+
+    def rows(*shape):
+        return torch.randint(0, 120, shape, generator=g, device=dev(), dtype=torch.uint8).view(E4M3) if dtype == E4M3 else \
+            torch.randn(shape, generator=g, device=dev()).to(dtype)
+
+    def pair():
+        if layout == "heads":                                  # slot by slot within a head
+            return [rows(P, heads, page, D).transpose(1, 2) for _ in range(2)]
+        if layout == "pairs":                                  # keys and values side by side, page by page
+            both = rows(P, 2, page, heads, D)
+            return [both[:, 0], both[:, 1]]
+        if layout == "slots together":                         # keys and values side by side, slot by slot
+            both = rows(P, page, 2, heads, D)
+            return [both[:, :, 0], both[:, :, 1]]
+        return [rows(P, page, heads, D) for _ in range(2)]
+    pairs = [pair() for _ in range(2)]
+    k, v = [x[0] for x in pairs], [x[1] for x in pairs]
+    scales = [[torch.rand(P, heads, page, generator=g, device=dev()) for _ in range(2)] for _ in range(2)] if dtype == E4M3 else (None, None)
+    return k, v, *scales
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
+@pytest.mark.parametrize("a,b", [("slots", "heads"), ("heads", "heads"), ("heads", "slots"), ("pairs", "slots together"),
+                                 ("slots together", "heads"), ("slots", "pairs")])
+def test_copy_of_large_pages(a, b, dtype):
+    """Pages of several parts of 32 KB, whole and partly, between layouts that are no single run of bytes."""
+    page, heads, D = 256, 5, 128
+    x, y = _layers(a, dtype, 7, page, heads, D, 1), _layers(b, dtype, 6, page, heads, D, 2)
+    src, dst, slots = [6, 0, 3, 5, 2], [0, 5, 2, 4, 1], [256, 255, 65, 1, 0]
+    for s in (slots, None):
+        want = [[bits(t) for t in list_] for list_ in y if list_]
+        for from_, to in zip([list_ for list_ in x if list_], want):
+            for f, t in zip((bits(f) for f in from_), to):
+                for i, j, m in zip(src, dst, s or [page] * 5):
+                    if t.ndim == 4:
+                        t[j, :m] = f[i, :m]
+                    else:
+                        t[j, :, :m] = f[i, :, :m]
+        PagePool(*y).copy_from(PagePool(*x), d_i32(src), d_i32(dst), None if s is None else d_i32(s))
+        torch.cuda.synchronize()
+        for got, to in zip([list_ for list_ in y if list_], want):
+            for g, t in zip(got, to):
+                assert np.array_equal(bits(g), t)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
+@pytest.mark.parametrize("layout", ["heads", "pairs", "slots together"])
+def test_fork_and_compact_large_pages(layout, dtype):
+    """The tail of a fork and a compaction's moves, of several parts of 32 KB a page."""
+    page, heads, D = 256, 5, 128
+    x = _layers(layout, dtype, 8, page, heads, D, 3)
+    contents = lambda: [bits(t) for list_ in x if list_ for t in list_]
+    pool = PagePool(*x, table=d_i32([[6, 7, -1], [-1] * 3, [1, -1, -1]]), refs=d_i32([0, 1, 0, 0, 0, 0, 1, 1]))
+    status = d_i32([9])
+    for call, moves in ((lambda: pool.fork(d_i32([0]), d_i32([1]), d_i32([page + 77]), status), [(7, 0, 77)]),
+                        (lambda: pool.compact(d_i32([0] * 8), d_i32([0])), [(6, 2, page), (7, 3, page)])):
+        want = contents()
+        for t in want:
+            for i, j, m in moves:
+                if t.ndim == 4:
+                    t[j, :m] = t[i, :m]
+                else:
+                    t[j, :, :m] = t[i, :, :m]
+        call()
+        torch.cuda.synchronize()
+        for g, t in zip(contents(), want):
+            assert np.array_equal(g, t)
+    assert status.item() == 0 and pool.table.tolist() == [[2, 3, -1], [2, 0, -1], [1, -1, -1]]
+    assert pool.refs.tolist() == [1, 1, 2, 1, 0, 0, 0, 0]
 
 
 def test_copy_far_pages():

@@ -64,3 +64,11 @@ def test_prompt_lookup_blocks_per_cu(kernels):
     assert sel == {1024: 2, 512: 4, 256: 8}
     one = [blocks_per_cu(k) for n, k in kernels.items() if "draft_prefix_kernel" in n]
     assert sorted(one) == [1, 2]
+
+
+def test_prompt_attention_blocks_per_cu(kernels):
+    """What the choice of block shapes counts on: two blocks of 128 rows a CU, or one of 256, with heads of 128,
+    three and two with heads of 64, one with heads of 256."""
+    got = {re.sub(r"\D+", " ", n[len("prompt_attn_kernel"):]).strip(): blocks_per_cu(k) for n, k in kernels.items() if n.startswith("prompt_attn")}
+    assert got == {"64 2 4 0": 2, "64 1 4 0": 3, "64 1 4 1": 3, "128 1 4 0": 2, "128 1 4 1": 2, "128 1 8 0": 1, "128 1 8 1": 1,
+                   "256 1 4 0": 1, "256 1 4 1": 1}
